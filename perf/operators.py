@@ -1,0 +1,510 @@
+"""A gated recurrent layer in training and serving, as measurable cases.
+
+Six kinds of call, each through the public binding where `own` is set and in
+elementary torch operations where it is not:
+
+  fwd     the gated linear recurrence over whole sequences,
+            r = sigmoid(ga), i = sigmoid(gi), s = rate * r, a = exp(-s),
+            h_t = a_t h_{t-1} + sqrt(1 - a_t^2) i_t x_t,   y = h,
+          channel by channel, from given states; a gate logit ga <= -64 holds
+          the state (a = 1, no input, whatever x is: masked rows)
+  bwd     its vector-Jacobian product from the inputs themselves
+  ckpt    forward and backward of a training step that keeps x, ga and gi
+          between the two in 8 bits instead of 16 (one exponent for 32 rows of
+          a channel; the states are recomputed from the kept values, from the
+          exact state that enters each chunk of 128 rows)
+  step    one generated token for each of a batch of sequences, their states
+          rows of a pool
+  pack    activations brought to the 8-bit form and read back
+  wgrad   the weight gradient of a token projection P = W u, dW = dP^T u, from
+          the activations u in their 8-bit form
+
+Sizes are those of the named workloads (fsa-perm and timeseries: 1024 state
+entries; hybrid-lm: 4096 features, 32 heads of 128 complex entries), odd ones of
+the test suite, or generic.  draw() spreads the same kinds over the sizes in
+between.
+"""
+import math
+
+import torch
+
+own = False
+DEV = "cuda"
+HOLD = -64.0   # a gate logit at or under this one holds the state
+CHUNK = 128    # rows between two saved states
+BLOCK = 32     # rows that share an exponent in the 8-bit form
+
+
+def listed():
+    return [
+        # the next 64 tokens of one prompt, state carried: latency counts
+        dict(name="fwd-short", kind="fwd", io="bf16", layout="dense", S=1, T=64, C=1024, state=True, masked=False),
+        # the state-tracking layer's training shape, 16 sequences of 2048
+        dict(name="fwd-fsa", kind="fwd", io="bf16", layout="dense", S=16, T=32768, C=1024, state=False, masked=False),
+        # its backward pass
+        dict(name="bwd-fsa", kind="bwd", io="bf16", layout="dense", S=16, T=32768, C=1024, state=False, masked=False),
+        # packed sequences of very different lengths, empty ones and masked rows among them, an odd
+        # number of channels, rows behind the last sequence, fp32
+        dict(name="bwd-ragged-fp32", kind="bwd", io="fp32", layout="ragged", S=61, T=20011, C=777, state=True,
+             masked=True),
+        # a training step of few very long sequences, activations kept in 8 bits
+        dict(name="ckpt-timeseries", kind="ckpt", io="bf16", layout="dense", S=8, T=144000, C=1024, state=False,
+             masked=False),
+        # the same on packed sequences with an odd number of channels
+        dict(name="ckpt-ragged", kind="ckpt", io="bf16", layout="ragged", S=23, T=9001, C=513, state=True, masked=True),
+        # one token of one sequence: latency only
+        dict(name="step-one", kind="step", io="bf16", S=1, pool=1, C=1024),
+        # batched serving, 512 sequences of a pool of 1024
+        dict(name="step-serving", kind="step", io="bf16", S=512, pool=1024, C=4096),
+        # the features of 32768 tokens of the hybrid-lm layer
+        dict(name="pack-hybrid", kind="pack", io="bf16", T=32768, C=4096),
+        # ragged edges of both axes, fp32
+        dict(name="pack-odd-fp32", kind="pack", io="fp32", T=1001, C=333),
+        # the weight gradient of one of the hybrid-lm layer's projections over 32768 tokens; the largest product
+        dict(name="wgrad-hybrid", kind="wgrad", T=32768, M=8192, Dm=4096),
+        # a small layer on 1000 tokens: few output tiles, a long sum, a ragged end
+        dict(name="wgrad-small", kind="wgrad", T=1000, M=528, Dm=288),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["fwd", "bwd", "ckpt", "step", "pack", "wgrad"])
+    io = rng.choice(["bf16", "bf16", "fp32"])
+    if kind in ("fwd", "bwd", "ckpt"):
+        C, T = _log(rng, 1, 4096), _log(rng, 1, 65536)
+        T = max(1, min(T, (1 << 25) // C))
+        layout = rng.choice(["dense", "ragged"])
+        S = _log(rng, 1, min(96, T))
+        if layout == "dense":
+            T = T // S * S
+        return dict(kind=kind, io=io, layout=layout, S=S, T=T, C=C, state=rng.random() < 0.5,
+                    masked=rng.random() < 0.5)
+    if kind == "step":
+        C, S = _log(rng, 8, 8192), _log(rng, 1, 2048)
+        S = max(1, min(S, (1 << 23) // C))
+        return dict(kind=kind, io=io, S=S, pool=S + rng.randrange(0, S + 1), C=C)
+    if kind == "pack":
+        C, T = _log(rng, 1, 8192), _log(rng, 1, 65536)
+        return dict(kind=kind, io=io, T=max(1, min(T, (1 << 26) // C)), C=C)
+    M, Dm, T = 8 * _log(rng, 2, 1024), 32 * _log(rng, 1, 128), _log(rng, 1, 65536)
+    return dict(kind=kind, T=max(1, min(T, (1 << 39) // (M * Dm))), M=M, Dm=Dm)
+
+
+def _type(case):
+    return torch.bfloat16 if case["io"] == "bf16" else torch.float32
+
+
+def _bounds(case, seed):
+    """First rows of the packed sequences, and their end: random cuts, some equal (empty sequences), a few rows left
+    behind the last sequence."""
+    g = torch.Generator().manual_seed(seed * 7919 + 5)
+    T, S = case["T"], case["S"]
+    end = T - min(T - 1, 5) if T > 8 else T
+    cuts = torch.randint(0, end + 1, (S - 1,), generator=g).sort().values
+    if S > 3:
+        cuts[S // 2] = cuts[S // 2 - 1]
+    return [0] + cuts.tolist() + [end]
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+
+    def normal(*shape, std=1.0, dtype=torch.float32):
+        return (torch.randn(shape, generator=g, device=DEV) * std).to(dtype)
+
+    kind = case["kind"]
+    if kind == "wgrad":
+        T, M, Dm = case["T"], case["M"], case["Dm"]
+        u = normal(T, Dm, dtype=torch.bfloat16) * torch.exp(normal(Dm, std=0.5)).to(torch.bfloat16)
+        q, e = _hold8(u)
+        return dict(kind=kind, dP=normal(T, M, std=0.02, dtype=torch.bfloat16), q=q, e=e)
+    t = _type(case)
+    if kind == "pack":
+        u = normal(case["T"], case["C"]) * torch.exp(normal(case["C"], std=0.5))
+        return dict(kind=kind, io=t, u=u.to(t))
+    C = case["C"]
+    # decay rates of channels that remember from a few steps to several thousand
+    st = dict(kind=kind, rate=8 * torch.exp(torch.empty(C, device=DEV).uniform_(math.log(1e-3), math.log(0.1),
+                                                                                generator=g)))
+    n = case["S"] if kind == "step" else case["T"]
+    # x, ga and gi are the three parts of one projection's rows, as a layer has them
+    rows = normal(n, 3 * C)
+    if kind == "step":
+        rows = rows.to(t)
+        st["x"], st["ga"], st["gi"] = rows[:, :C], rows[:, C:2 * C], rows[:, 2 * C:]
+        order = torch.randperm(case["pool"], generator=g, device=DEV)
+        st["slots"] = order[:n].to(torch.int32)
+        st["h"] = normal(case["pool"], C)
+        st["h_out"] = st["h"].clone()
+        return st
+    if case["masked"]:  # padded rows: the lowest value or -inf in the gate, anything in the others
+        pad = torch.rand(n, generator=g, device=DEV) < 0.04
+        low = torch.rand(n, generator=g, device=DEV) < 0.5
+        rows[pad & low, C:2 * C] = torch.finfo(t).min
+        rows[pad & ~low, C:2 * C] = -math.inf
+        rows[pad, :C] = math.inf
+        rows[pad & low, 2 * C:] = math.nan
+    rows = rows.to(t)
+    st["x"], st["ga"], st["gi"] = rows[:, :C], rows[:, C:2 * C], rows[:, 2 * C:]
+    S = case["S"]
+    if case["layout"] == "ragged":
+        st["cu"] = torch.tensor(_bounds(case, seed), dtype=torch.int32, device=DEV)
+        st["T_used"] = _bounds(case, seed)[-1]
+    else:
+        st["cu"], st["T_used"] = None, n
+    st["L"] = n // S
+    st["S"] = S
+    st["h0"] = normal(S, C) if case["state"] else None
+    if kind != "fwd":
+        st["dy"] = normal(n, C, dtype=t)
+        st["dh_final"] = normal(S, C) if case["state"] else None
+    if kind == "bwd":  # a backward pass finds the states that its forward pass saved
+        a, b, _ = _gates(st["x"], st["ga"], st["gi"], st["rate"])
+        st["saved"] = _saved(_scan(*_begin(st, a, b)), n)
+    return st
+
+
+# ---- the plain forms -------------------------------------------------------------------------------------------------
+
+
+def _power(e):
+    """2^e as float32, from its bits: exp2 need not be exact, and a value halfway between two codes shows it."""
+    return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
+
+
+def _hold8(u):
+    """The 8-bit form of u [T, C]: whole numbers q [T, C] and, for 32 rows of a column, the exponent e of the smallest
+    power of two with 127 * 2^e >= the largest magnitude: u = q * 2^e.  -inf keeps the code -128."""
+    T, C = u.shape
+    n = -(-T // BLOCK)
+    v = torch.zeros(n * BLOCK, C, device=u.device)
+    v[:T] = u
+    v = v.reshape(n, BLOCK, C)
+    low = v == -math.inf
+    m, k = torch.frexp(torch.where(low, 0.0, v).abs().amax(1))
+    e = torch.where(m <= 127 / 128, k - 7, k - 6).clamp(min=-126)
+    e = torch.where(m == 0, -126, e)
+    q = torch.round(torch.where(low, 0.0, v) * _power(-e)[:, None])
+    q = torch.where(low, -128.0, q).reshape(n * BLOCK, C)[:T]
+    return q.to(torch.int8), e.to(torch.int8)
+
+
+def _value8(q, e):
+    v = q.float() * _power(e).repeat_interleave(BLOCK, 0)[:q.shape[0]]
+    return torch.where(q == -128, -math.inf, v)
+
+
+def _gates(x, ga, gi, rate):
+    """a and the input term of every row, and what the backward pass needs of them: r, i, beta, s and the held rows."""
+    x, ga, gi = x.float(), ga.float(), gi.float()
+    hold = ga <= HOLD
+    r = torch.where(hold, 0.0, torch.sigmoid(ga))
+    i = torch.sigmoid(gi)
+    s = rate * r
+    beta = torch.sqrt(-torch.expm1(-2 * s))
+    return torch.exp(-s), torch.where(hold, 0.0, beta * i * x), (x, r, i, s, beta, hold)
+
+
+def _scan(a, b):
+    """h_t = a_t h_{t-1} + b_t along dim 0 from a zero state: pairs of rows are joined into one, the half as long
+    sequence is solved the same way, and gives every second row."""
+    n = b.shape[0]
+    if n == 1:
+        return b
+    m = n // 2
+    a1 = a[1:2 * m:2]
+    odd = _scan(a[0:2 * m:2] * a1, a1 * b[0:2 * m:2] + b[1:2 * m:2])
+    h = torch.empty_like(b)
+    h[0] = b[0]
+    h[1:2 * m:2] = odd
+    h[2::2] = a[2::2] * odd[:(n - 1) // 2] + b[2::2]
+    return h
+
+
+def _sequence(st):
+    """(sequence of each row up to the last sequence's end, whether a row begins one, whether it ends one, lengths)."""
+    if st["cu"] is None:
+        ids = torch.arange(st["T_used"], device=DEV) // st["L"]
+        return ids, torch.full((st["S"],), st["L"], device=DEV)
+    cu = st["cu"].long()
+    n = cu.diff()
+    return torch.repeat_interleave(torch.arange(st["S"], device=DEV), n, output_size=st["T_used"]), n
+
+
+def _firsts(st):
+    """Rows that begin a sequence, rows that end it, and which sequence it is; empty sequences have none."""
+    ids, n = _sequence(st)
+    change = torch.ones(ids.shape[0] + 1, dtype=torch.bool, device=DEV)
+    change[1:-1] = ids[1:] != ids[:-1]
+    first, last = change[:-1].nonzero()[:, 0], change[1:].nonzero()[:, 0]
+    return first, last, ids[first]
+
+
+def _begin(st, a, b):
+    """a, b of the rows in sequences, with the states that the sequences begin from put into their first rows."""
+    a, b = a[:st["T_used"]].clone(), b[:st["T_used"]].clone()
+    first, _, ids = _firsts(st)
+    if st["h0"] is not None:
+        b[first] += a[first] * st["h0"][ids]
+    a[first] = 0
+    return a, b
+
+
+def _saved(h, rows):
+    """The state before each chunk of CHUNK of the rows (zero before the first and behind the last sequence; a sequence
+    that begins with a chunk does not read it)."""
+    saved = torch.zeros(-(-rows // CHUNK), h.shape[1], device=h.device)
+    last = h[CHUNK - 1::CHUNK][:saved.shape[0] - 1]
+    saved[1:1 + last.shape[0]] = last
+    return saved
+
+
+def _final(st, h):
+    _, last, ids = _firsts(st)
+    out = torch.zeros(st["S"], h.shape[1], device=DEV) if st["h0"] is None else st["h0"].clone()
+    out[ids] = h[last]
+    return out
+
+
+def _plain_bwd(st, x, ga, gi, saved):
+    a, b, kept = _gates(x, ga, gi, st["rate"])
+    n = st["T_used"]
+    first, last, ids = _firsts(st)
+    x, r, i, s, beta, hold = (v[:n] for v in kept)
+    # the states from the saved ones: every chunk begins anew
+    a_in, b_in = _begin(st, a, b)
+    head = torch.arange(0, n, CHUNK, device=DEV)
+    saved = saved[:head.shape[0]]
+    b_in[head] += a_in[head] * saved
+    a_in[head] = 0
+    h = _scan(a_in, b_in)
+    before = torch.empty_like(h)
+    before[1:] = h[:-1]
+    before[head] = saved
+    before[first] = 0 if st["h0"] is None else st["h0"][ids]
+    # g_t = dy_t + a_{t+1} g_{t+1}, backwards
+    a = a[:n]
+    after = torch.zeros_like(a)
+    after[:-1] = a[1:]
+    after[last] = 0
+    dy = st["dy"][:n].float().clone()
+    if st["dh_final"] is not None:
+        dy[last] += st["dh_final"][ids]
+    g = _scan(after.flip(0), dy.flip(0)).flip(0)
+    ds = g * (torch.where(hold, 0.0, i * x * (s * a * a / beta)) - s * a * before)
+    ds = torch.where(hold, 0.0, ds)
+    dx = torch.where(hold, 0.0, g * beta * i)
+    dgi = torch.where(hold, 0.0, dx * x * (1 - i))
+    dh0 = torch.zeros(st["S"], a.shape[1], device=DEV) if st["dh_final"] is None else st["dh_final"].clone()
+    dh0[ids] = a[first] * g[first]
+    t = st["dy"].dtype
+    return dx.to(t), (ds * (1 - r)).to(t), dgi.to(t), ds.sum(0) / st["rate"], dh0
+
+
+def _plain(st):
+    kind = st["kind"]
+    if kind == "wgrad":
+        return st["dP"].float().t() @ _value8(st["q"], st["e"])
+    if kind == "pack":
+        return _value8(*_hold8(st["u"])).to(st["io"])
+    a, b, _ = _gates(st["x"], st["ga"], st["gi"], st["rate"])
+    if kind == "step":
+        rows = st["slots"].long()
+        h = a * st["h"][rows] + b
+        st["h_out"][rows] = h
+        return dict(y=h.to(st["x"].dtype), h=st["h_out"])
+    if kind == "bwd":
+        return dict(zip(("dx", "dga", "dgi", "drate", "dh0"), _plain_bwd(st, st["x"], st["ga"], st["gi"], st["saved"])))
+    h = _scan(*_begin(st, a, b))
+    out = dict(y=h.to(st["x"].dtype), h_final=_final(st, h))
+    if kind == "ckpt":
+        low = st["ga"].float() <= HOLD
+        kept = (_value8(*_hold8(torch.where(low, 0.0, st["x"].float()))),
+                _value8(*_hold8(torch.where(low, -math.inf, st["ga"].float()))),
+                _value8(*_hold8(torch.where(low, 0.0, st["gi"].float()))))
+        out |= zip(("dx", "dga", "dgi", "drate", "dh0"), _plain_bwd(st, *kept, _saved(h, st["x"].shape[0])))
+    return out
+
+
+# ---- the framework's operators ---------------------------------------------------------------------------------------
+
+
+def _rows(st, v):
+    """A row tensor as the binding takes it: [B, L, C] for sequences of one length, [T, C] for packed ones."""
+    return v.unflatten(0, (st["S"], st["L"])) if st["cu"] is None else v
+
+
+def _own(st):
+    from paper_2605_19150_amd import pdssm
+
+    kind = st["kind"]
+    if kind == "wgrad":
+        return pdssm.project_wgrad(st["dP"], (st["q"], st["e"]))
+    if kind == "pack":
+        return pdssm.unpack8(pdssm.pack8(st["u"]), dtype=st["io"])
+    if kind == "step":
+        h, y = pdssm.gated_step(st["x"], st["ga"], st["gi"], st["rate"], st["h"], slots=st["slots"], out=st["h_out"],
+                                check=False)
+        return dict(y=y, h=h)
+    n = st["T_used"]
+    x, ga, gi = (_rows(st, st[k]) for k in ("x", "ga", "gi"))
+    names = ("dx", "dga", "dgi", "drate", "dh0")
+    if kind == "bwd":
+        got = pdssm.gated_bwd(x, ga, gi, st["rate"], st["saved"], _rows(st, st["dy"]), cu=st["cu"], h0=st["h0"],
+                              dh_final=st["dh_final"], check=False)
+        out = dict(zip(names, got))
+    else:
+        got = pdssm.gated_fwd(x, ga, gi, st["rate"], cu=st["cu"], h0=st["h0"], hold8=kind == "ckpt", check=False)
+        out = dict(y=got[0], h_final=got[1])
+        if kind == "ckpt":
+            back = pdssm.gated_bwd(*got[3], st["rate"], got[2], _rows(st, st["dy"]), cu=st["cu"], h0=st["h0"],
+                                   dh_final=st["dh_final"], check=False)
+            out |= zip(names, back)
+    # rows behind the last sequence are not written
+    return {k: v.flatten(0, 1)[:n] if v.dim() == 3 else v[:n] if k in ("y", "dx", "dga", "dgi") else v
+            for k, v in out.items()}
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+# ---- the definition in 64 bits ---------------------------------------------------------------------------------------
+
+
+def _exact_powers():
+    """2^k at place k, for k from -127 to 127 (negative places count from the end)."""
+    return torch.tensor([2.0 ** k for k in [*range(128), *range(-127, 0)]], dtype=torch.float64, device=DEV)
+
+
+def _exact_kept(v):
+    """The values that the 8-bit form of v stands for, from its definition."""
+    v = v.double()
+    T, C = v.shape
+    out, powers = torch.empty_like(v), _exact_powers()
+    for k in range(0, T, BLOCK):
+        w = v[k:k + BLOCK]
+        fine = w > -math.inf
+        top = torch.where(fine, w, 0.0).abs().amax(0) / 127
+        m, p = torch.frexp(top)
+        e = torch.where(m > 0.5, p, p - 1).clamp(min=-126)
+        step = torch.where(top > 0, powers[e.long()], torch.ones_like(top))
+        out[k:k + BLOCK] = torch.where(fine, torch.round(w / step) * step, w)
+    return out
+
+
+def _exact_gates(x, ga, gi, rate):
+    x, ga, gi = x.double(), ga.double(), gi.double()
+    held = ~(ga > HOLD)
+    r = torch.where(held, torch.zeros_like(ga), 1 / (1 + torch.exp(-ga)))
+    i = 1 / (1 + torch.exp(-gi))
+    s = r * rate.double()
+    x, i = x.masked_fill(held, 0.0), i.masked_fill(held, 0.0)
+    return x, r, i, s, torch.exp(-s), torch.sqrt(-torch.expm1(-2 * s)), held
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "wgrad":
+        if case["T"] * case["M"] * case["Dm"] > 1 << 41:
+            return None
+        step = _exact_powers()[st["e"].long()]
+        q = st["q"].double()
+        for k in range(step.shape[0]):
+            q[k * BLOCK:(k + 1) * BLOCK] *= step[k]
+        return torch.matmul(st["dP"].double().T, q)
+    if kind == "pack":
+        return _exact_kept(st["u"])
+    rate = st["rate"].double()
+    x, r, i, s, a, beta, held = _exact_gates(st["x"], st["ga"], st["gi"], rate)
+    if kind == "step":
+        rows = st["slots"].long()
+        h = st["h"].double()
+        h[rows] = a * h[rows] + beta * i * x
+        return dict(y=h[rows], h=h)
+    cu = list(range(0, case["T"] + 1, st["L"])) if st["cu"] is None else st["cu"].tolist()
+    S, n = case["S"], st["T_used"]
+    by_length = sorted((k for k in range(S) if cu[k + 1] > cu[k]), key=lambda k: cu[k] - cu[k + 1])
+    length = [cu[k + 1] - cu[k] for k in by_length]
+    seq = torch.tensor(by_length, device=DEV)
+    start = torch.tensor([cu[k] for k in by_length], device=DEV)
+    end = torch.tensor([cu[k + 1] - 1 for k in by_length], device=DEV)
+    zero = torch.zeros(S, case["C"], dtype=torch.float64, device=DEV)
+    h0 = zero.clone() if st["h0"] is None else st["h0"].double()
+    h = torch.empty(n, case["C"], dtype=torch.float64, device=DEV)
+    cur = h0.clone()
+
+    def forward(h, before, x, i, a, beta, anew):
+        """Row by row; `before`: the state before each row; `anew`: the states that a chunk's first row takes."""
+        cur = h0.clone()[seq]
+        m = len(length)
+        for t in range(length[0] if length else 0):
+            while length[m - 1] <= t:
+                m -= 1
+            rows = start[:m] + t
+            if anew is not None and t > 0:
+                cur[:m] = torch.where((rows % CHUNK == 0)[:, None], anew[rows - 1], cur[:m])
+            if before is not None:
+                before[rows] = cur[:m]
+            cur[:m] = a[rows] * cur[:m] + beta[rows] * i[rows] * x[rows]
+            h[rows] = cur[:m]
+
+    forward(h, None, x, i, a, beta, None)
+    cur[seq] = h[end]
+    out = dict(y=h, h_final=cur)
+    if kind == "fwd":
+        return out
+    if kind == "ckpt":
+        x, r, i, s, a, beta, held = _exact_gates(_exact_kept(st["x"].masked_fill(st["ga"] <= HOLD, 0.0)),
+                                                 _exact_kept(st["ga"].masked_fill(st["ga"] <= HOLD, -math.inf)),
+                                                 _exact_kept(st["gi"].masked_fill(st["ga"] <= HOLD, 0.0)), rate)
+    else:
+        out = {}
+    before = torch.empty_like(h)
+    forward(torch.empty_like(h), before, x, i, a, beta, h)
+    g = torch.empty_like(h)
+    carry = zero.clone() if st["dh_final"] is None else st["dh_final"].double()
+    dh0 = carry.clone()
+    cur, m = carry[seq], len(length)
+    for t in range(length[0] if length else 0):
+        while length[m - 1] <= t:
+            m -= 1
+        rows = end[:m] - t
+        cur[:m] = cur[:m] + st["dy"][rows].double()
+        g[rows] = cur[:m]
+        cur[:m] = cur[:m] * a[rows]
+    dh0[seq] = cur
+    x, r, i, s, a, beta, held = (v[:n] for v in (x, r, i, s, a, beta, held))
+    slope = torch.where(held, torch.zeros_like(s), torch.exp(-2 * s) / beta)  # d beta / d s
+    ds = g * (x * i * slope - a * before).masked_fill(held, 0.0)
+    out |= dict(dx=g * beta * i, dga=ds * s * (1 - r), dgi=g * beta * x * i * (1 - i), drate=(ds * r).sum(0), dh0=dh0)
+    return out
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "wgrad":
+        T, M, Dm = case["T"], case["M"], case["Dm"]
+        return {"bytes": 2 * T * M + T * Dm + -(-T // BLOCK) * Dm + 4 * M * Dm, "flops": 2 * T * M * Dm}
+    w = 2 if case["io"] == "bf16" else 4
+    C = case["C"]
+    if kind == "pack":
+        kept = case["T"] * C + -(-case["T"] // BLOCK) * C
+        return {"bytes": 2 * w * case["T"] * C + 2 * kept, "flops": 3 * case["T"] * C}
+    if kind == "step":
+        return {"bytes": case["S"] * C * (4 * w + 8) + 4 * C + 4 * case["S"], "flops": 20 * case["S"] * C}
+    n, S = case["T"], case["S"]
+    states = 4 * C * (-(-n // CHUNK) + 1 + S * (2 if case["state"] else 1))
+    kept = 3 * (n * C + -(-n // BLOCK) * C)
+    fwd = 4 * w * n * C + states
+    bwd = 7 * w * n * C + states + 4 * C
+    if kind == "fwd":
+        return {"bytes": fwd, "flops": 20 * n * C}
+    if kind == "bwd":
+        return {"bytes": bwd, "flops": 50 * n * C}
+    return {"bytes": fwd + bwd - 3 * w * n * C + 2 * kept, "flops": 75 * n * C}
