@@ -322,10 +322,11 @@ def _plain(st):
     h = _scan(*_begin(st, a, b))
     out = dict(y=h.to(st["x"].dtype), h_final=_final(st, h))
     if kind == "ckpt":
-        low = st["ga"].float() <= HOLD
-        kept = (_value8(*_hold8(torch.where(low, 0.0, st["x"].float()))),
-                _value8(*_hold8(torch.where(low, -math.inf, st["ga"].float()))),
-                _value8(*_hold8(torch.where(low, 0.0, st["gi"].float()))))
+        # rows behind the last sequence are not kept, held rows keep nothing but that they are held
+        x, ga, gi = (st[k][:st["T_used"]].float() for k in ("x", "ga", "gi"))
+        low = ga <= HOLD
+        kept = (_value8(*_hold8(torch.where(low, 0.0, x))), _value8(*_hold8(torch.where(low, -math.inf, ga))),
+                _value8(*_hold8(torch.where(low, 0.0, gi))))
         out |= zip(("dx", "dga", "dgi", "drate", "dh0"), _plain_bwd(st, *kept, _saved(h, st["x"].shape[0])))
     return out
 
@@ -460,9 +461,11 @@ def exact(case, seed):
     if kind == "fwd":
         return out
     if kind == "ckpt":
-        x, r, i, s, a, beta, held = _exact_gates(_exact_kept(st["x"].masked_fill(st["ga"] <= HOLD, 0.0)),
-                                                 _exact_kept(st["ga"].masked_fill(st["ga"] <= HOLD, -math.inf)),
-                                                 _exact_kept(st["gi"].masked_fill(st["ga"] <= HOLD, 0.0)), rate)
+        x, ga, gi = (st[k][:n] for k in ("x", "ga", "gi"))
+        low = ga <= HOLD
+        x, r, i, s, a, beta, held = _exact_gates(_exact_kept(x.masked_fill(low, 0.0)),
+                                                 _exact_kept(ga.masked_fill(low, -math.inf)),
+                                                 _exact_kept(gi.masked_fill(low, 0.0)), rate)
     else:
         out = {}
     before = torch.empty_like(h)
