@@ -409,6 +409,133 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
                          const pdssm_c64* D, int32_t* pi_out, pdssm_c64* d_out,
                          int* dev_status, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Gated recurrent layers.  Beside the PD scan a stack has layers whose state
+ * is gated by the tokens, channel by channel: with r = sigmoid(ga),
+ * i = sigmoid(gi), s = rate[c] * r and a = exp(-s),
+ *
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) i_t x_t,      y_t = h_t.
+ *
+ * The operators below run such a recurrence over whole sequences, forward and
+ * backward, and one token at a time, keep its activations in 8 bits between
+ * forward and backward, and take the weight gradient of a token projection
+ * from activations in that form.
+ *
+ * Rows.  x, ga, gi, y, dy and the gradients are rows [T, C]: fp32, or bf16
+ * with PDSSM_FLAG_BF16_IO in desc->flags.  rate, the states (h0, h_final, saved, dh_final, dh0) and
+ * drate are fp32, and so is all arithmetic; every row output is rounded once,
+ * to nearest even.  Inputs may be parts of wider rows: pdssm_rows has the
+ * entries from one row to the next.  Any C >= 1, alignment of an entry.
+ *
+ * Sequences.  cu == NULL: S sequences of T / S rows each (S divides T).
+ * Otherwise cu [S+1] int32 on the device, cu[0] = 0 <= cu[1] <= ... <= cu[S]
+ * <= T, sequence s has rows cu[s] .. cu[s+1]-1, and may have none (h_final =
+ * h0, dh0 = dh_final).  Rows behind cu[S] are not used, and their outputs not
+ * written.  A cu that breaks the rule is reported as PDSSM_ERR_INDEX in
+ * *dev_status; every access stays in bounds and the results mean nothing.
+ *
+ * Held rows.  A logit ga <= PDSSM_GATE_HOLD (so also -inf and the type's
+ * lowest value) holds the state: a = 1, no input whatever x and gi are (inf
+ * and NaN too), and zero gradients of that row.
+ *
+ * rate [C] must be positive and finite (other values give NaN, in that
+ * channel only).
+ *
+ * The 8-bit form of rows [T, C]: whole numbers q [T, C] int8 and exponents
+ * e [ceil(T/32), C] int8, value q[t,c] * 2^e[t/32,c], with the smallest
+ * e >= -126 for which 127 * 2^e is at least the largest magnitude of the 32
+ * rows and q the nearest whole number, ties to even (at e = 122 at most 63 in
+ * magnitude: 64 would stand for 2^128).  Both ways are exact but for that
+ * rounding (at most 2^(e-1), at e = 122 2^e), also to bf16.  e = -128 marks a block
+ * that held a NaN or an infinity: its values read NaN.  q = -128 is the code
+ * of a held gate logit and reads -inf. */
+#define PDSSM_GATE_HOLD (-64.0f)
+#define PDSSM_GATED_CHUNK 128 /* rows between two saved states */
+#define PDSSM_KEPT_ROWS 32    /* rows that share an exponent in the 8-bit form */
+
+typedef struct pdssm_rows {
+    const void* p;   /* entry (t, c) at p + t*ld + c */
+    int64_t ld;      /* entries from one row to the next, >= C */
+    const int8_t* e; /* the 8-bit form: exponents [ceil(T/32), C] (p: int8); else NULL */
+} pdssm_rows;
+
+typedef struct pdssm_gated_desc {
+    int32_t T, C, S; /* rows, channels, sequences; T >= 0, C >= 1, S >= 1 */
+    uint32_t flags;  /* 0 or PDSSM_FLAG_BF16_IO */
+} pdssm_gated_desc;
+
+/* Workspace bytes of pdssm_gated_fwd (PDSSM_OP_FWD) or pdssm_gated_bwd
+ * (PDSSM_OP_BWD); (size_t)-1 if desc or op is invalid. */
+size_t pdssm_gated_workspace_size(const pdssm_gated_desc* desc, int op);
+
+/*
+ * Forward.  In: x, ga, gi rows; rate; cu and h0 [S, C] (optional).
+ * Out: y [T, C]; optional h_final [S, C]; optional saved
+ * [ceil(T/PDSSM_GATED_CHUNK), C], the state before each chunk of rows, which
+ * pdssm_gated_bwd needs (a row whose chunk begins with a sequence's first row
+ * is not read there); optional q[3], e[3]: x, ga, gi in the 8-bit form, all
+ * six or none (q == e == NULL).  In a held row x and gi are kept as 0 and ga as
+ * held.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned.
+ * Results are deterministic.
+ */
+int pdssm_gated_fwd(const pdssm_gated_desc* desc, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
+                    const float* rate, const int32_t* cu, const float* h0, void* y, float* h_final, float* saved,
+                    int8_t* const* q, int8_t* const* e, void* ws, size_t ws_bytes, int* dev_status, void* stream);
+
+/*
+ * Backward: the vector-Jacobian product of pdssm_gated_fwd.  With g_t the
+ * gradient reaching h_t, g_t = dy_t + a_{t+1} g_{t+1} (dh_final added at a
+ * sequence's last row) and beta = sqrt(1 - a^2):
+ *   dx = g beta i,  dgi = dx x (1 - i),  dga = w (1 - r),  drate = sum w / rate,
+ *   w = g s (i x a^2 / beta - a h_{t-1}),  dh0 = a_0 g_0.
+ * In: x, ga, gi rows, or all three in the 8-bit form; rate, cu, h0 as in the
+ * forward; saved, from it; dy rows; dh_final [S, C] (optional).  The states
+ * are recomputed within each chunk from the saved one, with the values of the
+ * 8-bit form where that is given.
+ * Out: d[0..2] = dx, dga, dgi, rows of ldd entries (>= C; parts of one wider
+ * row tensor when ldd > C); optional drate [C] and dh0 [S, C].
+ */
+int pdssm_gated_bwd(const pdssm_gated_desc* desc, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
+                    const float* rate, const int32_t* cu, const float* h0, const float* saved, const pdssm_rows* dy,
+                    const float* dh_final, void* const* d, int64_t ldd, float* drate, float* dh0, void* ws,
+                    size_t ws_bytes, int* dev_status, void* stream);
+
+/*
+ * One token of each of desc->T sequences (generation): desc->S is the number
+ * of states in the pool h_in, h_out [S, C].
+ *   slots [T] int32: row t advances state slots[t]; NULL: state t (T <= S).
+ * A row with a negative slot is skipped (padding of a batch).  A slot >= S, and a
+ * slot that an earlier row of the call has named, is reported as PDSSM_ERR_INDEX
+ * and its row skipped.  Skipped rows of y, and the entries of h_out of states
+ * that no row advances, are not written.  h_out may be h_in.  y [T, C].
+ */
+int pdssm_gated_step(const pdssm_gated_desc* desc, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
+                     const float* rate, const int32_t* slots, const float* h_in, float* h_out, void* y,
+                     int* dev_status, void* stream);
+
+/*
+ * Rows to the 8-bit form and back.  u: rows [T, C], fp32 or, with
+ * PDSSM_FLAG_BF16_IO, bf16; q [T, C], e [ceil(T/32), C]; out [T, C], fp32 or
+ * bf16 by the flag.  T >= 0, C >= 1.
+ */
+int pdssm_pack8(int32_t T, int32_t C, uint32_t flags, const pdssm_rows* u, int8_t* q, int8_t* e, void* stream);
+int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const int8_t* e, void* out, void* stream);
+
+/*
+ * Weight gradient of a token projection P = u W^T (those of pdssm_project
+ * among them) from activations in the 8-bit form:
+ *   dW[m, d] = sum_t dP[t, m] * u[t, d],   u = q * 2^e.
+ * dP [T, M] bf16 (the bf16 pairs dD, db, dc of pdssm_scan_bwd are such rows,
+ * M = 2 H N), q [T, Dm], e [ceil(T/32), Dm] as pdssm_pack8 writes them (no code
+ * -128), dW [M, Dm] fp32.  On the matrix cores with fp32 sums: both operands
+ * are exact in bf16.  T >= 0; M a multiple of 8, Dm of 16; T*M and T*Dm below 2^40
+ * entries; dP, q and dW 16-byte aligned.  ws:
+ * pdssm_project_wgrad_workspace_size bytes, 256-byte aligned.
+ */
+size_t pdssm_project_wgrad_workspace_size(int32_t T, int32_t M, int32_t Dm);
+int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, const int8_t* q, const int8_t* e,
+                        float* dW, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,6 +19,9 @@ SOURCES = [("pdssm_fused.hip", ["-DPDSSM_N=%d" % n], "pdssm_fused_n%d" % n)
     ("pdssm_decode.hip", [], "pdssm_decode"),
     ("pdssm_select.hip", [], "pdssm_select"),
     ("pdssm_noalloc.hip", [], "pdssm_noalloc"),
+    ("pdssm_gated.hip", [], "pdssm_gated"),
+    ("pdssm_kept.hip", [], "pdssm_kept"),
+    ("pdssm_wgrad.hip", [], "pdssm_wgrad"),
     ("pdssm_api.cpp", [], "pdssm_api"),
 ]
 

@@ -10,6 +10,7 @@
 #include "pdssm_decode.h"
 #include "pdssm_select.h"
 #include "pdssm_fused.h"
+#include "pdssm_gated.h"
 #include "pdssm_internal.h"
 
 namespace {
@@ -373,6 +374,41 @@ bool misaligned(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) % 1
 // int32 / fp32 arrays (idx, y, dy) are read and written as 4-byte words.
 bool misaligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) % 4) != 0; }
 
+static_assert(PDSSM_GATED_CHUNK == pdssm::kGatedChunk && PDSSM_KEPT_ROWS == pdssm::kKeptRows, "header constants");
+
+// ------------------------------------------------------------------ gated recurrence
+int check_gated(const pdssm_gated_desc* d) {
+    if (!d || (d->flags & ~PDSSM_FLAG_BF16_IO) != 0) return PDSSM_ERR_INVALID_ARG;
+    if (d->T < 0 || d->C < 1 || d->S < 1) return PDSSM_ERR_INVALID_ARG;
+    // row offsets are 64-bit; grids and per-chunk buffers stay below 2^31 entries
+    if ((long long)((d->T + 31LL) / 32) * ((d->C + 63) / 64) >= (1LL << 31) ||
+        (long long)d->S * ((d->C + 63) / 64) >= (1LL << 31))
+        return PDSSM_ERR_UNSUPPORTED;
+    return PDSSM_OK;
+}
+
+size_t row_bytes(uint32_t flags) { return flags & PDSSM_FLAG_BF16_IO ? 2 : 4; }
+
+bool misaligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n != 0; }
+
+// Rows of w-byte entries that the kernels may read: not NULL unless there are none.
+bool bad_rows(const pdssm_rows* r, int T, int C, size_t w) {
+    if (!r || r->ld < C || r->ld > (1LL << 40)) return true;
+    return T > 0 && (!r->p || misaligned_to(r->p, w));
+}
+
+Range rows_range(const pdssm_rows* r, int T, int C, size_t w) {
+    return {r->p, T > 0 ? ((size_t)(T - 1) * r->ld + C) * w : 0};
+}
+Range exps_range(const pdssm_rows* r, int T, int C) { return {r->e, (size_t)((T + 31) / 32) * C}; }
+
+pdssm::RowsIn rows_in(const pdssm_rows* r) { return {r->p, r->ld, r->e}; }
+
+// The layout of sequences: equal lengths, or cu.
+bool bad_sequences(const pdssm_gated_desc* d, const int32_t* cu) {
+    return cu ? misaligned4(cu) : d->T % d->S != 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -405,7 +441,7 @@ const char* pdssm_status_string(int st) {
         case PDSSM_ERR_UNSUPPORTED: return "PDSSM_ERR_UNSUPPORTED: N, K, chunk or total size outside the supported set";
         case PDSSM_ERR_WORKSPACE: return "PDSSM_ERR_WORKSPACE: workspace missing or smaller than pdssm_workspace_size";
         case PDSSM_ERR_HIP: return "PDSSM_ERR_HIP: a HIP kernel launch failed";
-        case PDSSM_ERR_INDEX: return "PDSSM_ERR_INDEX: idx or pi entry out of range";
+        case PDSSM_ERR_INDEX: return "PDSSM_ERR_INDEX: an index out of range (idx, pi, cu or slots)";
         default: return "unknown pdssm status";
     }
 }
@@ -770,6 +806,234 @@ int pdssm_compose_chunks(const pdssm_desc* d, const int32_t* idx, const int32_t*
     a.status = dev_status;
     hipError_t e = pdssm::launch_compose(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+size_t pdssm_gated_workspace_size(const pdssm_gated_desc* d, int op) {
+    if (check_gated(d) != PDSSM_OK || (op != PDSSM_OP_FWD && op != PDSSM_OP_BWD)) return (size_t)-1;
+    return pdssm::gated_workspace(d->T, d->C, d->S, op == PDSSM_OP_BWD);
+}
+
+int pdssm_gated_fwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
+                    const float* rate, const int32_t* cu, const float* h0, void* y, float* h_final, float* saved,
+                    int8_t* const* q, int8_t* const* e, void* ws, size_t ws_bytes, int* dev_status, void* stream) {
+    int st = check_gated(d);
+    if (st != PDSSM_OK) return st;
+    const int T = d->T, C = d->C;
+    const size_t w = row_bytes(d->flags), n = (size_t)T * C, ns = (size_t)d->S * C * 4;
+    const size_t nc = (size_t)((T + pdssm::kGatedChunk - 1) / pdssm::kGatedChunk) * C * 4;
+    const size_t ne = (size_t)((T + pdssm::kKeptRows - 1) / pdssm::kKeptRows) * C;
+    for (const pdssm_rows* r : {x, ga, gi})
+        if (bad_rows(r, T, C, w) || r->e) return PDSSM_ERR_INVALID_ARG;
+    if (!rate || bad_sequences(d, cu) || (T > 0 && (!y || misaligned_to(y, w)))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)rate, (const void*)h0, (const void*)h_final, (const void*)saved, (const void*)dev_status})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    if ((q == nullptr) != (e == nullptr)) return PDSSM_ERR_INVALID_ARG;
+    if (q && T > 0)
+        for (int i = 0; i < 3; ++i)
+            if (!q[i] || !e[i]) return PDSSM_ERR_INVALID_ARG;
+    const bool keep = q && T > 0;
+    const size_t need = pdssm::gated_workspace(T, C, d->S, false);
+    if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
+    if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{y, n * w}, {h_final, ns}, {saved, nc}, {ws, need}, {keep ? q[0] : nullptr, n},
+                     {keep ? q[1] : nullptr, n}, {keep ? q[2] : nullptr, n}, {keep ? e[0] : nullptr, ne},
+                     {keep ? e[1] : nullptr, ne}, {keep ? e[2] : nullptr, ne}},
+                    {rows_range(x, T, C, w), rows_range(ga, T, C, w), rows_range(gi, T, C, w), {rate, (size_t)C * 4},
+                     {cu, ((size_t)d->S + 1) * 4}, {h0, ns}}))
+        return PDSSM_ERR_INVALID_ARG;
+    pdssm::GatedArgs a = {};
+    a.T = T;
+    a.C = C;
+    a.S = d->S;
+    a.L = cu ? 0 : T / d->S;
+    a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.x = rows_in(x);
+    a.ga = rows_in(ga);
+    a.gi = rows_in(gi);
+    a.rate = rate;
+    a.cu = cu;
+    a.h0 = h0;
+    a.status = dev_status;
+    a.ws = ws;
+    a.y = y;
+    a.h_final = h_final;
+    a.saved = saved;
+    for (int i = 0; i < 3; ++i) {
+        a.q[i] = keep ? q[i] : nullptr;
+        a.e[i] = keep ? e[i] : nullptr;
+    }
+    return pdssm::launch_gated_fwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+int pdssm_gated_bwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
+                    const float* rate, const int32_t* cu, const float* h0, const float* saved, const pdssm_rows* dy,
+                    const float* dh_final, void* const* dd, int64_t ldd, float* drate, float* dh0, void* ws,
+                    size_t ws_bytes, int* dev_status, void* stream) {
+    int st = check_gated(d);
+    if (st != PDSSM_OK) return st;
+    const int T = d->T, C = d->C;
+    const size_t w = row_bytes(d->flags), ns = (size_t)d->S * C * 4;
+    const size_t nc = (size_t)((T + pdssm::kGatedChunk - 1) / pdssm::kGatedChunk) * C * 4;
+    if (!x || !ga || !gi) return PDSSM_ERR_INVALID_ARG;
+    const bool kept = x->e != nullptr;
+    const size_t wi = kept ? 1 : w;
+    for (const pdssm_rows* r : {x, ga, gi})
+        if (bad_rows(r, T, C, wi) || (r->e != nullptr) != kept) return PDSSM_ERR_INVALID_ARG;
+    if (bad_rows(dy, T, C, w) || dy->e || !rate || bad_sequences(d, cu) || (T > 0 && !saved) || !dd || ldd < C ||
+        ldd > (1LL << 40))
+        return PDSSM_ERR_INVALID_ARG;
+    for (int i = 0; i < 3; ++i)
+        if (T > 0 && (!dd[i] || misaligned_to(dd[i], w))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)rate, (const void*)h0, (const void*)saved, (const void*)dh_final, (const void*)drate,
+                          (const void*)dh0, (const void*)dev_status})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    const size_t need = pdssm::gated_workspace(T, C, d->S, true);
+    if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
+    if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
+    // the three gradients may be parts of one tensor of wider rows: then they
+    // interleave, C entries apart or more within a row
+    const pdssm_rows o[3] = {{dd[0], ldd, nullptr}, {dd[1], ldd, nullptr}, {dd[2], ldd, nullptr}};
+    const Range out[3] = {rows_range(&o[0], T, C, w), rows_range(&o[1], T, C, w), rows_range(&o[2], T, C, w)};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j) {
+            if (!overlap(out[i], out[j])) continue;
+            const uintptr_t p = reinterpret_cast<uintptr_t>(dd[i]), r = reinterpret_cast<uintptr_t>(dd[j]);
+            const uintptr_t apart = (p > r ? p - r : r - p) % ((uintptr_t)ldd * w);
+            if (apart < (uintptr_t)C * w || (uintptr_t)ldd * w - apart < (uintptr_t)C * w) return PDSSM_ERR_INVALID_ARG;
+        }
+    const Range ins[] = {rows_range(x, T, C, wi), rows_range(ga, T, C, wi), rows_range(gi, T, C, wi),
+                         exps_range(x, T, C), exps_range(ga, T, C), exps_range(gi, T, C), rows_range(dy, T, C, w),
+                         {rate, (size_t)C * 4}, {cu, ((size_t)d->S + 1) * 4}, {h0, ns}, {saved, nc}, {dh_final, ns}};
+    for (const Range& r : ins)
+        for (const Range& v : out)
+            if (overlap(r, v)) return PDSSM_ERR_INVALID_ARG;
+    for (const Range& v : out)
+        for (const Range& r : {Range{drate, (size_t)C * 4}, Range{dh0, ns}, Range{ws, need}})
+            if (overlap(r, v)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{drate, (size_t)C * 4}, {dh0, ns}, {ws, need}},
+                    {ins[0], ins[1], ins[2], ins[3], ins[4], ins[5], ins[6], ins[7], ins[8], ins[9], ins[10], ins[11]}))
+        return PDSSM_ERR_INVALID_ARG;
+    pdssm::GatedArgs a = {};
+    a.T = T;
+    a.C = C;
+    a.S = d->S;
+    a.L = cu ? 0 : T / d->S;
+    a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.kept = kept;
+    a.x = rows_in(x);
+    a.ga = rows_in(ga);
+    a.gi = rows_in(gi);
+    a.rate = rate;
+    a.cu = cu;
+    a.h0 = h0;
+    a.status = dev_status;
+    a.ws = ws;
+    a.saved = const_cast<float*>(saved);
+    a.dy = rows_in(dy);
+    a.dhf = dh_final;
+    for (int i = 0; i < 3; ++i) a.d[i] = dd[i];
+    a.ldd = ldd;
+    a.drate = drate;
+    a.dh0 = dh0;
+    return pdssm::launch_gated_bwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+int pdssm_gated_step(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
+                     const float* rate, const int32_t* slots, const float* h_in, float* h_out, void* y,
+                     int* dev_status, void* stream) {
+    int st = check_gated(d);
+    if (st != PDSSM_OK) return st;
+    const int B = d->T, C = d->C;
+    const size_t w = row_bytes(d->flags), ns = (size_t)d->S * C * 4;
+    if (B > 65535) return PDSSM_ERR_UNSUPPORTED;  // grid
+    for (const pdssm_rows* r : {x, ga, gi})
+        if (bad_rows(r, B, C, w) || r->e) return PDSSM_ERR_INVALID_ARG;
+    if (!slots && B > d->S) return PDSSM_ERR_INVALID_ARG;
+    if (!rate || !h_in || !h_out || (B > 0 && (!y || misaligned_to(y, w)))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)rate, (const void*)slots, (const void*)h_in, (const void*)h_out, (const void*)dev_status})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    const std::initializer_list<Range> ins = {rows_range(x, B, C, w), rows_range(ga, B, C, w), rows_range(gi, B, C, w),
+                                              {rate, (size_t)C * 4}, {slots, (size_t)B * 4}};
+    if (any_overlap({{h_out, ns}, {y, (size_t)B * C * w}}, ins) ||
+        overlap({h_in, ns}, {y, (size_t)B * C * w}) || (h_in != h_out && overlap({h_in, ns}, {h_out, ns})))
+        return PDSSM_ERR_INVALID_ARG;
+    if (B == 0) return PDSSM_OK;
+    pdssm::GatedStepArgs a = {};
+    a.B = B;
+    a.C = C;
+    a.pool = d->S;
+    a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.x = rows_in(x);
+    a.ga = rows_in(ga);
+    a.gi = rows_in(gi);
+    a.rate = rate;
+    a.slots = slots;
+    a.h_in = h_in;
+    a.h_out = h_out;
+    a.y = y;
+    a.status = dev_status;
+    return pdssm::launch_gated_step(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+int pdssm_pack8(int32_t T, int32_t C, uint32_t flags, const pdssm_rows* u, int8_t* q, int8_t* e, void* stream) {
+    const pdssm_gated_desc d = {T, C, 1, flags};
+    const int st = check_gated(&d);
+    if (st != PDSSM_OK) return st;
+    const size_t w = row_bytes(flags);
+    if (bad_rows(u, T, C, w) || u->e || (T > 0 && (!q || !e))) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{q, (size_t)T * C}, {e, (size_t)((T + 31) / 32) * C}}, {rows_range(u, T, C, w)}))
+        return PDSSM_ERR_INVALID_ARG;
+    if (T == 0) return PDSSM_OK;
+    return pdssm::launch_pack8(T, C, w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32, rows_in(u), q, e,
+                               static_cast<hipStream_t>(stream)) == hipSuccess
+               ? PDSSM_OK
+               : PDSSM_ERR_HIP;
+}
+
+int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const int8_t* e, void* out, void* stream) {
+    const pdssm_gated_desc d = {T, C, 1, flags};
+    const int st = check_gated(&d);
+    if (st != PDSSM_OK) return st;
+    const size_t w = row_bytes(flags);
+    if (T > 0 && (!q || !e || !out || misaligned_to(out, w))) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{out, (size_t)T * C * w}}, {{q, (size_t)T * C}, {e, (size_t)((T + 31) / 32) * C}}))
+        return PDSSM_ERR_INVALID_ARG;
+    if (T == 0) return PDSSM_OK;
+    return pdssm::launch_unpack8(T, C, w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32, q, e, out,
+                                 static_cast<hipStream_t>(stream)) == hipSuccess
+               ? PDSSM_OK
+               : PDSSM_ERR_HIP;
+}
+
+namespace {
+int check_wgrad(int32_t T, int32_t M, int32_t Dm) {
+    if (T < 0 || M < 1 || Dm < 1) return PDSSM_ERR_INVALID_ARG;
+    if (M % 8 != 0 || Dm % 16 != 0) return PDSSM_ERR_UNSUPPORTED;
+    if ((long long)T * M >= (1LL << 40) || (long long)T * Dm >= (1LL << 40) || (long long)M * Dm >= (1LL << 31) ||
+        M > (1 << 20) || Dm > (1 << 20))
+        return PDSSM_ERR_UNSUPPORTED;
+    return PDSSM_OK;
+}
+}  // namespace
+
+size_t pdssm_project_wgrad_workspace_size(int32_t T, int32_t M, int32_t Dm) {
+    return check_wgrad(T, M, Dm) != PDSSM_OK ? (size_t)-1 : pdssm::wgrad_workspace(T, M, Dm);
+}
+
+int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, const int8_t* q, const int8_t* e,
+                        float* dW, void* ws, size_t ws_bytes, void* stream) {
+    const int st = check_wgrad(T, M, Dm);
+    if (st != PDSSM_OK) return st;
+    if (!dW || (T > 0 && (!dP || !q || !e))) return PDSSM_ERR_INVALID_ARG;
+    if (misaligned(dP) || misaligned(q) || misaligned(dW)) return PDSSM_ERR_INVALID_ARG;
+    const size_t need = pdssm::wgrad_workspace(T, M, Dm);
+    if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
+    if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{dW, (size_t)M * Dm * 4}, {ws, need}},
+                    {{dP, (size_t)T * M * 2}, {q, (size_t)T * Dm}, {e, (size_t)((T + 31) / 32) * Dm}}))
+        return PDSSM_ERR_INVALID_ARG;
+    pdssm::WgradArgs a = {T, M, Dm, dP, q, e, dW, ws};
+    return pdssm::launch_wgrad(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
 }
 
 }  // extern "C"

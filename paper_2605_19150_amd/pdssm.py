@@ -18,8 +18,15 @@ The real-valued model (FLAG_REAL_IO): D, b, c, dD, db, dc and saved are
 Straight-through surrogate gradients (Sec. 3.1 Prop. 2): q [B,L,H,K] float32,
   z [B,L,H,N] complex64, G [H,K,N,N] float32, routing logits [B,L,H,K] and
   dense dictionary M [H,K,N,N] float32.
+Gated recurrent layers (gated_fwd and the functions after it) take rows:
+  x, ga, gi, dy [B,L,C] for B sequences of one length, or [T,C] with the
+  sequences' bounds cu [S+1] int32; float32 or bfloat16, any strides between
+  rows, entries of a row next to each other.  rate [C] and the states
+  [S,C] are float32.  Activations in the 8-bit form are pairs (q, e): int8
+  [T,C] and [ceil(T/32),C].
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -46,10 +53,20 @@ class Desc(ctypes.Structure):
                 ("flags", ctypes.c_uint32)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64), ("e", ctypes.c_void_p)]
+
+
+class GatedDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("C", ctypes.c_int32), ("S", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
 EXPORTS = ("pdssm_abi_version", "pdssm_chunk_len", "pdssm_num_chunks", "pdssm_workspace_size",
            "pdssm_uses_fused", "pdssm_scan_segments", "pdssm_status_string", "pdssm_prepare", "pdssm_scan_fwd", "pdssm_scan_fwd_noalloc",
            "pdssm_scan_bwd", "pdssm_compose_chunks", "pdssm_scan_bwd_ste", "pdssm_ste_grads",
-           "pdssm_softmax_vjp", "pdssm_decode_step", "pdssm_dict_argmax", "pdssm_route", "pdssm_project")
+           "pdssm_softmax_vjp", "pdssm_decode_step", "pdssm_dict_argmax", "pdssm_route", "pdssm_project",
+           "pdssm_gated_workspace_size", "pdssm_gated_fwd", "pdssm_gated_bwd", "pdssm_gated_step", "pdssm_pack8",
+           "pdssm_unpack8", "pdssm_project_wgrad_workspace_size", "pdssm_project_wgrad")
 
 
 def lib_path():
@@ -98,6 +115,19 @@ def load():
     L.pdssm_route.restype = I
     L.pdssm_project.argtypes = [I32] * 5 + [P] * 10 + [P]
     L.pdssm_project.restype = I
+    U32, I64, V3 = ctypes.c_uint32, ctypes.c_int64, ctypes.POINTER(ctypes.c_void_p)
+    G, R = ctypes.POINTER(GatedDesc), ctypes.POINTER(Rows)
+    L.pdssm_gated_workspace_size.argtypes, L.pdssm_gated_workspace_size.restype = [G, I], Z
+    L.pdssm_gated_fwd.argtypes = [G, R, R, R] + [P] * 6 + [V3, V3, P, Z, P, P]
+    L.pdssm_gated_fwd.restype = I
+    L.pdssm_gated_bwd.argtypes = [G, R, R, R] + [P] * 4 + [R, P, V3, I64] + [P] * 3 + [Z, P, P]
+    L.pdssm_gated_bwd.restype = I
+    L.pdssm_gated_step.argtypes = [G, R, R, R] + [P] * 7
+    L.pdssm_gated_step.restype = I
+    L.pdssm_pack8.argtypes, L.pdssm_pack8.restype = [I32, I32, U32, R, P, P, P], I
+    L.pdssm_unpack8.argtypes, L.pdssm_unpack8.restype = [I32, I32, U32, P, P, P, P], I
+    L.pdssm_project_wgrad_workspace_size.argtypes, L.pdssm_project_wgrad_workspace_size.restype = [I32] * 3, Z
+    L.pdssm_project_wgrad.argtypes, L.pdssm_project_wgrad.restype = [I32] * 3 + [P] * 5 + [Z, P], I
     if L.pdssm_abi_version() != 1:
         raise ImportError("libpdssm.so ABI version mismatch")
     _lib = L
@@ -595,3 +625,328 @@ def project(u, S=None, Wb=None, Wc=None, Wd=None, logits=True, N=None, stream=No
     if st != OK:
         raise PdssmError(st, "pdssm_project")
     return out
+
+
+# ---- gated recurrent layers ------------------------------------------------
+
+GATED_CHUNK = 128  # rows between two saved states
+KEPT_ROWS = 32     # rows that share an exponent in the 8-bit form
+GATE_HOLD = -64.0  # a gate logit at or under this one holds the state
+OP_SIZE_ERROR = ctypes.c_size_t(-1).value
+
+
+def _ceil(n, k):
+    return -(-n // k)
+
+
+class _On:
+    """The device and stream that a call on tensors of device dev runs on.  A
+    stream of the caller's own that is not the current one learns of every
+    tensor of the call (seen()), so that none is given to other work before it
+    has run."""
+
+    def __init__(self, dev, stream):
+        self.guard = torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else None
+        cur = torch.cuda.current_stream(dev)
+        self.stream = cur if stream is None else stream
+        self.other = self.stream if self.stream.cuda_stream != cur.cuda_stream else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+    def seen(self, *tensors):
+        if self.other is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.other)
+
+    def ptr(self):
+        return ctypes.c_void_p(self.stream.cuda_stream)
+
+
+def _row_layout(t, name, dtype, shape, dev):
+    """(pointer, entries from row to row) of rows [T,C] or [B,L,C] that may be a part of wider rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.device != dev or dev.type != "cuda":
+        raise ValueError("%s must be on %s" % (name, dev))
+    C = shape[-1]
+    if t.stride(-1) != 1 and C > 1:
+        raise ValueError("%s: the entries of a row must be next to each other" % name)
+    ld = C
+    if len(shape) == 3:
+        B, L = shape[0], shape[1]
+        if L > 1:
+            ld = t.stride(1)
+            if B > 1 and t.stride(0) != L * ld:
+                raise ValueError("%s: rows must be evenly spaced over the batch" % name)
+        elif B > 1:
+            ld = t.stride(0)
+    elif shape[0] > 1:
+        ld = t.stride(0)
+    if ld < C:
+        raise ValueError("%s: rows must not overlap" % name)
+    return t.data_ptr(), ld
+
+
+def _rows(t, name, dtype, shape, dev):
+    p, ld = _row_layout(t, name, dtype, shape, dev)
+    return Rows(p, ld, None)
+
+
+def _kept(pair, name, T, C, dev):
+    """A pair (q, e) in the 8-bit form."""
+    q, e = pair
+    _need(q, name + " codes", torch.int8, (T, C), dev)
+    _need(e, name + " exponents", torch.int8, (_ceil(T, KEPT_ROWS), C), dev)
+    return Rows(q.data_ptr(), C, e.data_ptr())
+
+
+def _row_type(t):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("rows must be a torch.Tensor")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("rows must be float32 or bfloat16, got %s" % t.dtype)
+    return FLAG_BF16_IO if t.dtype == torch.bfloat16 else 0
+
+
+def _sequences(t, cu):
+    """(T, C, S) of rows t [B,L,C], or [T,C] with the bounds cu [S+1]."""
+    if cu is None:
+        if t.dim() != 3:
+            raise ValueError("rows must be [B,L,C], or [T,C] with cu")
+        B, L, C = t.shape
+        T, S = B * L, B
+    else:
+        if t.dim() != 2:
+            raise ValueError("rows must be [T,C] when cu is given")
+        T, C = t.shape
+        if not isinstance(cu, torch.Tensor) or cu.dim() != 1 or cu.shape[0] < 2:
+            raise ValueError("cu must be [S+1] with S >= 1")
+        S = cu.shape[0] - 1
+        _need(cu, "cu", torch.int32, (S + 1,), t.device)
+    if C < 1 or S < 1:
+        raise ValueError("rows need at least one channel and one sequence")
+    return T, C, S
+
+
+def _gated_ws(d, op, dev):
+    n = load().pdssm_gated_workspace_size(ctypes.byref(d), op)
+    if n == OP_SIZE_ERROR:
+        raise PdssmError(ERR_UNSUPPORTED, "gated_workspace_size")
+    return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+
+
+def _state(t, name, S, C, dev):
+    if t is not None:
+        _need(t, name, torch.float32, (S, C), dev)
+
+
+def _checked(status, what, dev):
+    """Synchronise and raise if a kernel reported a bad index."""
+    if status is not None:
+        torch.cuda.synchronize(dev)
+        st = int(status.item())
+        if st != OK:
+            raise PdssmError(st, what)
+
+
+def _three(tensors):
+    return (ctypes.c_void_p * 3)(*[t.data_ptr() for t in tensors])
+
+
+def gated_fwd(x, ga, gi, rate, cu=None, h0=None, hold8=False, check=True, stream=None):
+    """The gated recurrence h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(gi_t) x_t
+    with a_t = exp(-rate * sigmoid(ga_t)), over every sequence from its state
+    in h0 [S,C] (default 0).  Returns (y, h_final [S,C], saved
+    [ceil(T/128),C]), y = h in the rows' type and shape; with hold8=True also
+    ((q, e) of x, of ga, of gi): the inputs in the 8-bit form, which gated_bwd
+    takes in their place.  check=False neither synchronises nor reports a bad cu."""
+    flags = _row_type(x)
+    T, C, S = _sequences(x, cu)
+    dev = x.device
+    r = [_rows(t, n, x.dtype, x.shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
+    _need(rate, "rate", torch.float32, (C,), dev)
+    _state(h0, "h0", S, C, dev)
+    d = GatedDesc(T, C, S, flags)
+    with _On(dev, stream) as on:
+        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
+        h_final = torch.empty((S, C), dtype=torch.float32, device=dev)
+        saved = torch.empty((_ceil(T, GATED_CHUNK), C), dtype=torch.float32, device=dev)
+        kept = q = e = None
+        if hold8:
+            kept = tuple((torch.empty((T, C), dtype=torch.int8, device=dev),
+                          torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)) for _ in range(3))
+            q, e = _three([k[0] for k in kept]), _three([k[1] for k in kept])
+        ws = _gated_ws(d, OP_FWD, dev)
+        status = torch.zeros(1, dtype=torch.int32, device=dev) if check else None
+        if check and on.other is not None:
+            on.other.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
+        on.seen(x, ga, gi, rate, cu, h0, y, h_final, saved, ws, status, *([t for k in kept for t in k] if hold8 else []))
+        st = load().pdssm_gated_fwd(ctypes.byref(d), ctypes.byref(r[0]), ctypes.byref(r[1]), ctypes.byref(r[2]),
+                                    _p(rate), _p(cu), _p(h0), _p(y), _p(h_final), _p(saved), q, e, _p(ws),
+                                    ws.numel() if ws is not None else 0, _p(status), on.ptr())
+        if st != OK:
+            raise PdssmError(st, "pdssm_gated_fwd")
+        _checked(status, "pdssm_gated_fwd", dev)
+    return (y, h_final, saved, kept) if hold8 else (y, h_final, saved)
+
+
+def gated_bwd(x, ga, gi, rate, saved, dy, cu=None, h0=None, dh_final=None, check=True, stream=None):
+    """Gradients of gated_fwd: (dx, dga, dgi, drate [C], dh0 [S,C]) from dy (rows
+    as y) and dh_final [S,C] (default 0); saved, cu and h0 as in the forward.  x, ga, gi are the
+    forward's rows, or all three the pairs (q, e) that it returned with
+    hold8=True.  dx, dga and dgi, in dy's type and shape, are the three parts of one
+    tensor [..., 3C], the gradient of a projection that makes the three."""
+    flags = _row_type(dy)
+    T, C, S = _sequences(dy, cu)
+    dev = dy.device
+    ins = ((x, "x"), (ga, "ga"), (gi, "gi"))
+    eight = isinstance(x, (tuple, list))
+    if any(isinstance(t, (tuple, list)) != eight for t, _ in ins):
+        raise TypeError("x, ga and gi must be all rows or all pairs (q, e)")
+    r = [_kept(t, n, T, C, dev) if eight else _rows(t, n, dy.dtype, dy.shape, dev) for t, n in ins]
+    rdy = _rows(dy, "dy", dy.dtype, dy.shape, dev)
+    _need(rate, "rate", torch.float32, (C,), dev)
+    _need(saved, "saved", torch.float32, (_ceil(T, GATED_CHUNK), C), dev)
+    _state(h0, "h0", S, C, dev)
+    _state(dh_final, "dh_final", S, C, dev)
+    d = GatedDesc(T, C, S, flags)
+    with _On(dev, stream) as on:
+        rows = torch.empty((*dy.shape[:-1], 3 * C), dtype=dy.dtype, device=dev)
+        grads = rows.split(C, -1)
+        drate = torch.empty(C, dtype=torch.float32, device=dev)
+        dh0 = torch.empty((S, C), dtype=torch.float32, device=dev)
+        ws = _gated_ws(d, OP_BWD, dev)
+        status = torch.zeros(1, dtype=torch.int32, device=dev) if check else None
+        if check and on.other is not None:
+            on.other.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
+        on.seen(*([t for k in (x, ga, gi) for t in k] if eight else (x, ga, gi)), rate, saved, dy, cu, h0, dh_final,
+                rows, drate, dh0, ws, status)
+        st = load().pdssm_gated_bwd(ctypes.byref(d), ctypes.byref(r[0]), ctypes.byref(r[1]), ctypes.byref(r[2]),
+                                    _p(rate), _p(cu), _p(h0), _p(saved), ctypes.byref(rdy), _p(dh_final),
+                                    _three(grads), 3 * C, _p(drate), _p(dh0), _p(ws),
+                                    ws.numel() if ws is not None else 0, _p(status), on.ptr())
+        if st != OK:
+            raise PdssmError(st, "pdssm_gated_bwd")
+        _checked(status, "pdssm_gated_bwd", dev)
+    return (*grads, drate, dh0)
+
+
+def gated_step(x, ga, gi, rate, h, slots=None, out=None, y=None, check=True, stream=None):
+    """One token of the gated recurrence for each row of x, ga, gi [B,C]: returns
+    (h_new [S,C], y [B,C]).  h [S,C] holds the states; row b advances state
+    slots[b] (int32; default b).  A negative slot skips its row; a slot past the
+    pool or named by an earlier row is an error and skips it too.  Skipped rows of
+    y, and states that no row advances, are not written.  out [S,C] takes the new
+    states; default: in place."""
+    flags = _row_type(x)
+    if x.dim() != 2:
+        raise ValueError("x must be [B,C]")
+    B, C = x.shape
+    dev = x.device
+    r = [_rows(t, n, x.dtype, (B, C), dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
+    _need(rate, "rate", torch.float32, (C,), dev)
+    if not isinstance(h, torch.Tensor) or h.dim() != 2:
+        raise ValueError("h must be [S,C]")
+    S = h.shape[0]
+    _need(h, "h", torch.float32, (S, C), dev)
+    out = h if out is None else out
+    _need(out, "out", torch.float32, (S, C), dev)
+    if slots is not None:
+        _need(slots, "slots", torch.int32, (B,), dev)
+    d = GatedDesc(B, C, S, flags)
+    with _On(dev, stream) as on:
+        if y is None:
+            y = torch.empty((B, C), dtype=x.dtype, device=dev)
+        _need(y, "y", x.dtype, (B, C), dev)
+        status = torch.zeros(1, dtype=torch.int32, device=dev) if check else None
+        if check and on.other is not None:
+            on.other.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
+        on.seen(x, ga, gi, rate, h, out, slots, y, status)
+        st = load().pdssm_gated_step(ctypes.byref(d), ctypes.byref(r[0]), ctypes.byref(r[1]), ctypes.byref(r[2]),
+                                     _p(rate), _p(slots), _p(h), _p(out), _p(y), _p(status), on.ptr())
+        if st != OK:
+            raise PdssmError(st, "pdssm_gated_step")
+        _checked(status, "pdssm_gated_step", dev)
+    return out, y
+
+
+def pack8(u, stream=None):
+    """(q, e): rows u [T,C] or [B,L,C] in the 8-bit form, q [T,C] and
+    e [ceil(T/32),C] int8 with T = B*L; the value of q[t,c] is q[t,c] * 2^e[t//32,c]."""
+    flags = _row_type(u)
+    if u.dim() not in (2, 3):
+        raise ValueError("u must be [T,C] or [B,L,C]")
+    C = u.shape[-1]
+    T = u.shape[0] if u.dim() == 2 else u.shape[0] * u.shape[1]
+    dev = u.device
+    r = _rows(u, "u", u.dtype, u.shape, dev)
+    with _On(dev, stream) as on:
+        q = torch.empty((T, C), dtype=torch.int8, device=dev)
+        e = torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)
+        on.seen(u, q, e)
+        st = load().pdssm_pack8(T, C, flags, ctypes.byref(r), _p(q), _p(e), on.ptr())
+        if st != OK:
+            raise PdssmError(st, "pdssm_pack8")
+    return q, e
+
+
+def unpack8(pair, dtype=torch.float32, stream=None):
+    """The values [T,C] that a pair (q, e) of the 8-bit form stands for, exact in float32 and bfloat16."""
+    q, e = pair
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("dtype must be float32 or bfloat16")
+    if not isinstance(q, torch.Tensor) or q.dim() != 2:
+        raise ValueError("q must be [T,C]")
+    T, C = q.shape
+    dev = q.device
+    _kept(pair, "u", T, C, dev)
+    with _On(dev, stream) as on:
+        out = torch.empty((T, C), dtype=dtype, device=dev)
+        on.seen(q, e, out)
+        st = load().pdssm_unpack8(T, C, FLAG_BF16_IO if dtype == torch.bfloat16 else 0, _p(q), _p(e), _p(out), on.ptr())
+        if st != OK:
+            raise PdssmError(st, "pdssm_unpack8")
+    return out
+
+
+def project_wgrad(dP, u8, stream=None):
+    """dW [M,Dm] float32 = dP^T u, the weight gradient of a projection P = u W^T:
+    dP bfloat16 with B*L rows of M entries in all (the bf16 pairs that
+    scan_bwd returns, [B,L,H,N,2], are rows of 2*H*N), u8 the activations u in
+    the 8-bit form (pack8)."""
+    q, e = u8
+    if not isinstance(q, torch.Tensor) or q.dim() != 2:
+        raise ValueError("u8 must be a pair (q, e) with q [T,Dm]")
+    T, Dm = q.shape
+    dev = q.device
+    _kept(u8, "u", T, Dm, dev)
+    if not isinstance(dP, torch.Tensor) or dP.dim() < 2:
+        raise ValueError("dP must be rows [T,M] or [B,L,...]")
+    _need(dP, "dP", torch.bfloat16, dP.shape, dev)
+    lead = 1 if dP.dim() == 2 else 2  # axes that count rows
+    if math.prod(dP.shape[:lead]) != T:
+        raise ValueError("dP and u8 disagree on the number of rows")
+    M = math.prod(dP.shape[lead:])
+    with _On(dev, stream) as on:
+        dW = torch.empty((M, Dm), dtype=torch.float32, device=dev)
+        n = load().pdssm_project_wgrad_workspace_size(T, M, Dm)
+        if n == OP_SIZE_ERROR:
+            raise PdssmError(ERR_UNSUPPORTED, "project_wgrad_workspace_size")
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+        on.seen(dP, q, e, dW, ws)
+        st = load().pdssm_project_wgrad(T, M, Dm, _p(dP), _p(q), _p(e), _p(dW), _p(ws), n, on.ptr())
+        if st != OK:
+            raise PdssmError(st, "pdssm_project_wgrad")
+    return dW

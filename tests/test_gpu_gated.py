@@ -1,0 +1,561 @@
+"""The gated recurrent operators on the GPU against their float64 reference.
+
+Tolerances, in units u = 2^-24 (half a step of fp32): one entry's gates take
+about 16 roundings of at most 2u each (two exponentials, two reciprocals, a
+square root, a series of six terms and products), and a state or gradient is a
+sum along the sequence in which every step may add its own: a state of an n-row
+sequence is off by at most (2n + 32) u of the sum of its terms' magnitudes, a
+gradient, a product of one chain each way, by (4n + 64) u of its.  The reference
+gives those sums.  A bf16 output adds half a step of bf16, 2^-8 of its value.
+"""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import gated as G
+from paper_2605_19150_amd import pdssm
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DEV = "cuda"
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Case:
+    """Inputs of one call on the GPU (parts of one wider row tensor when
+    wide) and the same values for the reference."""
+
+    def __init__(self, bounds, C, T=None, dtype=torch.float32, wide=True, dense=False, states=True, masked=False, seed=0):
+        self.bounds, self.C, self.dtype, self.dense = bounds, C, dtype, dense
+        T = self.T = bounds[-1] if T is None else T
+        S = self.S = len(bounds) - 1
+        g = torch.Generator().manual_seed(seed)
+        ld = 3 * C + 5 if wide else 3 * C
+        rows = torch.randn(T, ld, generator=g)
+        off = 1 if wide else 0  # an odd first entry
+        if masked and T:
+            pad = torch.rand(T, generator=g) < 0.2
+            pad[-1] = pad[0] = True
+            low = torch.rand(T, generator=g) < 0.5
+            rows[:, off + C:off + 2 * C][pad & low] = torch.finfo(dtype).min
+            rows[:, off + C:off + 2 * C][pad & ~low] = -math.inf
+            rows[:, off:off + C][pad] = math.inf
+            rows[:, off + 2 * C:off + 3 * C][pad & low] = math.nan
+            if S > 1:  # a whole sequence held
+                rows[bounds[S - 2]:bounds[S - 1], off + C:off + 2 * C] = -1e9
+        rows = rows.to(dtype).to(DEV)
+        self.x, self.ga, self.gi = (rows[:, off + k * C:off + (k + 1) * C] for k in range(3))
+        self.rate = torch.exp(torch.empty(C).uniform_(math.log(0.008), math.log(2.0), generator=g)).to(DEV)
+        self.dy = torch.randn(T, C, generator=g).to(dtype).to(DEV)
+        self.h0 = torch.randn(S, C, generator=g).to(DEV) if states else None
+        self.dhf = torch.randn(S, C, generator=g).to(DEV) if states else None
+        self.cu = None if dense else torch.tensor(bounds, dtype=torch.int32, device=DEV)
+        self.longest = max(b - a for a, b in zip(bounds, bounds[1:]))
+        self.end = bounds[-1]
+
+    def rows(self, t):
+        return t.unflatten(0, (self.S, self.T // self.S)) if self.dense else t
+
+    def fwd(self, **kw):
+        return pdssm.gated_fwd(self.rows(self.x), self.rows(self.ga), self.rows(self.gi), self.rate, cu=self.cu,
+                               h0=self.h0, **kw)
+
+    def bwd(self, saved, kept=None, **kw):
+        x, ga, gi = kept or (self.rows(self.x), self.rows(self.ga), self.rows(self.gi))
+        return pdssm.gated_bwd(x, ga, gi, self.rate, saved, self.rows(self.dy), cu=self.cu, h0=self.h0,
+                               dh_final=self.dhf, **kw)
+
+    def ref(self):
+        a = [_np(t) for t in (self.x, self.ga, self.gi, self.rate)]
+        return a, None if self.h0 is None else _np(self.h0)
+
+
+def _near(name, got, want, scale, units, dtype=torch.float32):
+    got, want, scale = got.reshape(want.shape), np.asarray(want), np.asarray(scale)
+    tol = units * U * scale + 1e-35
+    if dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * (np.abs(want) + tol)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), "%s: %d of %d, worst %.3g of its tolerance" % (
+        name, bad.sum(), bad.size, np.nanmax(np.abs(got - want) / tol))
+
+
+def _check_fwd(case, y, h_final):
+    args, h0 = case.ref()
+    n, end = case.longest, case.end
+    h, fin = G.gated_fwd(*args, case.bounds, h0)
+    size, fin_size = G.gated_fwd(*args, case.bounds, h0, absolute=True)
+    _near("y", _np(y).reshape(case.T, case.C)[:end], h[:end], size[:end], 2 * n + 32, case.dtype)
+    _near("h_final", _np(h_final), fin, fin_size, 2 * n + 32)
+    return h, size
+
+
+def _check_bwd(case, got, h, size, kept=None):
+    args, h0 = case.ref()
+    dhf = None if case.dhf is None else _np(case.dhf)
+    n, end = case.longest, case.end
+    used = list(args)
+    if kept is None:
+        before = G.states_before(h, case.bounds, h0)
+    else:
+        used[:3] = kept
+        before = G.states_before(h, case.bounds, h0, anew=h, x=kept[0], ga=kept[1], gi=kept[2], rate=args[3])
+    # magnitudes of the terms of the states that the kernel recomputes
+    _, beta, _, i, x, _, _ = G.gates(*used)
+    h0a = np.zeros((case.S, case.C)) if h0 is None else np.abs(h0)
+    before_size = G.states_before(size, case.bounds, h0a) + np.abs(np.nan_to_num(before))
+    want = G.gated_bwd(*used, case.bounds, before, _np(case.dy), dhf)
+    terms = G.gated_bwd(*used, case.bounds, before_size, _np(case.dy), dhf, absolute=True)
+    for name, t in zip(("dx", "dga", "dgi", "drate", "dh0"), got):
+        rows = name in ("dx", "dga", "dgi")
+        v = _np(t).reshape(case.T, case.C)[:end] if rows else _np(t)
+        w, m = (want[name][:end], terms[name][:end]) if rows else (want[name], terms[name])
+        _near(name, v, w, m, 4 * n + 64 + (case.T if name == "drate" else 0), case.dtype if rows else torch.float32)
+
+
+BOUNDS = {
+    "one": [0, 1], "two": [0, 2], "chunk-1": [0, 127], "chunk": [0, 128], "chunk+1": [0, 129], "three": [0, 300],
+    "ones": list(range(0, 20)), "empty": [0, 0, 5, 5, 5, 128, 128, 256, 300, 300],
+    "edges": [0, 127, 128, 129, 256, 257, 512, 700], "long": [0, 3, 1500, 1501],
+}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("C", [1, 63, 64, 65, 130])
+@pytest.mark.parametrize("which", sorted(BOUNDS))
+def test_packed_sequences(which, C, dtype):
+    b = BOUNDS[which]
+    case = Case(b, C, T=b[-1] + (7 if C != 64 else 0), dtype=dtype, states=C != 65, seed=len(b) + C)
+    y, fin, saved = case.fwd()
+    h, size = _check_fwd(case, y, fin)
+    _check_bwd(case, case.bwd(saved), h, size)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("B,L,C", [(1, 1, 1), (3, 1, 70), (5, 37, 64), (2, 128, 33), (4, 256, 128), (3, 421, 96)])
+def test_sequences_of_one_length(B, L, C, dtype):
+    case = Case([k * L for k in range(B + 1)], C, dtype=dtype, dense=True, wide=C % 2 == 1, states=B != 3, seed=B * L)
+    y, fin, saved = case.fwd()
+    assert y.shape == (B, L, C)
+    h, size = _check_fwd(case, y, fin)
+    got = case.bwd(saved)
+    assert got[0].shape == (B, L, C)
+    _check_bwd(case, got, h, size)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("which,C", [("edges", 65), ("empty", 64), ("ones", 3), ("three", 130)])
+def test_masked_rows(which, C, dtype):
+    """Padding with the type's lowest value, -inf or -1e9 in the gate and inf or NaN elsewhere; one sequence all masked."""
+    case = Case(BOUNDS[which], C, T=BOUNDS[which][-1] + 3, dtype=dtype, masked=True, seed=C)
+    y, fin, saved = case.fwd()
+    h, size = _check_fwd(case, y, fin)
+    got = case.bwd(saved)
+    _check_bwd(case, got, h, size)
+    held = _np(case.ga)[:case.end] <= G.HOLD
+    for t in got[:3]:
+        assert (_np(t)[:case.end][held] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("which,C,masked", [("one", 1, False), ("edges", 65, True), ("empty", 64, False),
+                                            ("long", 130, True), ("chunk+1", 33, False)])
+def test_eight_bit_checkpoint(which, C, masked, dtype):
+    """hold8 keeps exactly what the form says, and the backward pass is that of the kept values."""
+    b = BOUNDS[which]
+    case = Case(b, C, T=b[-1] + 5, dtype=dtype, masked=masked, seed=7)
+    y, fin, saved, kept = case.fwd(hold8=True)
+    h, size = _check_fwd(case, y, fin)
+    want = G.kept(*(_np(t) for t in (case.x, case.ga, case.gi)), case.end)
+    blocks = -(-case.end // 32)
+    for (q, e), w in zip(kept, want):
+        v = G.unpack8(q.cpu().numpy()[:case.end], e.cpu().numpy()[:blocks])
+        assert np.array_equal(v, w[:case.end])
+        assert np.array_equal(_np(pdssm.unpack8((q, e)))[:case.end], w[:case.end])
+    _check_bwd(case, case.bwd(saved, kept), h, size, kept=want)
+
+
+def test_rows_behind_and_untouched_outputs():
+    """Rows behind the last sequence: no output of theirs is written, and what they hold does not matter."""
+    case = Case([0, 40, 130], 65, T=300, seed=3)
+    outs = []
+    for junk in (0.0, math.nan):
+        for t in (case.x, case.ga, case.gi):
+            t[130:] = junk
+        case.dy[130:] = junk
+        d = pdssm.GatedDesc(case.T, case.C, case.S, 0)
+        r = [pdssm.Rows(t.data_ptr(), t.stride(0), None) for t in (case.x, case.ga, case.gi)]
+        y = torch.full((300, 65), 7.0, device=DEV)
+        q = [torch.full((300, 65), 7, dtype=torch.int8, device=DEV) for _ in range(3)]
+        e = [torch.full((10, 65), 7, dtype=torch.int8, device=DEV) for _ in range(3)]
+        fin, saved = torch.empty(2, 65, device=DEV), torch.zeros(3, 65, device=DEV)
+        lib, P = pdssm.load(), ctypes.byref
+        ws = torch.empty(max(1, lib.pdssm_gated_workspace_size(P(d), pdssm.OP_BWD),
+                             lib.pdssm_gated_workspace_size(P(d), pdssm.OP_FWD)), dtype=torch.uint8, device=DEV)
+        s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        p = pdssm._p
+        assert lib.pdssm_gated_fwd(P(d), P(r[0]), P(r[1]), P(r[2]), p(case.rate), p(case.cu), p(case.h0), p(y), p(fin),
+                                   p(saved), pdssm._three(q), pdssm._three(e), p(ws), ws.numel(), None, s) == 0
+        g = [torch.full((300, 65), 7.0, device=DEV) for _ in range(3)]
+        drate, dh0 = torch.empty(65, device=DEV), torch.empty(2, 65, device=DEV)
+        rdy = pdssm.Rows(case.dy.data_ptr(), 65, None)
+        assert lib.pdssm_gated_bwd(P(d), P(r[0]), P(r[1]), P(r[2]), p(case.rate), p(case.cu), p(case.h0), p(saved),
+                                   P(rdy), p(case.dhf), pdssm._three(g), 65, p(drate), p(dh0), p(ws), ws.numel(), None,
+                                   s) == 0
+        torch.cuda.synchronize()
+        for t in [y, *q, *g]:
+            assert (t[130:] == 7).all() and not (t[:130] == 7).all()
+        assert all((t[5:] == 7).all() for t in e)
+        outs.append([y, fin, *q, *[t[:5] for t in e], *g, drate, dh0])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_optional_outputs():
+    """h_final, saved, drate and dh0 may be left out; what remains is the same."""
+    case = Case([0, 100, 150], 30, seed=5)
+    y, fin, saved = case.fwd()
+    got = case.bwd(saved)
+    lib, P, p = pdssm.load(), ctypes.byref, pdssm._p
+    d = pdssm.GatedDesc(case.T, case.C, case.S, 0)
+    r = [pdssm.Rows(t.data_ptr(), t.stride(0), None) for t in (case.x, case.ga, case.gi)]
+    n = max(lib.pdssm_gated_workspace_size(P(d), k) for k in (pdssm.OP_FWD, pdssm.OP_BWD))
+    ws = torch.empty(max(n, 1), dtype=torch.uint8, device=DEV)
+    s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    y2, g = torch.empty_like(y), [torch.empty(150, 30, device=DEV) for _ in range(3)]
+    assert lib.pdssm_gated_fwd(P(d), P(r[0]), P(r[1]), P(r[2]), p(case.rate), p(case.cu), p(case.h0), p(y2), None, None,
+                               None, None, p(ws), ws.numel(), None, s) == 0
+    rdy = pdssm.Rows(case.dy.data_ptr(), 30, None)
+    assert lib.pdssm_gated_bwd(P(d), P(r[0]), P(r[1]), P(r[2]), p(case.rate), p(case.cu), p(case.h0), p(saved), P(rdy),
+                               p(case.dhf), pdssm._three(g), 30, None, None, p(ws), ws.numel(), None, s) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(y2, y) and all(torch.equal(a, b) for a, b in zip(g, got))
+
+
+def test_a_nan_stays_in_its_sequence_and_channel():
+    case = Case([0, 90, 400, 900], 66, seed=9)
+    y0, f0, s0 = case.fwd()
+    g0 = case.bwd(s0)
+    case.x[200, 5] = math.nan
+    y, f, saved = case.fwd()
+    g = case.bwd(saved)
+    assert torch.isnan(y[200:400, 5]).all() and torch.isnan(f[1, 5])
+    keep = torch.ones_like(y, dtype=torch.bool)
+    keep[200:400, 5] = False
+    assert torch.equal(y[keep], y0[keep])
+    keep[90:400, 5] = False
+    for a, b in zip(g[:3], g0[:3]):
+        assert torch.equal(a[keep], b[keep])
+    other = [c for c in range(66) if c != 5]
+    assert torch.equal(g[3][other], g0[3][other]) and torch.equal(g[4][[0, 2]], g0[4][[0, 2]])
+
+
+@pytest.mark.parametrize("T,C,S", [(40000, 3, 1), (20000, 130, 2), (9000, 64, 400)])
+def test_long_sequences_and_repeatability(T, C, S):
+    """Hundreds of chunks in a row, and the same bits in every run."""
+    cuts = np.sort(np.random.default_rng(T).integers(0, T + 1, S - 1)).tolist()
+    case = Case([0, *cuts, T], C, dtype=torch.float32, seed=T)
+    first = None
+    for _ in range(5):
+        y, fin, saved = case.fwd(check=False)
+        got = [y, fin, *case.bwd(saved, check=False)]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+    h, size = _check_fwd(case, y, fin)
+    _check_bwd(case, got[2:], h, size)
+
+
+def test_bounds_out_of_order_are_reported():
+    case = Case([0, 40, 100], 20, seed=1)
+    for bad in ([0, 200, 100], [0, -5, 100], [3, 40, 100], [0, 60, 40], [0, 40, 101]):
+        cu = torch.tensor(bad, dtype=torch.int32, device=DEV)
+        with pytest.raises(pdssm.PdssmError, match="INDEX"):
+            pdssm.gated_fwd(case.x, case.ga, case.gi, case.rate, cu=cu)
+        saved = torch.zeros(1, 20, device=DEV)
+        with pytest.raises(pdssm.PdssmError, match="INDEX"):
+            pdssm.gated_bwd(case.x, case.ga, case.gi, case.rate, saved, case.dy, cu=cu)
+
+
+def test_no_rows():
+    case = Case([0, 0, 0], 10, T=0)
+    y, fin, saved, kept = case.fwd(hold8=True)
+    assert y.shape == (0, 10) and saved.shape == (0, 10) and torch.equal(fin, case.h0)
+    for k in (None, kept):
+        dx, dga, dgi, drate, dh0 = case.bwd(saved, k)
+        assert dx.shape == (0, 10) and torch.equal(dh0, case.dhf) and (drate == 0).all()
+    z = torch.empty(2, 0, 10, device=DEV)
+    y, fin, _ = pdssm.gated_fwd(z, z, z, case.rate)
+    assert y.shape == (2, 0, 10) and (fin == 0).all()
+    q, e = pdssm.pack8(torch.empty(0, 10, device=DEV))
+    assert pdssm.unpack8((q, e)).shape == (0, 10)
+    w = pdssm.project_wgrad(torch.empty(0, 16, dtype=torch.bfloat16, device=DEV), pdssm.pack8(torch.empty(0, 32, device=DEV)))
+    assert w.shape == (16, 32) and (w == 0).all()
+    h = torch.ones(3, 10, device=DEV)
+    z = torch.empty(0, 10, device=DEV)
+    pdssm.gated_step(z, z, z, case.rate, h)
+    assert (h == 1).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("B,C,pool", [(1, 1, 1), (3, 65, 5), (40, 300, 64), (300, 17, 300)])
+def test_one_token(B, C, pool, dtype):
+    case = Case(list(range(B + 1)), C, dtype=dtype, masked=B == 40, seed=B)
+    order = torch.randperm(pool, generator=torch.Generator().manual_seed(B))[:B].to(torch.int32)
+    h = torch.randn(pool, C, device=DEV)
+    want, size = (G.gated_fwd(*case.ref()[0], case.bounds, _np(h)[order.long().numpy()], absolute=k)[0] for k in (False, True))
+    out = torch.full_like(h, 9.0)
+    got, y = pdssm.gated_step(case.x, case.ga, case.gi, case.rate, h, slots=order.to(DEV), out=out)
+    assert got is out
+    rows = order.long().to(DEV)
+    _near("h", _np(out[rows]), want, size, 34)
+    _near("y", _np(y), want, size, 34, dtype)
+    rest = torch.ones(pool, dtype=torch.bool, device=DEV)
+    rest[rows] = False
+    assert (out[rest] == 9).all()
+    before = h.clone()
+    pdssm.gated_step(case.x, case.ga, case.gi, case.rate, h, slots=order.to(DEV))  # in place
+    assert torch.equal(h[rows], out[rows]) and torch.equal(h[rest], before[rest])
+    own = before[rows].contiguous()
+    pdssm.gated_step(case.x, case.ga, case.gi, case.rate, own)  # row b is state b
+    assert torch.equal(own, out[rows])
+
+
+def test_one_token_refused_and_skipped_rows():
+    case = Case(list(range(6)), 40, seed=2)
+    h = torch.randn(4, 40, device=DEV)
+    start = h.clone()
+    y = torch.full((5, 40), 5.0, device=DEV)
+    ok = torch.tensor([2, -1, 0, -7, 1], dtype=torch.int32, device=DEV)
+    pdssm.gated_step(case.x, case.ga, case.gi, case.rate, h, slots=ok, y=y)
+    assert (y[[1, 3]] == 5).all() and torch.equal(h[3], start[3]) and not torch.equal(h[0], start[0])
+    alone = start.clone()
+    y1 = torch.empty(1, 40, device=DEV)
+    pdssm.gated_step(case.x[:1], case.ga[:1], case.gi[:1], case.rate, alone, slots=ok[:1], y=y1)
+    for slots in ([1, 4, 2, 0, 3], [2, 0, 2, 1, 3]):
+        h = start.clone()
+        with pytest.raises(pdssm.PdssmError, match="INDEX"):
+            pdssm.gated_step(case.x, case.ga, case.gi, case.rate, h,
+                             slots=torch.tensor(slots, dtype=torch.int32, device=DEV))
+    assert torch.equal(h[2], alone[2])  # the first of the two rows that named slot 2
+
+
+def test_steps_equal_the_sequence():
+    """Prefill, then token by token: the states and outputs of one long run."""
+    case = Case([0, 200], 70, seed=4)
+    y, fin, _ = case.fwd()
+    y1, h, _ = pdssm.gated_fwd(case.x[:150], case.ga[:150], case.gi[:150], case.rate,
+                               cu=torch.tensor([0, 150], dtype=torch.int32, device=DEV), h0=case.h0)
+    out = [y1]
+    for t in range(150, 200):
+        h, yt = pdssm.gated_step(case.x[t:t + 1], case.ga[t:t + 1], case.gi[t:t + 1], case.rate, h)
+        out.append(yt)
+    args, h0 = case.ref()
+    size, fin_size = G.gated_fwd(*args, case.bounds, h0, absolute=True)
+    _near("y", _np(torch.cat(out)), _np(y), size, 2 * 432)
+    _near("h", _np(h), _np(fin), fin_size, 2 * 432)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("T,C", [(1, 1), (31, 5), (32, 64), (33, 130), (200, 257), (65, 1024)])
+def test_pack_and_unpack(T, C, dtype):
+    u = (torch.randn(T, C) * torch.exp(2 * torch.randn(C))).to(dtype)
+    u[T // 2, C // 2] = 0
+    if C > 4:
+        u[:, 1] = 0
+        u[0, 2], u[T - 1, 3] = math.nan, math.inf
+        u[0, 4] = torch.finfo(dtype).max
+    if C > 60:
+        u[:, 50] = torch.finfo(dtype).tiny
+        u[:, 51] = 127 * 2.0 ** -3  # the largest magnitude that its exponent holds
+        u[T - 1, 51] = 63.5 * 2.0 ** -3
+    wide = torch.zeros(T, C + 3, dtype=dtype)
+    wide[:, 1:C + 1] = u
+    q, e = pdssm.pack8(wide.to(DEV)[:, 1:C + 1])
+    wq, we = G.pack8(u.double().numpy())
+    ok = np.repeat(we != -128, 32, 0)[:T]
+    assert np.array_equal(e.cpu().numpy(), we) and np.array_equal(q.cpu().numpy()[ok], wq[ok])
+    for t in (torch.float32, torch.bfloat16):
+        v = pdssm.unpack8((q, e), dtype=t)
+        assert v.dtype == t and np.array_equal(_np(v), G.unpack8(q.cpu().numpy(), we), equal_nan=True)
+
+
+@pytest.mark.parametrize("T,M,Dm", [(1, 8, 16), (31, 16, 32), (33, 72, 48), (100, 256, 256), (257, 264, 272), (1000, 136, 528),
+                                    (5000, 520, 64), (64, 1024, 1040), (20000, 64, 32)])
+def test_weight_gradient(T, M, Dm):
+    """Both operands are exact in bf16: a sum of T products is off by T roundings of fp32 at most, of the sum of
+    their magnitudes."""
+    dP = torch.randn(T, M).to(torch.bfloat16).to(DEV)
+    u8 = pdssm.pack8(torch.randn(T, Dm).to(torch.bfloat16).to(DEV))
+    u, p = _np(pdssm.unpack8(u8)), _np(dP)
+    dW = pdssm.project_wgrad(dP, u8)
+    assert dW.shape == (M, Dm)
+    _near("dW", _np(dW), p.T @ u, np.abs(p).T @ np.abs(u), T + 2)
+    assert torch.equal(dW, pdssm.project_wgrad(dP, u8))
+
+
+def test_weight_gradient_of_values_that_are_not_finite():
+    dP = torch.randn(70, 16).to(torch.bfloat16).to(DEV)
+    u = torch.randn(70, 32).to(DEV)
+    want = pdssm.project_wgrad(dP, pdssm.pack8(u))
+    u[40, 3] = math.nan
+    got = pdssm.project_wgrad(dP, pdssm.pack8(u))
+    keep = [c for c in range(32) if c != 3]
+    assert torch.isnan(got[:, 3]).all() and torch.equal(got[:, keep], want[:, keep])
+    dP[69, 5] = math.inf
+    got = pdssm.project_wgrad(dP, pdssm.pack8(u))
+    assert not torch.isfinite(got[5]).any() and torch.equal(got[:5][:, keep], want[:5][:, keep])
+
+
+def _all_ops(case, kept=True):
+    y, fin, saved, k = case.fwd(hold8=True, check=False)
+    g = case.bwd(saved, k if kept else None, check=False)
+    dP = torch.cat([t.reshape(case.T, case.C) for t in g[:3]], 1).to(torch.bfloat16)
+    h, ys = pdssm.gated_step(case.x[:case.S], case.ga[:case.S], case.gi[:case.S], case.rate, fin, out=torch.empty_like(fin),
+                             check=False)
+    dW = pdssm.project_wgrad(dP.contiguous(), k[0])
+    return [y, fin, saved, *g, h, ys, dW, pdssm.unpack8(k[1])]
+
+
+def test_on_another_stream():
+    case = Case([0, 100, 700], 48, T=700, dtype=torch.bfloat16, seed=8)
+    want = _all_ops(case)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        got = _all_ops(case)
+    s.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    # handed over as an argument: the scratch and outputs must outlive the call
+    outs = []
+    for _ in range(3):
+        y, fin, saved = case.fwd(check=False, stream=s)
+        outs.append((y, case.bwd(saved, check=False, stream=s)[0]))
+    torch.empty(1 << 20, device=DEV).fill_(1.0)
+    s.synchronize()
+    for y, dx in outs:
+        assert torch.equal(y, want[0])
+    y, fin, saved = case.fwd(stream=s)
+    assert torch.equal(y, want[0]) and torch.equal(case.bwd(saved, stream=s)[0], outs[0][1])
+
+
+def test_captured_and_replayed():
+    """A graph of the whole set, replayed with new inputs and eager work in between."""
+    case = Case([0, 130, 130, 1000], 80, T=1003, dtype=torch.bfloat16, seed=6)
+    _all_ops(case)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = _all_ops(case)
+    for k in range(4):
+        with torch.no_grad():
+            case.x.copy_(torch.randn_like(case.x))
+            case.dy.copy_(torch.randn_like(case.dy))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        want = _all_ops(case)
+        torch.cuda.synchronize()
+        for n, (a, b) in enumerate(zip(got, want)):
+            rows = case.end if a.dim() == 2 and a.shape[0] == case.T else a.shape[0]
+            if n == 10:  # the weight gradient sums over rows behind the last sequence too, which nobody wrote
+                continue
+            assert torch.equal(a[:rows], b[:rows]), (k, n)
+
+
+def test_layer_step_together():
+    """A gated layer as it is trained and served: projection to x, ga, gi, recurrence with its activations and the
+    layer's input kept in 8 bits, backward, weight gradient; then prefill and tokens."""
+    B, L, Dm, C = 2, 200, 64, 64
+    g = torch.Generator().manual_seed(11)
+    u = torch.randn(B, L, Dm, generator=g).to(torch.bfloat16).to(DEV)
+    W = (torch.randn(3, C, Dm, generator=g) / 8).to(torch.bfloat16).to(DEV)  # x, ga and gi as three heads of N = 32
+    P = torch.view_as_real(pdssm.project(u, Wb=W)["b"]).reshape(B, L, 3 * C).to(torch.bfloat16)
+    x, ga, gi = P.split(C, -1)
+    rate = torch.full((C,), 0.3, device=DEV)
+    u8 = pdssm.pack8(u)
+    y, fin, saved, kept = pdssm.gated_fwd(x, ga, gi, rate, hold8=True)
+    dy = torch.randn(B, L, C, generator=g).to(torch.bfloat16).to(DEV)
+    grads = pdssm.gated_bwd(*kept, rate, saved, dy)
+    dP = torch.cat(grads[:3], -1)
+    dW = pdssm.project_wgrad(dP, u8)
+    # the reference from the same kept values and the same rounded dP
+    bounds = [0, L, 2 * L]
+    args = [_np(t).reshape(B * L, C) for t in (x, ga, gi)]
+    h, _ = G.gated_fwd(*args, _np(rate), bounds)
+    v = G.kept(*args, B * L)
+    before = G.states_before(h, bounds, None, anew=h, x=v[0], ga=v[1], gi=v[2], rate=_np(rate))
+    want = G.gated_bwd(*v, _np(rate), bounds, before, _np(dy).reshape(B * L, C))
+    for t, key in zip(grads, ("dx", "dga", "dgi")):
+        got = _np(t).reshape(B * L, C)
+        # 2^-8 of each value, and 4 * 200 + 64 roundings of terms that are of the size of the largest value
+        assert (np.abs(got - want[key]) <= 2.0 ** -8 * np.abs(want[key]) + 864 * U * 20 * np.abs(want[key]).max()).all()
+    p, uu = _np(dP).reshape(B * L, 3 * C), G.unpack8(*(t.cpu().numpy() for t in u8))
+    _near("dW", _np(dW), p.T @ uu, np.abs(p).T @ np.abs(uu), B * L + 2)
+    # serving: the first 150 rows at once, the rest token by token
+    _, hs, _ = pdssm.gated_fwd(*(t[:, :150].contiguous() for t in (x, ga, gi)), rate)
+    for t in range(150, L):
+        hs, yt = pdssm.gated_step(x[:, t], ga[:, t], gi[:, t], rate, hs)
+    size = np.abs(h).max()
+    assert (np.abs(_np(hs) - _np(fin)) <= 864 * U * 20 * size).all()
+
+
+def test_weight_gradient_of_a_scan():
+    """The bf16 gradients of the PD scan are the rows of a projection's weight gradient as they are."""
+    from paper_2605_19150_amd.inputs import make_inputs
+    B, L, H, N, K, Dm = 2, 70, 3, 32, 4, 64
+    inp = make_inputs(B=B, L=L, H=H, N=N, K=K, seed=1)
+    T = {k: torch.from_numpy(np.ascontiguousarray(v)).to(DEV) for k, v in inp.items()}
+    D, b, c = (torch.view_as_real(T[k]).to(torch.bfloat16).contiguous() for k in ("D", "b", "c"))
+    _, _, saved = pdssm.scan_fwd(T["idx"], T["pi"], D, b, c)
+    _, db, dc, _ = pdssm.scan_bwd(T["idx"], T["pi"], D, b, c, saved, T["dy"])
+    u8 = pdssm.pack8(torch.randn(B, L, Dm, device=DEV).to(torch.bfloat16))
+    for g in (db, dc):
+        dW = pdssm.project_wgrad(g, u8)
+        p, u = _np(g).reshape(B * L, 2 * H * N), _np(pdssm.unpack8(u8))
+        _near("dW", _np(dW), p.T @ u, np.abs(p).T @ np.abs(u), B * L + 2)
+
+
+def test_refused_tensors():
+    case = Case([0, 50], 10, seed=1)
+    cu, rate = case.cu, case.rate
+    x, ga, gi = (t.contiguous() for t in (case.x, case.ga, case.gi))
+    saved = torch.zeros(1, 10, device=DEV)
+    with pytest.raises(TypeError):
+        pdssm.gated_fwd(x, ga.to(torch.bfloat16), gi, rate, cu=cu)
+    with pytest.raises(TypeError):
+        pdssm.gated_fwd(x.half(), ga.half(), gi.half(), rate, cu=cu)
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x, ga, gi[:, :9], rate, cu=cu)
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x, ga, gi, rate)  # [T,C] without bounds
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x[None], ga[None], gi[None], rate, cu=cu)
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x, ga, gi, rate.cpu(), cu=cu)
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x.t().contiguous().t(), ga, gi, rate, cu=cu)
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x[:1].expand(50, 10), ga, gi, rate, cu=cu)
+    with pytest.raises(TypeError):
+        pdssm.gated_fwd(x, ga, gi, rate, cu=cu.long())
+    with pytest.raises(ValueError):
+        pdssm.gated_fwd(x, ga, gi, rate, cu=cu, h0=torch.zeros(2, 10, device=DEV))
+    with pytest.raises(ValueError):
+        pdssm.gated_bwd(x, ga, gi, rate, saved[:0], case.dy, cu=cu)
+    with pytest.raises(TypeError):
+        pdssm.gated_bwd(pdssm.pack8(x), ga, gi, rate, saved, case.dy, cu=cu)
+    with pytest.raises(ValueError):
+        pdssm.gated_step(x, ga, gi, rate, torch.zeros(60, 9, device=DEV))
+    with pytest.raises(pdssm.PdssmError):
+        pdssm.gated_step(x, ga, gi, rate, torch.zeros(40, 10, device=DEV))  # more rows than states
+    with pytest.raises(pdssm.PdssmError):
+        pdssm.project_wgrad(torch.zeros(50, 12, dtype=torch.bfloat16, device=DEV), pdssm.pack8(torch.zeros(50, 16, device=DEV)))
+    with pytest.raises(ValueError):
+        pdssm.project_wgrad(torch.zeros(49, 16, dtype=torch.bfloat16, device=DEV), pdssm.pack8(torch.zeros(50, 16, device=DEV)))
+    with pytest.raises(TypeError):
+        pdssm.project_wgrad(torch.zeros(50, 16, device=DEV), pdssm.pack8(torch.zeros(50, 16, device=DEV)))
