@@ -8,9 +8,23 @@
 // dh_final added at a sequence's last row) and beta = sqrt(1 - a^2):
 //
 //   dx_t = g_t beta_t i_t              dgi_t = g_t beta_t x_t i_t (1 - i_t)
-//   s ds_t = g_t s_t (i_t x_t a_t^2 / beta_t - a_t h_{t-1})
-//   dga_t = s ds_t (1 - r_t)           drate = sum_t s ds_t / rate
+//   w_t = g_t s_t (i_t x_t a_t^2 / beta_t - a_t h_{t-1})
+//   dga_t = w_t (1 - r_t)              drate = sum_t w_t / rate
 //   dh0 = a_0 g_0
+//
+// One read of the inputs.  The rows of all sequences are one axis, cut into
+// chunks of kGatedChunk rows without regard to where sequences begin (a row
+// that begins one drops what comes from its left), so packed sequences of any
+// lengths make equal pieces of work.  A workgroup has one chunk of 64 channels:
+// eight waves of 16 rows, a channel a lane.  A wave folds its rows into one
+// step (A, B): h_out = A h_in + B; the wave steps are folded in LDS into the
+// chunk's; and the state that enters the chunk comes from the chunks before
+// it, whose workgroups publish their step as soon as they have it and the state
+// behind them when they know it: a chunk takes the nearest known state and the
+// steps from there on (chunk_entry).  Then the rows run again, from registers.
+//
+// Every fold goes in row order from left to right (the backward one from right
+// to left), whatever was known when: results do not depend on timing.
 #include "pdssm_gated.h"
 
 #include "pdssm_device.h"
@@ -19,118 +33,513 @@
 namespace pdssm {
 namespace {
 
-__device__ __forceinline__ float row_get(const RowsIn& r, int io, int kept, int C, int t, int c, bool gate = false) {
-    const size_t o = (size_t)t * r.ld + c;
-    if (kept) {
-        const int q = static_cast<const int8_t*>(r.p)[o];
-        if (gate && q == kKeptLow) return -INFINITY;
-        return (float)q * kept_scale(r.e[(size_t)(t / kKeptRows) * C + c]);
-    }
-    return io == kRowBf16 ? Entry<kRowBf16>::get(static_cast<const uint16_t*>(r.p)[o]) : static_cast<const float*>(r.p)[o];
+// Rows of a wave, and waves of a workgroup, in each direction.
+#ifndef FWD_ROWS
+#define FWD_ROWS 16
+#endif
+#ifndef BWD_ROWS
+#define BWD_ROWS 8
+#endif
+#ifndef FWD_OCC
+#define FWD_OCC 4
+#endif
+#ifndef BWD_OCC
+#define BWD_OCC 4
+#endif
+#ifndef TOGETHER
+#define TOGETHER 2
+#endif
+constexpr int kTogether = TOGETHER;
+constexpr int kFwdRows = FWD_ROWS, kBwdRows = BWD_ROWS;
+
+// ------------------------------------------------------------------ workspace
+// A ticket, then a word for every chunk and channel: empty, a chunk's step
+// (A in the high half, which is never negative; B in the low half), or the
+// state behind it (sign bit of the high half set).  Value and kind are one
+// 8-byte word, so a reader needs no fence.
+constexpr uint64_t kEmpty = ~0ull;
+constexpr size_t kWordsAt = 256;
+
+__host__ __device__ inline int chunks_of(int T) { return (T + kGatedChunk - 1) / kGatedChunk; }
+__host__ __device__ inline int blocks_of(int C) { return (C + 63) / 64; }
+inline size_t words_of(int T, int C) { return (size_t)chunks_of(T) * blocks_of(C) * 64; }
+
+__device__ __forceinline__ uint64_t step_word(float A, float B) {
+    return (uint64_t)(__float_as_uint(A) & 0x7fffffffu) << 32 | __float_as_uint(B);
 }
-__device__ __forceinline__ void row_put(void* p, size_t o, int io, float v) {
-    if (io == kRowBf16) static_cast<uint16_t*>(p)[o] = Entry<kRowBf16>::put(v);
-    else static_cast<float*>(p)[o] = v;
+__device__ __forceinline__ uint64_t state_word(float h) { return 0x8000000000000000ull | __float_as_uint(h); }
+__device__ __forceinline__ void put_word(uint64_t* p, uint64_t w) {
+    __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-__device__ __forceinline__ void seq_rows(const GatedArgs& a, int s, int& t0, int& t1) {
-    if (!a.cu) {
-        t0 = s * a.L;
-        t1 = t0 + a.L;
-        return;
-    }
-    t0 = a.cu[s];
-    t1 = a.cu[s + 1];
-    bool bad = t0 < 0 || t1 < t0 || t1 > a.T || (s == 0 && t0 != 0);
-    t0 = min(max(t0, 0), a.T);
-    t1 = min(max(t1, t0), a.T);
-    if (bad) report_index_error(a.status);
+__global__ __launch_bounds__(256) void k_gated_clear(unsigned* ticket, uint64_t* words, size_t n) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i == 0) *ticket = 0;
+    if (i < n) words[i] = kEmpty;
 }
 
-__global__ void k_gated_fwd(GatedArgs a) {
-    const int c = blockIdx.x * blockDim.x + threadIdx.x, s = blockIdx.y;
-    if (c >= a.C) return;
-    int t0, t1;
-    seq_rows(a, s, t0, t1);
-    const float rate = a.rate[c];
-    float h = a.h0 ? a.h0[(size_t)s * a.C + c] : 0.f;
-    for (int t = t0; t < t1; ++t) {
-        if (a.saved && t % kGatedChunk == 0) a.saved[(size_t)(t / kGatedChunk) * a.C + c] = t == t0 ? 0.f : h;
-        const Gate g = gate_of(row_get(a.ga, a.io, 0, a.C, t, c), row_get(a.gi, a.io, 0, a.C, t, c), rate);
-        const float b = g.hold ? 0.f : g.beta * g.i * row_get(a.x, a.io, 0, a.C, t, c);
-        h = fmaf(1.f + g.em, h, b);
-        row_put(a.y, (size_t)t * a.C + c, a.io, h);
-    }
-    if (a.h_final) a.h_final[(size_t)s * a.C + c] = h;
-}
+// The state (or gradient) that enters a chunk, for the 64 channels of a wave:
+// near points at the words of the chunk it comes from, step is the distance to
+// the next one further away, n their number.  Words are looked at in batches,
+// the nearest first, until one has a state with no gap in front of it; then
+// they are folded from there towards the chunk: a state sets the value, a step
+// advances it.  Chunks are handed out in the order in which they depend on
+// each other (the ticket), so the chunks waited for are running or done, the
+// first one waits for nobody, and every wait ends; a wait of kWaitLimit looks
+// (over a second) ends all the same, reports PDSSM_ERR_HIP and gives NaN.
+constexpr int kBatch = 8, kBatches = 8;
+constexpr int kWaitLimit = 1 << 20;
+constexpr int kErrWait = -4;  // PDSSM_ERR_HIP
 
-// The 8-bit form of x, ga and gi: rows of one block that lie in a sequence.
-__global__ void k_gated_keep(GatedArgs a) {
-    const int c = blockIdx.x * blockDim.x + threadIdx.x, k = blockIdx.y;
-    if (c >= a.C) return;
-    const int end = a.cu ? min(a.T, max(0, a.cu[a.S])) : a.T;
-    const int t0 = k * kKeptRows, t1 = min(t0 + kKeptRows, end);
-    if (t0 >= t1) return;
-    for (int n = 0; n < 3; ++n) {
-        const RowsIn& r = n == 0 ? a.x : n == 1 ? a.ga : a.gi;
-        uint32_t top = 0;
-        for (int t = t0; t < t1; ++t) {
-            if (row_get(a.ga, a.io, 0, a.C, t, c) <= kGateHold) continue;
-            top = max(top, __float_as_uint(row_get(r, a.io, 0, a.C, t, c)) & 0x7fffffffu);
-        }
-        const int e = kept_exponent(top);
-        a.e[n][(size_t)k * a.C + c] = (int8_t)e;
-        for (int t = t0; t < t1; ++t) {
-            const bool hold = row_get(a.ga, a.io, 0, a.C, t, c) <= kGateHold;
-            a.q[n][(size_t)t * a.C + c] =
-                hold ? (n == 1 ? kKeptLow : 0) : (int8_t)kept_code(row_get(r, a.io, 0, a.C, t, c), kept_inverse(e), kept_limit(e));
-        }
+// Folds words d * kBatch .. of the n into h; known: h is a value; gap: an empty word.
+__device__ __forceinline__ void fold_batch(const uint64_t* near, ptrdiff_t step, int n, int d, float& h, bool& known,
+                                           bool& gap) {
+    uint64_t w[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+        const int i = d * kBatch + j;
+        w[j] = i < n ? __hip_atomic_load(near + i * step + lane_id(), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : kEmpty;
+    }
+    gap = false;
+#pragma unroll
+    for (int j = kBatch - 1; j >= 0; --j) {
+        const uint32_t hi = (uint32_t)(w[j] >> 32);
+        const float lo = __uint_as_float((uint32_t)w[j]);
+        const bool state = (int)hi < 0, empty = w[j] == kEmpty;
+        h = state ? lo : fmaf(__uint_as_float(hi), h, lo);
+        known = !empty && (state || known);
+        gap |= empty;
     }
 }
 
-__global__ void k_gated_bwd(GatedArgs a, float* part) {
-    const int c = blockIdx.x * blockDim.x + threadIdx.x, s = blockIdx.y;
-    if (c >= a.C) return;
-    int t0, t1;
-    seq_rows(a, s, t0, t1);
-    const float rate = a.rate[c];
-    float g = a.dhf ? a.dhf[(size_t)s * a.C + c] : 0.f, sum = 0.f;
-    float before[kGatedChunk];
-    for (int hi = t1; hi > t0;) {
-        const int lo = max(t0, (hi - 1) / kGatedChunk * kGatedChunk);
-        float h = lo > t0 ? a.saved[(size_t)(lo / kGatedChunk) * a.C + c] : a.h0 ? a.h0[(size_t)s * a.C + c] : 0.f;
-        for (int t = lo; t < hi; ++t) {
-            before[t - lo] = h;
-            const Gate k = gate_of(row_get(a.ga, a.io, a.kept, a.C, t, c, true), row_get(a.gi, a.io, a.kept, a.C, t, c), rate);
-            h = fmaf(1.f + k.em, h, k.hold ? 0.f : k.beta * k.i * row_get(a.x, a.io, a.kept, a.C, t, c));
+__device__ __forceinline__ float chunk_entry(const uint64_t* near, ptrdiff_t step, int n, int* status) {
+    for (int looks = 0; looks < kWaitLimit; ++looks) {
+        float h = 0.f;
+        for (int d = 0; d < kBatches; ++d) {
+            bool known = false, gap;
+            fold_batch(near, step, n, d, h, known, gap);
+            if (__all(known)) {
+                // nearer words may have become states since: the same bits as the fold gives
+                while (--d >= 0) fold_batch(near, step, n, d, h, known, gap);
+                return h;
+            }
+            if (__any(gap && !known)) break;  // a chunk in front of the nearest state is not folded yet
         }
-        for (int t = hi - 1; t >= lo; --t) {
-            const Gate k = gate_of(row_get(a.ga, a.io, a.kept, a.C, t, c, true), row_get(a.gi, a.io, a.kept, a.C, t, c), rate);
-            const float x = k.hold ? 0.f : row_get(a.x, a.io, a.kept, a.C, t, c);
-            const float ac = 1.f + k.em, gi = k.hold ? 0.f : k.i, sr = rate * k.r;
-            g += row_get(a.dy, a.io, 0, a.C, t, c);
-            const float dx = g * k.beta * gi;
-            const float ds = k.hold ? 0.f : g * sr * (gi * x * ac * ac / k.beta - ac * before[t - lo]);
-            const size_t o = (size_t)t * a.ldd + c;
-            row_put(a.d[0], o, a.io, k.hold ? 0.f : dx);
-            row_put(a.d[1], o, a.io, ds * (1.f - k.r));
-            row_put(a.d[2], o, a.io, k.hold ? 0.f : dx * x * (1.f - gi));
-            sum += ds;
-            g *= ac;
-        }
-        hi = lo;
+        __builtin_amdgcn_s_sleep(2);
     }
-    if (a.dh0) a.dh0[(size_t)s * a.C + c] = g;
-    part[(size_t)s * a.C + c] = sum;
+    if (status && lane_id() == 0) *status = kErrWait;
+    return __uint_as_float(0x7fc00000u);
 }
-__global__ void k_gated_rate(const float* part, const float* rate, float* drate, int n, int C) {
-    const int c = blockIdx.x * blockDim.x + threadIdx.x;
-    if (c >= C) return;
+
+// ------------------------------------------------------------------ sequences
+// Sequence of row t, or -1 outside all of them: the last s with cu[s] <= t.
+__device__ __forceinline__ int sequence_of(const GatedArgs& a, int t) {
+    if (t < 0 || t >= a.T) return -1;
+    if (!a.cu) return t / a.L;
+    int lo = 0, hi = a.S + 1;  // cu[lo - 1] <= t < cu[hi], as far as cu is in order
+    while (lo < hi) {
+        const int m = (lo + hi) >> 1;
+        if (a.cu[m] <= t) lo = m + 1;
+        else hi = m;
+    }
+    return lo == a.S + 1 ? -1 : lo - 1;
+}
+
+// What a wave's rows are: bit i of each mask is row i.
+struct RowKinds {
+    uint32_t used, first, last;
+    int id;  // lane i + 1: sequence of row i
+    __device__ __forceinline__ int seq(int i) const { return readlane_i(id, i + 1); }
+};
+
+template <int ROWS>
+__device__ __forceinline__ RowKinds row_kinds(const GatedArgs& a, int row0) {
+    RowKinds k;
+    constexpr uint32_t kAll = (1u << ROWS) - 1;
+    const int lane = lane_id();
+    k.id = lane < ROWS + 2 ? sequence_of(a, row0 - 1 + lane) : -1;
+    const int before = __shfl_up(k.id, 1), after = __shfl_down(k.id, 1);
+    k.used = (uint32_t)(__ballot(k.id >= 0) >> 1) & kAll;
+    k.first = (uint32_t)(__ballot(k.id >= 0 && k.id != before) >> 1) & kAll;
+    k.last = (uint32_t)(__ballot(k.id >= 0 && k.id != after) >> 1) & kAll;
+    return k;
+}
+
+// cu is in order and in range, or the call is reported; out[s] = in[s] (0 if
+// in is null) for the sequences without rows.  By one wave for 64 channels.
+__device__ void empty_sequences(const GatedArgs& a, const float* in, float* out, int c, bool check) {
+    if (!a.cu) return;
+    const int lane = lane_id();
+    for (int s0 = 0; s0 < a.S; s0 += 64) {
+        const int s = s0 + lane;
+        const int lo = s < a.S ? a.cu[s] : 0, hi = s < a.S ? a.cu[s + 1] : 0;
+        if (check && s < a.S && (lo < 0 || hi < lo || hi > a.T || (s == 0 && lo != 0))) report_index_error(a.status);
+        uint64_t none = __ballot(s < a.S && lo == hi);
+        while (none) {
+            const int k = s0 + __builtin_ctzll(none);
+            none &= none - 1;
+            if (out && c < a.C) out[(size_t)k * a.C + c] = in ? in[(size_t)k * a.C + c] : 0.f;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ rows
+// A wave's rows as a buffer: reads behind the last row give 0, stores there
+// are dropped, and so are those of lanes past the last channel, whose offset
+// lies past every buffer.
+struct RowBlock {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t ld;    // bytes from row to row
+    uint32_t last;  // offset of the last row (the scalar offset stays within the buffer)
+    __device__ __forceinline__ uint32_t at(int i) const { return min((uint32_t)i * ld, last); }
+};
+constexpr uint32_t kPast = 0x80000000u;  // 16 rows of at most 2^26 bytes and an entry end below it
+
+template <int ROWS>
+__device__ __forceinline__ RowBlock row_block_of(const void* p, int64_t ld, int size, int T, int C, int row0) {
+    RowBlock b;
+    const int n = min(T - row0, ROWS);
+    b.ld = (uint32_t)ld * size;
+    b.last = n > 0 ? (uint32_t)(n - 1) * b.ld : 0;
+    b.r = row_block(static_cast<const char*>(p) + (n > 0 ? (int64_t)row0 * ld * size : 0),
+                    n > 0 ? b.last + (uint32_t)C * size : 0);
+    return b;
+}
+
+template <class T>
+__device__ __forceinline__ T load_entry(const RowBlock& b, int i, uint32_t voff) {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(b.r, voff, b.at(i), 0));
+    else if constexpr (sizeof(T) == 2) return (T)__builtin_amdgcn_raw_buffer_load_b16(b.r, voff, b.at(i), 0);
+    else return (T)__builtin_amdgcn_raw_buffer_load_b8(b.r, voff, b.at(i), 0);
+}
+template <class T>
+__device__ __forceinline__ void store_entry(const RowBlock& b, int i, uint32_t voff, T v) {
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), b.r, voff, b.at(i), 0);
+    else if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, b.r, voff, b.at(i), 0);
+    else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, b.r, voff, b.at(i), 0);
+}
+
+// This lane's entries of the wave's rows (rows behind the last: 0).
+template <int IO, int ROWS>
+__device__ __forceinline__ void load_rows(typename Entry<IO>::T (&v)[ROWS], const RowsIn& r, int T, int C, int row0, int c) {
+    using E = typename Entry<IO>::T;
+    const RowBlock b = row_block_of<ROWS>(r.p, r.ld, sizeof(E), T, C, row0);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) v[i] = load_entry<E>(b, i, (uint32_t)c * sizeof(E));
+}
+
+__device__ __forceinline__ int take_ticket(unsigned* ticket) {
+    __shared__ int mine;
+    if (threadIdx.x == 0) mine = (int)atomicAdd(ticket, 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(mine);
+}
+
+// ------------------------------------------------------------------ forward
+template <int IO, bool KEEP>
+__global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_fwd(GatedArgs a) {
+    using En = Entry<IO>;
+    constexpr int kRows = kFwdRows, kWaves = kGatedChunk / kRows;
+    __shared__ float2 fold[kWaves][64];
+    __shared__ int cuts[kWaves];
+    __shared__ float entry[64];
+    __shared__ uint32_t tops[KEEP ? 3 : 1][kWaves][64];
+    __shared__ int some[KEEP ? kWaves : 1];
+    const int wv = wave_id(), lane = lane_id();
+    const int NC = chunks_of(a.T), NB = blocks_of(a.C);
+    uint64_t* words = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt);
+    const int job = NC > 1 ? take_ticket(static_cast<unsigned*>(a.ws)) : blockIdx.x;
+    const int k = job / NB, cb = job - k * NB;
+    const int row0 = k * kGatedChunk + wv * kRows;
+    const int c = cb * 64 + lane;
+    const bool live = c < a.C;
+    const int cc = live ? c : a.C - 1;
+
+    typename En::T x[kRows], ga[kRows], gi[kRows];
+    load_rows<IO>(ga, a.ga, a.T, a.C, row0, cc);
+    load_rows<IO>(gi, a.gi, a.T, a.C, row0, cc);
+    load_rows<IO>(x, a.x, a.T, a.C, row0, cc);
+    const float rate = a.rate[cc];
+    const RowKinds rows = row_kinds<kRows>(a, row0);
+    if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.h0, a.h_final, c, cb == 0);
+
+    if constexpr (KEEP) {
+        // the 8-bit form of the rows in sequences; held rows keep only that
+        uint32_t top[3] = {0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (!(rows.used >> i & 1)) continue;
+            const float l = En::get(ga[i]);
+            const bool hold = l <= kGateHold;
+            const float v[3] = {En::get(x[i]), l, En::get(gi[i])};
+#pragma unroll
+            for (int n = 0; n < 3; ++n) top[n] = max(top[n], hold ? 0u : __float_as_uint(v[n]) & 0x7fffffffu);
+        }
+#pragma unroll
+        for (int n = 0; n < 3; ++n) tops[n][wv][lane] = top[n];
+        if (lane == 0) some[wv] = rows.used != 0;
+        __syncthreads();
+        float inv[3], lim[3];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            constexpr int kShare = kKeptRows / kRows;  // waves of a block
+            uint32_t all = 0;
+            bool any = false;
+#pragma unroll
+            for (int w = 0; w < kShare; ++w) {
+                all = max(all, tops[n][(wv & -kShare) + w][lane]);
+                any |= __builtin_amdgcn_readfirstlane(some[(wv & -kShare) + w]);
+            }
+            const int e = kept_exponent(all);
+            inv[n] = kept_inverse(e);
+            lim[n] = kept_limit(e);
+            if (wv % kShare == 0 && any && live) a.e[n][(size_t)(row0 / kKeptRows) * a.C + c] = (int8_t)e;
+        }
+        const RowBlock q0 = row_block_of<kRows>(a.q[0], a.C, 1, a.T, a.C, row0);
+        const RowBlock q1 = row_block_of<kRows>(a.q[1], a.C, 1, a.T, a.C, row0);
+        const RowBlock q2 = row_block_of<kRows>(a.q[2], a.C, 1, a.T, a.C, row0);
+        const uint32_t voff = live ? (uint32_t)c : kPast;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (!(rows.used >> i & 1)) continue;
+            const float l = En::get(ga[i]);
+            const bool hold = l <= kGateHold;
+            store_entry(q0, i, voff, (int8_t)(hold ? 0 : kept_code(En::get(x[i]), inv[0], lim[0])));
+            store_entry(q1, i, voff, (int8_t)(hold ? kKeptLow : kept_code(l, inv[1], lim[1])));
+            store_entry(q2, i, voff, (int8_t)(hold ? 0 : kept_code(En::get(gi[i]), inv[2], lim[2])));
+        }
+    }
+
+    float av[kRows], bv[kRows];
+    float A = 1.f, B = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const Gate g = gate_of(En::get(ga[i]), En::get(gi[i]), rate);
+        av[i] = 1.f + g.em;
+        bv[i] = g.hold ? 0.f : g.beta * g.i * En::get(x[i]);
+        if (!(rows.used >> i & 1)) av[i] = 1.f, bv[i] = 0.f;
+        if (rows.first >> i & 1) {
+            const float h0 = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+            bv[i] = fmaf(av[i], h0, bv[i]);
+            B = bv[i];
+        } else {
+            B = fmaf(av[i], B, bv[i]);
+            A *= av[i];
+        }
+        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    fold[wv][lane] = make_float2(A, B);
+    if (lane == 0) cuts[wv] = rows.first != 0;
+    __syncthreads();
+    if (wv == 0) {
+        float At = 1.f, Bt = 0.f;
+        bool cut = k == 0;  // nothing from the left reaches the last row
+#pragma unroll 4
+        for (int w = 0; w < kWaves; ++w) {
+            const float2 f = fold[w][lane];
+            const bool cw = __builtin_amdgcn_readfirstlane(cuts[w]);
+            Bt = cw ? f.y : fmaf(f.x, Bt, f.y);
+            At *= f.x;
+            cut |= cw;
+        }
+        uint64_t* mine = words + ((size_t)k * NB + cb) * 64;
+        const bool more = k + 1 < NC;
+        if (more) put_word(mine + lane, cut ? state_word(Bt) : step_word(At, Bt));
+        float h = 0.f;
+        if (k > 0 && !(rows.first & 1)) {
+            h = chunk_entry(mine - (size_t)NB * 64, -(ptrdiff_t)NB * 64, k, a.status);
+            if (more && !cut) put_word(mine + lane, state_word(fmaf(At, h, Bt)));
+        }
+        entry[lane] = h;
+        if (a.saved && live && (rows.used & 1)) a.saved[(size_t)k * a.C + c] = h;
+    }
+    __syncthreads();
+    float h = entry[lane];
+    for (int w = 0; w < wv; ++w) {
+        const float2 f = fold[w][lane];
+        h = __builtin_amdgcn_readfirstlane(cuts[w]) ? f.y : fmaf(f.x, h, f.y);
+    }
+    const RowBlock y = row_block_of<kRows>(a.y, a.C, sizeof(typename En::T), a.T, a.C, row0);
+    const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        h = rows.first >> i & 1 ? bv[i] : fmaf(av[i], h, bv[i]);
+        if (rows.used >> i & 1) store_entry(y, i, voff, En::put(h));
+        if ((rows.last >> i & 1) && live && a.h_final) a.h_final[(size_t)rows.seq(i) * a.C + c] = h;
+    }
+}
+
+// ------------------------------------------------------------------ backward
+// IN: format of x, ga, gi (IO's, or the 8-bit form).
+template <int IO, int IN>
+__global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_bwd(GatedArgs a, float* part) {
+    using En = Entry<IO>;
+    constexpr int kRows = kBwdRows, kWaves = kGatedChunk / kRows;
+    __shared__ float fold[3][kWaves][64];
+    __shared__ int cuts[2][kWaves];
+    __shared__ float entry[64];
+    const int wv = wave_id(), lane = lane_id();
+    const int NC = chunks_of(a.T), NB = blocks_of(a.C);
+    uint64_t* words = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt);
+    const int job = NC > 1 ? take_ticket(static_cast<unsigned*>(a.ws)) : blockIdx.x;
+    const int k = NC - 1 - job / NB, cb = job % NB;  // from the last chunk to the first
+    const int row0 = k * kGatedChunk + wv * kRows;
+    const int c = cb * 64 + lane;
+    const bool live = c < a.C;
+    const int cc = live ? c : a.C - 1;
+
+    typename Entry<IN>::T xr[kRows], gar[kRows], gir[kRows];
+    typename En::T dyr[kRows];
+    load_rows<IN>(gar, a.ga, a.T, a.C, row0, cc);
+    load_rows<IN>(gir, a.gi, a.T, a.C, row0, cc);
+    load_rows<IN>(xr, a.x, a.T, a.C, row0, cc);
+    load_rows<IO>(dyr, a.dy, a.T, a.C, row0, cc);
+    float scale[3] = {1.f, 1.f, 1.f};
+    if constexpr (IN == kRowKept) {
+        const size_t o = (size_t)(min(row0, a.T - 1) / kKeptRows) * a.C + cc;
+        scale[0] = kept_scale(a.x.e[o]);
+        scale[1] = kept_scale(a.ga.e[o]);
+        scale[2] = kept_scale(a.gi.e[o]);
+    }
+    const float rate = a.rate[cc];
+    const float before_chunk = a.saved[(size_t)k * a.C + cc];
+    const RowKinds rows = row_kinds<kRows>(a, row0);
+    if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.dhf, a.dh0, c, cb == 0);
+
+    // gates, and the wave's two folds: states from the left, gradients from the right
+    float x[kRows], em[kRows], r[kRows], in[kRows], hb[kRows], dy[kRows];
+    float A = 1.f, B = 0.f, G = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const float l = Entry<IN>::gate(gar[i], scale[1]);
+        const Gate g = gate_of(l, Entry<IN>::get(gir[i], scale[2]), rate);
+        const bool used = rows.used >> i & 1;
+        const bool off = g.hold || !used;  // no input, no gradient
+        x[i] = off ? 0.f : Entry<IN>::get(xr[i], scale[0]);
+        in[i] = off ? 0.f : g.i;
+        r[i] = used ? g.r : 0.f;
+        em[i] = used ? g.em : 0.f;
+        dy[i] = used ? En::get(dyr[i]) : 0.f;
+        const float av = 1.f + em[i], b = off ? 0.f : g.beta * in[i] * x[i];
+        hb[i] = b;
+        if (rows.first >> i & 1) {
+            const float h0 = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+            B = fmaf(av, h0, b);
+        } else {
+            B = fmaf(av, B, b);
+        }
+        A *= av;
+        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = kRows - 1; i >= 0; --i) {
+        if (rows.last >> i & 1) G = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        G = (1.f + em[i]) * (dy[i] + G);
+    }
+    fold[0][wv][lane] = A;
+    fold[1][wv][lane] = B;
+    fold[2][wv][lane] = G;
+    if (lane == 0) {
+        cuts[0][wv] = rows.first != 0;
+        cuts[1][wv] = rows.last != 0;
+    }
+    __syncthreads();
+    // the last wave's rows end the chunk: it finds what comes from the right
+    if (wv == kWaves - 1) {
+        float At = 1.f, Gt = 0.f;
+        bool cut = k == NC - 1;
+#pragma unroll 4
+        for (int w = kWaves - 1; w >= 0; --w) {
+            const bool cw = __builtin_amdgcn_readfirstlane(cuts[1][w]);
+            Gt = cw ? fold[2][w][lane] : fmaf(fold[0][w][lane], Gt, fold[2][w][lane]);
+            At *= fold[0][w][lane];
+            cut |= cw;
+        }
+        uint64_t* mine = words + ((size_t)k * NB + cb) * 64;
+        if (k > 0) put_word(mine + lane, cut ? state_word(Gt) : step_word(At, Gt));
+        float u = 0.f;
+        if (k + 1 < NC && !(rows.last >> (kRows - 1) & 1)) {
+            u = chunk_entry(mine + (size_t)NB * 64, (ptrdiff_t)NB * 64, NC - 1 - k, a.status);
+            if (k > 0 && !cut) put_word(mine + lane, state_word(fmaf(At, u, Gt)));
+        }
+        entry[lane] = u;
+    }
+    __syncthreads();
+    float h = before_chunk, u = entry[lane];
+    for (int w = 0; w < wv; ++w)
+        h = __builtin_amdgcn_readfirstlane(cuts[0][w]) ? fold[1][w][lane] : fmaf(fold[0][w][lane], h, fold[1][w][lane]);
+    for (int w = kWaves - 1; w > wv; --w)
+        u = __builtin_amdgcn_readfirstlane(cuts[1][w]) ? fold[2][w][lane] : fmaf(fold[0][w][lane], u, fold[2][w][lane]);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (rows.first >> i & 1) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        const float b = hb[i];
+        hb[i] = h;
+        h = fmaf(1.f + em[i], h, b);
+    }
+    RowBlock d[3];
+#pragma unroll
+    for (int n = 0; n < 3; ++n) d[n] = row_block_of<kRows>(a.d[n], a.ldd, sizeof(typename En::T), a.T, a.C, row0);
+    const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = kRows - 1; i >= 0; --i) {
+        if (rows.last >> i & 1) u = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        const float g = dy[i] + u, av = 1.f + em[i];
+        const float beta = __builtin_amdgcn_sqrtf(-em[i] * (2.f + em[i]));
+        const float dx = g * beta * in[i];
+        // r = 0 where the state is held: there beta = 0 and nothing moves
+        const float move = in[i] * x[i] * av * __builtin_amdgcn_rcpf(beta) - hb[i];
+        const float w = r[i] == 0.f ? 0.f : g * (rate * r[i]) * av * move;
+        sum += w;
+        u = av * g;
+        if (rows.used >> i & 1) {
+            store_entry(d[0], i, voff, En::put(dx));
+            store_entry(d[1], i, voff, En::put(w * (1.f - r[i])));
+            store_entry(d[2], i, voff, En::put(dx * x[i] * (1.f - in[i])));
+        }
+        if (i % kTogether == 0) __builtin_amdgcn_sched_barrier(0);
+        if ((rows.first >> i & 1) && live && a.dh0) a.dh0[(size_t)rows.seq(i) * a.C + c] = u;
+    }
+    if (!a.drate) return;
+    __syncthreads();
+    fold[0][wv][lane] = sum;
+    __syncthreads();
+    if (wv == 0 && live) {
+        float all = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) all += fold[0][w][lane];
+        if (NC > 1) part[(size_t)k * a.C + c] = all;
+        else a.drate[c] = all / rate;
+    }
+}
+
+// drate from the chunks' sums: 16 waves take every 16th chunk of 64 channels.
+__global__ __launch_bounds__(1024) void k_gated_rate(const float* part, const float* rate, float* drate, int NC, int C) {
+    __shared__ float sums[16][64];
+    const int wv = wave_id(), lane = lane_id(), c = blockIdx.x * 64 + lane;
     float s = 0.f;
-    for (int k = 0; k < n; ++k) s += part[(size_t)k * C + c];
+    if (c < C)
+        for (int k = wv; k < NC; k += 16) s += part[(size_t)k * C + c];
+    sums[wv][lane] = s;
+    __syncthreads();
+    if (wv != 0 || c >= C) return;
+    s = 0.f;
+    for (int w = 0; w < 16; ++w) s += sums[w][lane];
     drate[c] = s / rate[c];
 }
 
+// No rows at all: out = in for every sequence, and a zero rate gradient.
+__global__ __launch_bounds__(64) void k_gated_none(GatedArgs a, const float* in, float* out) {
+    const int c = blockIdx.x * 64 + threadIdx.x;
+    if (a.cu) empty_sequences(a, in, out, c, blockIdx.x == 0);
+    if (c >= a.C) return;
+    if (!a.cu && out)
+        for (int s = 0; s < a.S; ++s) out[(size_t)s * a.C + c] = in ? in[(size_t)s * a.C + c] : 0.f;
+    if (a.drate) a.drate[c] = 0.f;
+}
+
+template <int IO>
 __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
     const int c = blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
     int slot = b;
@@ -150,33 +559,67 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
         return;
     }
     if (c >= a.C) return;
-    const Gate g = gate_of(row_get(a.ga, a.io, 0, a.C, b, c), row_get(a.gi, a.io, 0, a.C, b, c), a.rate[c]);
+    using En = Entry<IO>;
+    auto at = [&](const RowsIn& r) { return En::get(static_cast<const typename En::T*>(r.p)[(size_t)b * r.ld + c]); };
+    const Gate g = gate_of(at(a.ga), at(a.gi), a.rate[c]);
     const size_t o = (size_t)slot * a.C + c;
-    const float in = g.hold ? 0.f : g.beta * g.i * row_get(a.x, a.io, 0, a.C, b, c);
+    const float in = g.hold ? 0.f : g.beta * g.i * at(a.x);
     const float h = fmaf(1.f + g.em, a.h_in[o], in);
     a.h_out[o] = h;
-    row_put(a.y, (size_t)b * a.C + c, a.io, h);
+    static_cast<typename En::T*>(a.y)[(size_t)b * a.C + c] = En::put(h);
 }
 
 }  // namespace
 
-size_t gated_workspace(int T, int C, int S, bool bwd) { return bwd ? (size_t)S * C * 4 : 0; }
+size_t gated_workspace(int T, int C, int S, bool bwd) {
+    if (chunks_of(T) <= 1) return 0;
+    return kWordsAt + words_of(T, C) * 8 + (bwd ? (size_t)chunks_of(T) * C * 4 : 0);
+}
+
+namespace {
+void clear_words(const GatedArgs& a, hipStream_t s) {
+    const size_t n = words_of(a.T, a.C);
+    hipLaunchKernelGGL(k_gated_clear, dim3((n + 255) / 256), dim3(256), 0, s, static_cast<unsigned*>(a.ws),
+                       reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt), n);
+}
+}  // namespace
 
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(k_gated_fwd, dim3((a.C + 63) / 64, a.S), dim3(64), 0, s, a);
-    if (a.q[0] && a.T)
-        hipLaunchKernelGGL(k_gated_keep, dim3((a.C + 63) / 64, (a.T + kKeptRows - 1) / kKeptRows), dim3(64), 0, s, a);
+    const int NC = chunks_of(a.T), NB = blocks_of(a.C);
+    if (NC == 0) {
+        hipLaunchKernelGGL(k_gated_none, dim3(NB), dim3(64), 0, s, a, a.h0, a.h_final);
+        return hipGetLastError();
+    }
+    if (NC > 1) clear_words(a, s);
+    constexpr int kWaves = kGatedChunk / kFwdRows;
+    auto* f = a.io == kRowBf16 ? (a.q[0] ? k_gated_fwd<kRowBf16, true> : k_gated_fwd<kRowBf16, false>)
+                               : (a.q[0] ? k_gated_fwd<kRowF32, true> : k_gated_fwd<kRowF32, false>);
+    hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a);
     return hipGetLastError();
 }
+
 hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(k_gated_bwd, dim3((a.C + 63) / 64, a.S), dim3(64), 0, s, a, static_cast<float*>(a.ws));
-    if (a.drate)
-        hipLaunchKernelGGL(k_gated_rate, dim3((a.C + 63) / 64), dim3(64), 0, s, static_cast<const float*>(a.ws), a.rate,
-                           a.drate, a.S, a.C);
+    const int NC = chunks_of(a.T), NB = blocks_of(a.C);
+    if (NC == 0) {
+        hipLaunchKernelGGL(k_gated_none, dim3(NB), dim3(64), 0, s, a, a.dhf, a.dh0);
+        return hipGetLastError();
+    }
+    float* part = nullptr;
+    if (NC > 1) {
+        clear_words(a, s);
+        part = reinterpret_cast<float*>(static_cast<char*>(a.ws) + kWordsAt + words_of(a.T, a.C) * 8);
+    }
+    constexpr int kWaves = kGatedChunk / kBwdRows;
+    auto* f = a.io == kRowBf16 ? (a.kept ? k_gated_bwd<kRowBf16, kRowKept> : k_gated_bwd<kRowBf16, kRowBf16>)
+                               : (a.kept ? k_gated_bwd<kRowF32, kRowKept> : k_gated_bwd<kRowF32, kRowF32>);
+    hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a, part);
+    if (NC > 1 && a.drate) hipLaunchKernelGGL(k_gated_rate, dim3(NB), dim3(1024), 0, s, part, a.rate, a.drate, NC, a.C);
     return hipGetLastError();
 }
+
 hipError_t launch_gated_step(const GatedStepArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(k_gated_step, dim3((a.C + 255) / 256, a.B), dim3(256), 0, s, a);
+    auto* f = a.io == kRowBf16 ? k_gated_step<kRowBf16> : k_gated_step<kRowF32>;
+    hipLaunchKernelGGL(f, dim3((a.C + 255) / 256, a.B), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
