@@ -27,6 +27,8 @@
 // to left), whatever was known when: results do not depend on timing.
 #include "pdssm_gated.h"
 
+#include <type_traits>
+
 #include "pdssm_device.h"
 #include "pdssm_gated_math.h"
 
@@ -38,7 +40,7 @@ namespace {
 #define FWD_ROWS 16
 #endif
 #ifndef BWD_ROWS
-#define BWD_ROWS 8
+#define BWD_ROWS 16
 #endif
 #ifndef FWD_OCC
 #define FWD_OCC 4
@@ -149,6 +151,8 @@ __device__ __forceinline__ int sequence_of(const GatedArgs& a, int t) {
 struct RowKinds {
     uint32_t used, first, last;
     int id;  // lane i + 1: sequence of row i
+    uint32_t all;
+    __device__ __forceinline__ bool plain() const { return used == all && first == 0 && last == 0; }
     __device__ __forceinline__ int seq(int i) const { return readlane_i(id, i + 1); }
 };
 
@@ -159,6 +163,7 @@ __device__ __forceinline__ RowKinds row_kinds(const GatedArgs& a, int row0) {
     const int lane = lane_id();
     k.id = lane < ROWS + 2 ? sequence_of(a, row0 - 1 + lane) : -1;
     const int before = __shfl_up(k.id, 1), after = __shfl_down(k.id, 1);
+    k.all = kAll;
     k.used = (uint32_t)(__ballot(k.id >= 0) >> 1) & kAll;
     k.first = (uint32_t)(__ballot(k.id >= 0 && k.id != before) >> 1) & kAll;
     k.last = (uint32_t)(__ballot(k.id >= 0 && k.id != after) >> 1) & kAll;
@@ -221,7 +226,7 @@ __device__ __forceinline__ void store_entry(const RowBlock& b, int i, uint32_t v
 
 // This lane's entries of the wave's rows (rows behind the last: 0).
 template <int IO, int ROWS>
-__device__ __forceinline__ void load_rows(typename Entry<IO>::T (&v)[ROWS], const RowsIn& r, int T, int C, int row0, int c) {
+__device__ __forceinline__ void load_rows(typename Entry<IO>::R (&v)[ROWS], const RowsIn& r, int T, int C, int row0, int c) {
     using E = typename Entry<IO>::T;
     const RowBlock b = row_block_of<ROWS>(r.p, r.ld, sizeof(E), T, C, row0);
 #pragma unroll
@@ -234,6 +239,11 @@ __device__ __forceinline__ int take_ticket(unsigned* ticket) {
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(mine);
 }
+
+// A kernel argument that stays in a scalar register from here on: past the
+// one-lane branch of the ticket the compiler has carried such values in vector
+// registers, and then loops over the lanes for every buffer access.
+__device__ __forceinline__ void keep_scalar(int& v) { asm volatile("" : "+s"(v)); }
 
 // ------------------------------------------------------------------ forward
 template <int IO, bool KEEP>
@@ -249,17 +259,19 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
     uint64_t* words = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt);
     const int job = NC > 1 ? take_ticket(static_cast<unsigned*>(a.ws)) : blockIdx.x;
-    const int k = job / NB, cb = job - k * NB;
+    const int k = __builtin_amdgcn_readfirstlane(job / NB), cb = job - k * NB;
+    keep_scalar(a.T);
+    keep_scalar(a.C);
     const int row0 = k * kGatedChunk + wv * kRows;
     const int c = cb * 64 + lane;
     const bool live = c < a.C;
     const int cc = live ? c : a.C - 1;
 
-    typename En::T x[kRows], ga[kRows], gi[kRows];
+    typename En::R x[kRows], ga[kRows], gi[kRows];
     load_rows<IO>(ga, a.ga, a.T, a.C, row0, cc);
     load_rows<IO>(gi, a.gi, a.T, a.C, row0, cc);
     load_rows<IO>(x, a.x, a.T, a.C, row0, cc);
-    const float rate = a.rate[cc];
+    const float rate2 = a.rate[cc] * kLog2e;
     const RowKinds rows = row_kinds<kRows>(a, row0);
     if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.h0, a.h_final, c, cb == 0);
 
@@ -310,24 +322,32 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
         }
     }
 
+    // most waves' rows are all in one sequence and neither begin nor end it
+    const bool plain = rows.plain();
     float av[kRows], bv[kRows];
     float A = 1.f, B = 0.f;
+    auto gates = [&](auto plain_) {
+        constexpr bool PLAIN = decltype(plain_)::value;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const Gate g = gate_of(En::get(ga[i]), En::get(gi[i]), rate);
-        av[i] = 1.f + g.em;
-        bv[i] = g.hold ? 0.f : g.beta * g.i * En::get(x[i]);
-        if (!(rows.used >> i & 1)) av[i] = 1.f, bv[i] = 0.f;
-        if (rows.first >> i & 1) {
-            const float h0 = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-            bv[i] = fmaf(av[i], h0, bv[i]);
-            B = bv[i];
-        } else {
+        for (int i = 0; i < kRows; ++i) {
+            const float r = recurrence_gate(En::get(ga[i]));
+            const Decay d = decay_of(r, rate2);
+            av[i] = d.a;
+            bv[i] = input_term(r, d.beta2, sigmoid_f(En::get(gi[i])), En::get(x[i]));
+            if constexpr (!PLAIN) {
+                if (!(rows.used >> i & 1)) av[i] = 1.f, bv[i] = 0.f;
+                if (rows.first >> i & 1) {
+                    const float h0 = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+                    B = bv[i] = fmaf(av[i], h0, bv[i]);
+                    continue;
+                }
+            }
             B = fmaf(av[i], B, bv[i]);
             A *= av[i];
         }
-        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
-    }
+    };
+    if (plain) gates(std::true_type{});
+    else gates(std::false_type{});
     fold[wv][lane] = make_float2(A, B);
     if (lane == 0) cuts[wv] = rows.first != 0;
     __syncthreads();
@@ -361,12 +381,18 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
     }
     const RowBlock y = row_block_of<kRows>(a.y, a.C, sizeof(typename En::T), a.T, a.C, row0);
     const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
+    auto emit = [&](auto plain_) {
+        constexpr bool PLAIN = decltype(plain_)::value;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        h = rows.first >> i & 1 ? bv[i] : fmaf(av[i], h, bv[i]);
-        if (rows.used >> i & 1) store_entry(y, i, voff, En::put(h));
-        if ((rows.last >> i & 1) && live && a.h_final) a.h_final[(size_t)rows.seq(i) * a.C + c] = h;
-    }
+        for (int i = 0; i < kRows; ++i) {
+            h = !PLAIN && (rows.first >> i & 1) ? bv[i] : fmaf(av[i], h, bv[i]);
+            if (PLAIN || (rows.used >> i & 1)) store_entry(y, i, voff, En::put(h));
+            if constexpr (!PLAIN)
+                if ((rows.last >> i & 1) && live && a.h_final) a.h_final[(size_t)rows.seq(i) * a.C + c] = h;
+        }
+    };
+    if (plain) emit(std::true_type{});
+    else emit(std::false_type{});
 }
 
 // ------------------------------------------------------------------ backward
@@ -382,14 +408,17 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
     uint64_t* words = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt);
     const int job = NC > 1 ? take_ticket(static_cast<unsigned*>(a.ws)) : blockIdx.x;
-    const int k = NC - 1 - job / NB, cb = job % NB;  // from the last chunk to the first
+    const int turn = __builtin_amdgcn_readfirstlane(job / NB), cb = job - turn * NB;
+    const int k = NC - 1 - turn;  // from the last chunk to the first
+    keep_scalar(a.T);
+    keep_scalar(a.C);
     const int row0 = k * kGatedChunk + wv * kRows;
     const int c = cb * 64 + lane;
     const bool live = c < a.C;
     const int cc = live ? c : a.C - 1;
 
-    typename Entry<IN>::T xr[kRows], gar[kRows], gir[kRows];
-    typename En::T dyr[kRows];
+    typename Entry<IN>::R xr[kRows], gar[kRows], gir[kRows];
+    typename En::R dyr[kRows];
     load_rows<IN>(gar, a.ga, a.T, a.C, row0, cc);
     load_rows<IN>(gir, a.gi, a.T, a.C, row0, cc);
     load_rows<IN>(xr, a.x, a.T, a.C, row0, cc);
@@ -401,40 +430,36 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
         scale[1] = kept_scale(a.ga.e[o]);
         scale[2] = kept_scale(a.gi.e[o]);
     }
-    const float rate = a.rate[cc];
+    const float rate = a.rate[cc], rate2 = rate * kLog2e;
     const float before_chunk = a.saved[(size_t)k * a.C + cc];
     const RowKinds rows = row_kinds<kRows>(a, row0);
     if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.dhf, a.dh0, c, cb == 0);
 
-    // gates, and the wave's two folds: states from the left, gradients from the right
-    float x[kRows], em[kRows], r[kRows], in[kRows], hb[kRows], dy[kRows];
+    // gates, and the wave's two folds: states from the left, gradients from the
+    // right.  hb: the row's input term, later the state before it.  a and beta
+    // are computed anew from r wherever they are needed: with them kept, a
+    // wave's 16 rows would not leave room for a second workgroup on the CU,
+    // which is what hides this one's waits (203 us with rows halved and all
+    // kept, one workgroup a CU, at B16 L2048 C1024 bf16)
+    const bool plain = rows.plain();
+    float r[kRows], in[kRows], hb[kRows];
     float A = 1.f, B = 0.f, G = 0.f;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        const float l = Entry<IN>::gate(gar[i], scale[1]);
-        const Gate g = gate_of(l, Entry<IN>::get(gir[i], scale[2]), rate);
-        const bool used = rows.used >> i & 1;
-        const bool off = g.hold || !used;  // no input, no gradient
-        x[i] = off ? 0.f : Entry<IN>::get(xr[i], scale[0]);
-        in[i] = off ? 0.f : g.i;
-        r[i] = used ? g.r : 0.f;
-        em[i] = used ? g.em : 0.f;
-        dy[i] = used ? En::get(dyr[i]) : 0.f;
-        const float av = 1.f + em[i], b = off ? 0.f : g.beta * in[i] * x[i];
-        hb[i] = b;
-        if (rows.first >> i & 1) {
-            const float h0 = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-            B = fmaf(av, h0, b);
-        } else {
-            B = fmaf(av, B, b);
-        }
-        A *= av;
-        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll
-    for (int i = kRows - 1; i >= 0; --i) {
-        if (rows.last >> i & 1) G = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-        G = (1.f + em[i]) * (dy[i] + G);
+        r[i] = recurrence_gate(Entry<IN>::gate(gar[i], scale[1]));
+        in[i] = sigmoid_f(Entry<IN>::get(gir[i], scale[2]));
+        if (!(rows.used >> i & 1)) r[i] = 0.f, dyr[i] = {};
+        const Decay d = decay_of(r[i], rate2);
+        hb[i] = input_term(r[i], d.beta2, in[i], Entry<IN>::get(xr[i], scale[0]));
+        float h = B;
+        if (rows.first >> i & 1) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        B = fmaf(d.a, h, hb[i]);
+        A *= d.a;
+        // the gradient that leaves the first row: dy of each row times the a's up to it
+        if (!(rows.last & ((1u << i) - 1))) G = fmaf(A, En::get(dyr[i]), G);
+        if ((rows.last & ((2u << i) - 1)) == 1u << i)  // the first that ends a sequence
+            G = fmaf(A, a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f, G);
+        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);  // not more rows at once than registers
     }
     fold[0][wv][lane] = A;
     fold[1][wv][lane] = B;
@@ -464,43 +489,57 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
         }
         entry[lane] = u;
     }
-    __syncthreads();
-    float h = before_chunk, u = entry[lane];
+    // the states before the rows, while that wave may wait
+    float h = before_chunk;
+#pragma unroll 4
     for (int w = 0; w < wv; ++w)
         h = __builtin_amdgcn_readfirstlane(cuts[0][w]) ? fold[1][w][lane] : fmaf(fold[0][w][lane], h, fold[1][w][lane]);
-    for (int w = kWaves - 1; w > wv; --w)
-        u = __builtin_amdgcn_readfirstlane(cuts[1][w]) ? fold[2][w][lane] : fmaf(fold[0][w][lane], u, fold[2][w][lane]);
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        if (rows.first >> i & 1) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        if (!plain && (rows.first >> i & 1)) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
         const float b = hb[i];
         hb[i] = h;
-        h = fmaf(1.f + em[i], h, b);
+        h = fmaf(__builtin_amdgcn_exp2f(-rate2 * r[i]), h, b);
+        // what comes of these is computed again below, not kept
+        asm volatile("" : "+v"(r[i]), "+v"(xr[i]), "+v"(dyr[i]));
     }
-    RowBlock d[3];
+    __syncthreads();
+    float u = entry[lane];
+#pragma unroll 4
+    for (int w = kWaves - 1; w > wv; --w)
+        u = __builtin_amdgcn_readfirstlane(cuts[1][w]) ? fold[2][w][lane] : fmaf(fold[0][w][lane], u, fold[2][w][lane]);
+    RowBlock out[3];
 #pragma unroll
-    for (int n = 0; n < 3; ++n) d[n] = row_block_of<kRows>(a.d[n], a.ldd, sizeof(typename En::T), a.T, a.C, row0);
+    for (int n = 0; n < 3; ++n) out[n] = row_block_of<kRows>(a.d[n], a.ldd, sizeof(typename En::T), a.T, a.C, row0);
     const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
     float sum = 0.f;
+    auto emit = [&](auto plain_) {
+        constexpr bool PLAIN = decltype(plain_)::value;
 #pragma unroll
-    for (int i = kRows - 1; i >= 0; --i) {
-        if (rows.last >> i & 1) u = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-        const float g = dy[i] + u, av = 1.f + em[i];
-        const float beta = __builtin_amdgcn_sqrtf(-em[i] * (2.f + em[i]));
-        const float dx = g * beta * in[i];
-        // r = 0 where the state is held: there beta = 0 and nothing moves
-        const float move = in[i] * x[i] * av * __builtin_amdgcn_rcpf(beta) - hb[i];
-        const float w = r[i] == 0.f ? 0.f : g * (rate * r[i]) * av * move;
-        sum += w;
-        u = av * g;
-        if (rows.used >> i & 1) {
-            store_entry(d[0], i, voff, En::put(dx));
-            store_entry(d[1], i, voff, En::put(w * (1.f - r[i])));
-            store_entry(d[2], i, voff, En::put(dx * x[i] * (1.f - in[i])));
+        for (int i = kRows - 1; i >= 0; --i) {
+            if constexpr (!PLAIN)
+                if (rows.last >> i & 1) u = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+            const float g = En::get(dyr[i]) + u, x = Entry<IN>::get(xr[i], scale[0]);
+            const bool hold = r[i] == 0.f;
+            const Decay d = decay_of(r[i], rate2);
+            const float t = in[i] * __builtin_amdgcn_rsqf(d.beta2);  // i / beta
+            const float dx = hold ? 0.f : g * d.beta2 * t;
+            u = g * d.a;
+            const float w = hold ? 0.f : rate * r[i] * u * fmaf(x * d.a, t, -hb[i]);
+            const float dxx = dx * x;
+            sum += w;
+            if (PLAIN || (rows.used >> i & 1)) {
+                store_entry(out[0], i, voff, En::put(dx));
+                store_entry(out[1], i, voff, En::put(fmaf(-w, r[i], w)));
+                store_entry(out[2], i, voff, En::put(hold ? 0.f : fmaf(-dxx, in[i], dxx)));
+            }
+            if constexpr (!PLAIN)
+                if ((rows.first >> i & 1) && live && a.dh0) a.dh0[(size_t)rows.seq(i) * a.C + c] = u;
+            if (i % kTogether == 0) __builtin_amdgcn_sched_barrier(0);
         }
-        if (i % kTogether == 0) __builtin_amdgcn_sched_barrier(0);
-        if ((rows.first >> i & 1) && live && a.dh0) a.dh0[(size_t)rows.seq(i) * a.C + c] = u;
-    }
+    };
+    if (plain) emit(std::true_type{});
+    else emit(std::false_type{});
     if (!a.drate) return;
     __syncthreads();
     fold[0][wv][lane] = sum;
@@ -561,10 +600,10 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
     if (c >= a.C) return;
     using En = Entry<IO>;
     auto at = [&](const RowsIn& r) { return En::get(static_cast<const typename En::T*>(r.p)[(size_t)b * r.ld + c]); };
-    const Gate g = gate_of(at(a.ga), at(a.gi), a.rate[c]);
+    const float r = recurrence_gate(at(a.ga));
+    const Decay d = decay_of(r, a.rate[c] * kLog2e);
     const size_t o = (size_t)slot * a.C + c;
-    const float in = g.hold ? 0.f : g.beta * g.i * at(a.x);
-    const float h = fmaf(1.f + g.em, a.h_in[o], in);
+    const float h = fmaf(d.a, a.h_in[o], input_term(r, d.beta2, sigmoid_f(at(a.gi)), at(a.x)));
     a.h_out[o] = h;
     static_cast<typename En::T*>(a.y)[(size_t)b * a.C + c] = En::put(h);
 }
