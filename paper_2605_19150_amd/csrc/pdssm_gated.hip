@@ -35,36 +35,25 @@
 namespace pdssm {
 namespace {
 
-// Rows of a wave, and waves of a workgroup, in each direction.
-#ifndef FWD_ROWS
-#define FWD_ROWS 16
-#endif
-#ifndef BWD_ROWS
-#define BWD_ROWS 16
-#endif
-#ifndef FWD_OCC
-#define FWD_OCC 4
-#endif
-#ifndef BWD_OCC
-#define BWD_OCC 4
-#endif
-#ifndef TOGETHER
-#define TOGETHER 2
-#endif
-constexpr int kTogether = TOGETHER;
-constexpr int kFwdRows = FWD_ROWS, kBwdRows = BWD_ROWS;
+// Rows of a wave in each direction, and how many of them the compiler may work
+// on at once (more would cost registers, and with them a workgroup of the CU).
+constexpr int kFwdRows = 16, kBwdRows = 16, kTogether = 4;
 
 // ------------------------------------------------------------------ workspace
-// A ticket, then a word for every chunk and channel: empty, a chunk's step
+// A ticket counter for every 64 channels, kTicketStride bytes apart, then a
+// word for every chunk and channel: empty, a chunk's step
 // (A in the high half, which is never negative; B in the low half), or the
 // state behind it (sign bit of the high half set).  Value and kind are one
 // 8-byte word, so a reader needs no fence.
 constexpr uint64_t kEmpty = ~0ull;
-constexpr size_t kWordsAt = 256;
+constexpr size_t kTicketStride = 256;  // bytes: counters on cache lines of their own
 
 __host__ __device__ inline int chunks_of(int T) { return (T + kGatedChunk - 1) / kGatedChunk; }
 __host__ __device__ inline int blocks_of(int C) { return (C + 63) / 64; }
 inline size_t words_of(int T, int C) { return (size_t)chunks_of(T) * blocks_of(C) * 64; }
+__host__ __device__ inline uint64_t* words_in(void* ws, int NB) {
+    return reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + NB * kTicketStride);
+}
 
 __device__ __forceinline__ uint64_t step_word(float A, float B) {
     return (uint64_t)(__float_as_uint(A) & 0x7fffffffu) << 32 | __float_as_uint(B);
@@ -74,10 +63,10 @@ __device__ __forceinline__ void put_word(uint64_t* p, uint64_t w) {
     __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-__global__ __launch_bounds__(256) void k_gated_clear(unsigned* ticket, uint64_t* words, size_t n) {
+__global__ __launch_bounds__(256) void k_gated_clear(void* ws, int NB, size_t n) {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i == 0) *ticket = 0;
-    if (i < n) words[i] = kEmpty;
+    if (i < (size_t)NB) *reinterpret_cast<unsigned*>(static_cast<char*>(ws) + i * kTicketStride) = 0;
+    if (i < n) words_in(ws, NB)[i] = kEmpty;
 }
 
 // The state (or gradient) that enters a chunk, for the 64 channels of a wave:
@@ -86,7 +75,7 @@ __global__ __launch_bounds__(256) void k_gated_clear(unsigned* ticket, uint64_t*
 // the nearest first, until one has a state with no gap in front of it; then
 // they are folded from there towards the chunk: a state sets the value, a step
 // advances it.  Chunks are handed out in the order in which they depend on
-// each other (the ticket), so the chunks waited for are running or done, the
+// each other (chunk_ticket), so the chunks waited for are running or done, the
 // first one waits for nobody, and every wait ends; a wait of kWaitLimit looks
 // (over a second) ends all the same, reports PDSSM_ERR_HIP and gives NaN.
 constexpr int kBatch = 8, kBatches = 8;
@@ -152,7 +141,8 @@ struct RowKinds {
     uint32_t used, first, last;
     int id;  // lane i + 1: sequence of row i
     uint32_t all;
-    __device__ __forceinline__ bool plain() const { return used == all && first == 0 && last == 0; }
+    // rows that begin or end a sequence or are in none; most waves have no such row
+    __device__ __forceinline__ uint32_t special() const { return (all & ~used) | first | last; }
     __device__ __forceinline__ int seq(int i) const { return readlane_i(id, i + 1); }
 };
 
@@ -217,11 +207,13 @@ __device__ __forceinline__ T load_entry(const RowBlock& b, int i, uint32_t voff)
     else if constexpr (sizeof(T) == 2) return (T)__builtin_amdgcn_raw_buffer_load_b16(b.r, voff, b.at(i), 0);
     else return (T)__builtin_amdgcn_raw_buffer_load_b8(b.r, voff, b.at(i), 0);
 }
+// Nobody reads the outputs here again: stored past the caches (nontemporal),
+// 147 -> 138 us for the backward at B16 L2048 C1024 bf16.
 template <class T>
 __device__ __forceinline__ void store_entry(const RowBlock& b, int i, uint32_t voff, T v) {
-    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), b.r, voff, b.at(i), 0);
-    else if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, b.r, voff, b.at(i), 0);
-    else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, b.r, voff, b.at(i), 0);
+    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), b.r, voff, b.at(i), kLoadStream);
+    else if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, b.r, voff, b.at(i), kLoadStream);
+    else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, b.r, voff, b.at(i), kLoadStream);
 }
 
 // This lane's entries of the wave's rows (rows behind the last: 0).
@@ -233,10 +225,16 @@ __device__ __forceinline__ void load_rows(typename Entry<IO>::R (&v)[ROWS], cons
     for (int i = 0; i < ROWS; ++i) v[i] = load_entry<E>(b, i, (uint32_t)c * sizeof(E));
 }
 
-__device__ __forceinline__ int take_ticket(unsigned* ticket) {
+// A barrier for LDS alone: __syncthreads would also wait for the stores of rows.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The turn of this workgroup among those of its 64 channels (cb), in the order
+// in which they begin.  One counter for all of them would hand out tickets
+// 12.5 ns apart, 51 us at B16 L2048 C1024, as long as the data takes.
+__device__ __forceinline__ int chunk_ticket(void* ws, int cb) {
     __shared__ int mine;
-    if (threadIdx.x == 0) mine = (int)atomicAdd(ticket, 1u);
-    __syncthreads();
+    if (threadIdx.x == 0) mine = (int)atomicAdd(reinterpret_cast<unsigned*>(static_cast<char*>(ws) + cb * kTicketStride), 1u);
+    lds_barrier();
     return __builtin_amdgcn_readfirstlane(mine);
 }
 
@@ -247,7 +245,7 @@ __device__ __forceinline__ void keep_scalar(int& v) { asm volatile("" : "+s"(v))
 
 // ------------------------------------------------------------------ forward
 template <int IO, bool KEEP>
-__global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_fwd(GatedArgs a) {
+__global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, 6) void k_gated_fwd(GatedArgs a) {
     using En = Entry<IO>;
     constexpr int kRows = kFwdRows, kWaves = kGatedChunk / kRows;
     __shared__ float2 fold[kWaves][64];
@@ -257,9 +255,8 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
     __shared__ int some[KEEP ? kWaves : 1];
     const int wv = wave_id(), lane = lane_id();
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
-    uint64_t* words = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt);
-    const int job = NC > 1 ? take_ticket(static_cast<unsigned*>(a.ws)) : blockIdx.x;
-    const int k = __builtin_amdgcn_readfirstlane(job / NB), cb = job - k * NB;
+    const int cb = (blockIdx.x + blockIdx.x / NB) % NB;
+    const int k = NC > 1 ? chunk_ticket(a.ws, cb) : 0;
     keep_scalar(a.T);
     keep_scalar(a.C);
     const int row0 = k * kGatedChunk + wv * kRows;
@@ -322,32 +319,35 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
         }
     }
 
-    // most waves' rows are all in one sequence and neither begin nor end it
-    const bool plain = rows.plain();
+    // what few rows need stands in branches that the others jump over
+    const uint32_t special = rows.special();
     float av[kRows], bv[kRows];
     float A = 1.f, B = 0.f;
-    auto gates = [&](auto plain_) {
-        constexpr bool PLAIN = decltype(plain_)::value;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const float r = recurrence_gate(En::get(ga[i]));
-            const Decay d = decay_of(r, rate2);
-            av[i] = d.a;
-            bv[i] = input_term(r, d.beta2, sigmoid_f(En::get(gi[i])), En::get(x[i]));
-            if constexpr (!PLAIN) {
-                if (!(rows.used >> i & 1)) av[i] = 1.f, bv[i] = 0.f;
-                if (rows.first >> i & 1) {
-                    const float h0 = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-                    B = bv[i] = fmaf(av[i], h0, bv[i]);
-                    continue;
-                }
-            }
-            B = fmaf(av[i], B, bv[i]);
-            A *= av[i];
+    for (int i = 0; i < kRows; ++i) {
+        const float l = En::get(ga[i]);
+        float r = sigmoid_f(l), in = sigmoid_f(En::get(gi[i])), xi = En::get(x[i]);
+        const bool hold = l <= kGateHold;
+        if (__builtin_expect(__any(hold), 0)) {
+            r = hold ? 0.f : r;  // a = 1 and beta = 0
+            in = hold ? 0.f : in;
+            xi = hold ? 0.f : xi;
         }
-    };
-    if (plain) gates(std::true_type{});
-    else gates(std::false_type{});
+        const Decay d = decay_of(r, rate2);
+        av[i] = d.a;
+        bv[i] = __builtin_amdgcn_sqrtf(d.beta2) * in * xi;
+        float h = B;
+        if (__builtin_expect(special >> i & 1, 0)) {
+            if (!(rows.used >> i & 1)) av[i] = 1.f, bv[i] = 0.f;
+            if (rows.first >> i & 1) {
+                bv[i] = fmaf(av[i], a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f, bv[i]);
+                h = 0.f;
+            }
+        }
+        B = fmaf(av[i], h, bv[i]);
+        A *= av[i];
+        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
+    }
     fold[wv][lane] = make_float2(A, B);
     if (lane == 0) cuts[wv] = rows.first != 0;
     __syncthreads();
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
             At *= f.x;
             cut |= cw;
         }
-        uint64_t* mine = words + ((size_t)k * NB + cb) * 64;
+        uint64_t* mine = words_in(a.ws, NB) + ((size_t)k * NB + cb) * 64;
         const bool more = k + 1 < NC;
         if (more) put_word(mine + lane, cut ? state_word(Bt) : step_word(At, Bt));
         float h = 0.f;
@@ -391,14 +391,14 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, FWD_OCC) void k_gated_
                 if ((rows.last >> i & 1) && live && a.h_final) a.h_final[(size_t)rows.seq(i) * a.C + c] = h;
         }
     };
-    if (plain) emit(std::true_type{});
+    if (special == 0) emit(std::true_type{});
     else emit(std::false_type{});
 }
 
 // ------------------------------------------------------------------ backward
 // IN: format of x, ga, gi (IO's, or the 8-bit form).
 template <int IO, int IN>
-__global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_bwd(GatedArgs a, float* part) {
+__global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, 4) void k_gated_bwd(GatedArgs a, float* part) {
     using En = Entry<IO>;
     constexpr int kRows = kBwdRows, kWaves = kGatedChunk / kRows;
     __shared__ float fold[3][kWaves][64];
@@ -406,10 +406,8 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
     __shared__ float entry[64];
     const int wv = wave_id(), lane = lane_id();
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
-    uint64_t* words = reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt);
-    const int job = NC > 1 ? take_ticket(static_cast<unsigned*>(a.ws)) : blockIdx.x;
-    const int turn = __builtin_amdgcn_readfirstlane(job / NB), cb = job - turn * NB;
-    const int k = NC - 1 - turn;  // from the last chunk to the first
+    const int cb = (blockIdx.x + blockIdx.x / NB) % NB;
+    const int k = NC - 1 - (NC > 1 ? chunk_ticket(a.ws, cb) : 0);  // from the last chunk to the first
     keep_scalar(a.T);
     keep_scalar(a.C);
     const int row0 = k * kGatedChunk + wv * kRows;
@@ -441,26 +439,37 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
     // wave's 16 rows would not leave room for a second workgroup on the CU,
     // which is what hides this one's waits (203 us with rows halved and all
     // kept, one workgroup a CU, at B16 L2048 C1024 bf16)
-    const bool plain = rows.plain();
+    const uint32_t special = rows.special();
+
     float r[kRows], in[kRows], hb[kRows];
-    float A = 1.f, B = 0.f, G = 0.f;
+    float A = 1.f, B = 0.f, G = 0.f, Gend = 0.f;
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        r[i] = recurrence_gate(Entry<IN>::gate(gar[i], scale[1]));
+        const float l = Entry<IN>::gate(gar[i], scale[1]);
+        r[i] = sigmoid_f(l);
         in[i] = sigmoid_f(Entry<IN>::get(gir[i], scale[2]));
-        if (!(rows.used >> i & 1)) r[i] = 0.f, dyr[i] = {};
-        const Decay d = decay_of(r[i], rate2);
-        hb[i] = input_term(r[i], d.beta2, in[i], Entry<IN>::get(xr[i], scale[0]));
+        float ix = in[i] * Entry<IN>::get(xr[i], scale[0]);
+        const bool hold = l <= kGateHold;
+
+        r[i] = hold ? 0.f : r[i];
+        ix = hold ? 0.f : ix;
         float h = B;
-        if (rows.first >> i & 1) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        if (__builtin_expect(special >> i & 1, 0)) {
+            if (!(rows.used >> i & 1)) r[i] = 0.f;
+            if (rows.first >> i & 1) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        }
+        const Decay d = decay_of(r[i], rate2);
+        hb[i] = __builtin_amdgcn_sqrtf(d.beta2) * ix;
         B = fmaf(d.a, h, hb[i]);
         A *= d.a;
-        // the gradient that leaves the first row: dy of each row times the a's up to it
-        if (!(rows.last & ((1u << i) - 1))) G = fmaf(A, En::get(dyr[i]), G);
-        if ((rows.last & ((2u << i) - 1)) == 1u << i)  // the first that ends a sequence
-            G = fmaf(A, a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f, G);
-        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);  // not more rows at once than registers
+        // the gradient that leaves the first row: dy of each row times the a's up to it ...
+        G = fmaf(A, En::get(dyr[i]), G);
+        // ... as far as the first row that ends a sequence
+        if (__builtin_expect((rows.last & ((2u << i) - 1)) == 1u << i, 0))
+            Gend = fmaf(A, a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f, G);
+        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
     }
+    if (rows.last) G = Gend;
     fold[0][wv][lane] = A;
     fold[1][wv][lane] = B;
     fold[2][wv][lane] = G;
@@ -480,7 +489,7 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
             At *= fold[0][w][lane];
             cut |= cw;
         }
-        uint64_t* mine = words + ((size_t)k * NB + cb) * 64;
+        uint64_t* mine = words_in(a.ws, NB) + ((size_t)k * NB + cb) * 64;
         if (k > 0) put_word(mine + lane, cut ? state_word(Gt) : step_word(At, Gt));
         float u = 0.f;
         if (k + 1 < NC && !(rows.last >> (kRows - 1) & 1)) {
@@ -496,7 +505,7 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
         h = __builtin_amdgcn_readfirstlane(cuts[0][w]) ? fold[1][w][lane] : fmaf(fold[0][w][lane], h, fold[1][w][lane]);
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
-        if (!plain && (rows.first >> i & 1)) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        if (__builtin_expect(rows.first >> i & 1, 0)) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
         const float b = hb[i];
         hb[i] = h;
         h = fmaf(__builtin_amdgcn_exp2f(-rate2 * r[i]), h, b);
@@ -513,33 +522,32 @@ __global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, BWD_OCC) void k_gated_
     for (int n = 0; n < 3; ++n) out[n] = row_block_of<kRows>(a.d[n], a.ldd, sizeof(typename En::T), a.T, a.C, row0);
     const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
     float sum = 0.f;
-    auto emit = [&](auto plain_) {
-        constexpr bool PLAIN = decltype(plain_)::value;
 #pragma unroll
-        for (int i = kRows - 1; i >= 0; --i) {
-            if constexpr (!PLAIN)
-                if (rows.last >> i & 1) u = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-            const float g = En::get(dyr[i]) + u, x = Entry<IN>::get(xr[i], scale[0]);
+    for (int i = kRows - 1; i >= 0; --i) {
+        if (__builtin_expect(rows.last >> i & 1, 0)) u = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+        const float g = En::get(dyr[i]) + u, x = Entry<IN>::get(xr[i], scale[0]);
+        const Decay d = decay_of(r[i], rate2);
+        const float t = in[i] * __builtin_amdgcn_rsqf(d.beta2);  // i / beta
+        float dx = g * d.beta2 * t;
+        u = g * d.a;
+        float w = rate * r[i] * u * fmaf(x * d.a, t, -hb[i]);
+        float dxx = dx * x;
+        dxx = fmaf(-dxx, in[i], dxx);
+        {
             const bool hold = r[i] == 0.f;
-            const Decay d = decay_of(r[i], rate2);
-            const float t = in[i] * __builtin_amdgcn_rsqf(d.beta2);  // i / beta
-            const float dx = hold ? 0.f : g * d.beta2 * t;
-            u = g * d.a;
-            const float w = hold ? 0.f : rate * r[i] * u * fmaf(x * d.a, t, -hb[i]);
-            const float dxx = dx * x;
-            sum += w;
-            if (PLAIN || (rows.used >> i & 1)) {
-                store_entry(out[0], i, voff, En::put(dx));
-                store_entry(out[1], i, voff, En::put(fmaf(-w, r[i], w)));
-                store_entry(out[2], i, voff, En::put(hold ? 0.f : fmaf(-dxx, in[i], dxx)));
-            }
-            if constexpr (!PLAIN)
-                if ((rows.first >> i & 1) && live && a.dh0) a.dh0[(size_t)rows.seq(i) * a.C + c] = u;
-            if (i % kTogether == 0) __builtin_amdgcn_sched_barrier(0);
+            dx = hold ? 0.f : dx;
+            w = hold ? 0.f : w;
+            dxx = hold ? 0.f : dxx;
         }
-    };
-    if (plain) emit(std::true_type{});
-    else emit(std::false_type{});
+        sum += w;
+        if (rows.used >> i & 1) {
+            store_entry(out[0], i, voff, En::put(dx));
+            store_entry(out[1], i, voff, En::put(fmaf(-w, r[i], w)));
+            store_entry(out[2], i, voff, En::put(dxx));
+        }
+        if (__builtin_expect((rows.first >> i & 1) && live && a.dh0, 0)) a.dh0[(size_t)rows.seq(i) * a.C + c] = u;
+        if (i % kTogether == 0) __builtin_amdgcn_sched_barrier(0);
+    }
     if (!a.drate) return;
     __syncthreads();
     fold[0][wv][lane] = sum;
@@ -600,10 +608,12 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
     if (c >= a.C) return;
     using En = Entry<IO>;
     auto at = [&](const RowsIn& r) { return En::get(static_cast<const typename En::T*>(r.p)[(size_t)b * r.ld + c]); };
-    const float r = recurrence_gate(at(a.ga));
-    const Decay d = decay_of(r, a.rate[c] * kLog2e);
+    const float l = at(a.ga);
+    const bool hold = l <= kGateHold;
+    const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), a.rate[c] * kLog2e);
+    const float in = hold ? 0.f : __builtin_amdgcn_sqrtf(d.beta2) * sigmoid_f(at(a.gi)) * at(a.x);
     const size_t o = (size_t)slot * a.C + c;
-    const float h = fmaf(d.a, a.h_in[o], input_term(r, d.beta2, sigmoid_f(at(a.gi)), at(a.x)));
+    const float h = fmaf(d.a, a.h_in[o], in);
     a.h_out[o] = h;
     static_cast<typename En::T*>(a.y)[(size_t)b * a.C + c] = En::put(h);
 }
@@ -612,14 +622,14 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
 
 size_t gated_workspace(int T, int C, int S, bool bwd) {
     if (chunks_of(T) <= 1) return 0;
-    return kWordsAt + words_of(T, C) * 8 + (bwd ? (size_t)chunks_of(T) * C * 4 : 0);
+    return blocks_of(C) * kTicketStride + words_of(T, C) * 8 + (bwd ? (size_t)chunks_of(T) * C * 4 : 0);
 }
 
 namespace {
 void clear_words(const GatedArgs& a, hipStream_t s) {
-    const size_t n = words_of(a.T, a.C);
-    hipLaunchKernelGGL(k_gated_clear, dim3((n + 255) / 256), dim3(256), 0, s, static_cast<unsigned*>(a.ws),
-                       reinterpret_cast<uint64_t*>(static_cast<char*>(a.ws) + kWordsAt), n);
+    const int NB = blocks_of(a.C);
+    const size_t n = words_of(a.T, a.C);  // at least 128 for each counter
+    hipLaunchKernelGGL(k_gated_clear, dim3((n + 255) / 256), dim3(256), 0, s, a.ws, NB, n);
 }
 }  // namespace
 
@@ -646,7 +656,7 @@ hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) {
     float* part = nullptr;
     if (NC > 1) {
         clear_words(a, s);
-        part = reinterpret_cast<float*>(static_cast<char*>(a.ws) + kWordsAt + words_of(a.T, a.C) * 8);
+        part = reinterpret_cast<float*>(words_in(a.ws, NB) + words_of(a.T, a.C));
     }
     constexpr int kWaves = kGatedChunk / kBwdRows;
     auto* f = a.io == kRowBf16 ? (a.kept ? k_gated_bwd<kRowBf16, kRowKept> : k_gated_bwd<kRowBf16, kRowBf16>)

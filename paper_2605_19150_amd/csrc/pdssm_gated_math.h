@@ -21,12 +21,12 @@ __device__ __forceinline__ float sigmoid_f(float v) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504088896340736f));
 }
 
-// a = e^(-s) and beta^2 = 1 - a^2 of one entry.  The latter needs care near a = 1, where the
-// difference keeps only its last bits (s is rate * r, often 1e-3 and less):
-// 1 - e^(-2s) = 2 e^(-s) sinh(s), and sinh's series converges fast.  Up to s =
-// 0.5 its first omitted term is 1.1e-8 of the sum; from there on 1 - a^2 is off
-// by 2e-7 of itself.  With v = s log2 e the powers of ln 2 sit in the
-// coefficients.
+// a = e^(-s) and beta^2 = 1 - a^2 of one entry.  The latter needs care near
+// a = 1, where the difference keeps only its last bits (s is rate * r, often
+// 1e-3 and less): 1 - e^(-2s) = 2 e^(-s) sinh(s), and sinh's series converges
+// fast.  Up to s = 0.3 its first omitted term is 1.5e-7 of the sum; from there
+// on 1 - a^2 is off by 4e-7 of itself.  With v = s log2 e the powers of ln 2
+// sit in the coefficients.
 struct Decay {
     float a;
     float beta2;   // 1 - a^2, beta squared
@@ -36,22 +36,12 @@ __device__ __forceinline__ Decay decay_of(float r, float rate2) {  // rate2 = ra
     Decay d;
     const float v = rate2 * r, u = v * v;
     d.a = __builtin_amdgcn_exp2f(-v);
-    // 2 ln2 (1 + (ln2 v)^2 / 6 + (ln2 v)^4 / 120 + (ln2 v)^6 / 5040)
-    float p = fmaf(u, 3.0505468e-5f, 2.6667116e-3f);
-    p = fmaf(u, p, 0.11100822f);
-    p = fmaf(u, p, 1.3862944f);
-    d.beta2 = v < 0.72134752f ? d.a * v * p : fmaf(-d.a, d.a, 1.f);
+    // 2 ln2 (1 + (ln2 v)^2 / 6 + (ln2 v)^4 / 120)
+    const float p = fmaf(u, fmaf(u, 2.6667116e-3f, 0.11100822f), 1.3862944f);
+    d.beta2 = v < 0.43280851f ? d.a * v * p : fmaf(-d.a, d.a, 1.f);
     return d;
 }
 
-// The recurrence gate: r = sigmoid(ga), and 0 where the state is held (no other
-// logit gives it), so that there a = 1 and beta = 0.
-__device__ __forceinline__ float recurrence_gate(float ga) { return ga <= kGateHold ? 0.f : sigmoid_f(ga); }
-
-// A row's input term beta i x, and none where the state is held, whatever x and i are.
-__device__ __forceinline__ float input_term(float r, float beta2, float i, float x) {
-    return r == 0.f ? 0.f : __builtin_amdgcn_sqrtf(beta2) * i * x;
-}
 constexpr float kLog2e = 1.44269504088896340736f;
 
 }  // namespace pdssm
