@@ -529,7 +529,7 @@ int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const i
  * M = 2 H N), q [T, Dm], e [ceil(T/32), Dm] as pdssm_pack8 writes them (no code
  * -128), dW [M, Dm] fp32.  On the matrix cores with fp32 sums: both operands
  * are exact in bf16.  T >= 0; M a multiple of 8, Dm of 16; T*M and T*Dm below 2^40
- * entries; dP, q and dW 16-byte aligned.  ws:
+ * entries; dP, q, e and dW 16-byte aligned.  ws:
  * pdssm_project_wgrad_workspace_size bytes, 256-byte aligned.
  */
 size_t pdssm_project_wgrad_workspace_size(int32_t T, int32_t M, int32_t Dm);

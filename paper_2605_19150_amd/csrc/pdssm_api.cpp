@@ -1025,7 +1025,7 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
     const int st = check_wgrad(T, M, Dm);
     if (st != PDSSM_OK) return st;
     if (!dW || (T > 0 && (!dP || !q || !e))) return PDSSM_ERR_INVALID_ARG;
-    if (misaligned(dP) || misaligned(q) || misaligned(dW)) return PDSSM_ERR_INVALID_ARG;
+    if (misaligned(dP) || misaligned(q) || misaligned(e) || misaligned(dW)) return PDSSM_ERR_INVALID_ARG;
     const size_t need = pdssm::wgrad_workspace(T, M, Dm);
     if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
     if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;

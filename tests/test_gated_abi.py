@@ -181,7 +181,7 @@ def test_weight_gradient(lib):
     T, M, Dm = 5000, 16, 32
     need = size(T, M, Dm)
     good = [_at(1), _at(2), _at(3), _at(4), _at(5), 64 * MB]
-    for k, v in ((0, None), (1, None), (2, None), (3, None), (0, _at(1) + 8), (1, _at(2) + 8), (3, _at(4) + 4),
+    for k, v in ((0, None), (1, None), (2, None), (3, None), (0, _at(1) + 8), (1, _at(2) + 8), (2, _at(3) + 8), (3, _at(4) + 4),
                  (3, _at(1)), (3, _at(2) + 64), (3, _at(3))):
         args = list(good)
         args[k] = v
