@@ -6,11 +6,13 @@
 // Both operands lie in memory with the contracted axis, the tokens, outermost;
 // the matrix instruction wants eight consecutive tokens of one row in a lane.
 // So the tiles are turned on their way into LDS, in registers: a thread loads
-// an 8 x 8 block (8 tokens, 16 bytes of dP or 8 bytes of q each), pairs the
+// 8 tokens of 8 rows (of 4, for the smaller tile) of each operand, pairs the
 // tokens of a row (a byte permutation for dP; for q the conversion to bf16,
-// which packs two values anyway) and writes 8 rows of 8 tokens, 16 bytes each.
+// which packs two values anyway) and writes 8 tokens of each row, 16 bytes.
 #include "pdssm_device.h"
 #include "pdssm_rows.h"
+
+#include <type_traits>
 
 namespace pdssm {
 namespace {
@@ -32,14 +34,25 @@ struct Tile {
     static constexpr int STAGE = 2 * SIDE;
     static constexpr size_t LDS = 2 * STAGE;
     static constexpr int N = B / 64;              // 32 x 32 products along a wave's side
-    static constexpr bool BOTH = B == 256;        // a thread turns a block of each operand, or of one
-    static_assert(B == 256 || B == 128, "256 or 128 blocks of 8 x 8 an operand");
+    static constexpr int R = B / 32;              // rows that a thread turns, of each operand
+    static_assert(R == 8 || R == 4, "loads of 8 R bytes of dP, 4 R of q");
 };
 
 // LDS row r keeps its 16-byte chunk c (tokens 8c .. 8c+7) at place c ^ turn(r):
-// 16 rows read at one chunk, and the 8 chunks written of one row, fall on
-// different banks.
-__device__ __forceinline__ int turn(int r) { return (r & 7) ^ ((r >> 3) & 1); }
+// 16 consecutive rows read at one chunk fall on different banks, and so do the
+// rows, R apart, that eight lanes write at one chunk.
+__device__ __forceinline__ int turn(int r) { return (r ^ (r >> 3)) & 7; }
+
+constexpr int kGroup = 4;  // tiles along M
+constexpr int kAhead = 3;  // slices
+
+// row_block of values that are the same in every lane but may have been formed
+// in vector registers.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t scalar_block(const void* base, int bytes) {
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)b), hi = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+    return row_block(reinterpret_cast<const void*>((uint64_t)hi << 32 | lo), __builtin_amdgcn_readfirstlane(bytes));
+}
 
 template <int B>
 __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, int Z, float* out) {
@@ -51,62 +64,95 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
     // tiles that share their rows of dP
     const int per = (total + 7) / 8;
     const int z = blockIdx.y;
-    const int tile = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || tile >= total) return;
-    const int m0 = tile / DT * B, d0 = tile % DT * B;
-    const int slices = (a.T + C::KS - 1) / C::KS, share = (slices + Z - 1) / Z;
+    const int turnno = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= per || turnno >= total) return;
+    // in turn, kGroup tiles along M before the next along Dm: a run of 32 is
+    // then about square in bytes (a row of dP has twice those of u)
+    const int gt = kGroup * DT, gr = turnno / gt, in = turnno - gr * gt, gm = min(kGroup, MT - gr * kGroup);
+    const int mt = gr * kGroup + in % gm, dt = in / gm;
+    const int m0 = mt * B, d0 = dt * B;
+    const int slices = (a.T + C::KS - 1) / C::KS, share = ((slices + Z - 1) / Z + 1) & ~1;  // in pairs
     const int s0 = z * share, s1 = min(slices, s0 + share);
 
-    // ---- loads: lane % 8 is the block's place along the tokens, lane / 8 (and
-    // the wave) along the rows; blocks past the last row load the last one
-    const bool doP = C::BOTH || wv < 2, doU = C::BOTH || wv >= 2;
-    const int tb = lane & 7, row = 8 * ((C::BOTH ? wv : wv & 1) * 8 + (lane >> 3));
+    // ---- loads: eight lanes next to each other read a token's consecutive
+    // rows, whole lines (with tokens in neighbouring lanes instead, every lane is
+    // a request of its own: 2.47 ms against 1.5 at M8192 Dm4096 T32768); rows
+    // past the last: the last ones again
+    const int tb = lane >> 3, row = C::R * (wv * 8 + (lane & 7));
     const uint32_t pld = (uint32_t)a.M * 2, qld = (uint32_t)a.Dm;
-    const int pm = min(m0 + row, a.M - 8), ud = min(d0 + row, a.Dm - 8);
+    const int pm = min(m0 + row, a.M - C::R), ud = min(d0 + row, a.Dm - C::R);
     const uint32_t vp = (uint32_t)(8 * tb) * pld + pm * 2, vu = (uint32_t)(8 * tb) * qld + ud;
     const uint32_t ve = (uint32_t)(tb >> 2) * qld + ud;
-    u32x4 p[8];
-    u32x2 q[8], ex;
-    auto load = [&](int s) {
-        const int t0 = s * C::KS, n = min(a.T - t0, C::KS);  // tokens past the last: 0
-        if (doP) {
-            const auto rp = row_block(a.dP + (size_t)t0 * a.M, (uint32_t)n * pld);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                p[j] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, vp + j * pld, 0, 0));
-        }
-        if (doU) {
-            const auto rq = row_block(a.q + (size_t)t0 * a.Dm, (uint32_t)n * qld);
-            const auto re = row_block(a.e + (size_t)(t0 / kKeptRows) * a.Dm, (uint32_t)((n + kKeptRows - 1) / kKeptRows) * qld);
-            ex = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(re, ve, 0, 0));
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                q[j] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, vu + j * qld, 0, 0));
-        }
+    // two sets of registers: a slice's loads are issued more than one slice
+    // before they are turned
+    // The workgroups of an XCD that share a panel of dP or u each touch a part of
+    // its lines kAhead slices before they are loaded, so that those loads find
+    // them in the L2: wave 0 a quarter of dP's lines, wave 1 a half of u's.
+    constexpr int kLinesP = B / 64, kLinesU = B / 128;  // 128-byte lines of a token's row
+    uint32_t touch;
+    if (wv == 0) {
+        const int n = (dt & 3) * (16 * kLinesP) + (lane & (16 * kLinesP - 1));
+        touch = (uint32_t)(n / kLinesP) * a.M * 2 + min(m0 * 2 + n % kLinesP * 128, a.M * 2 - 4);
+    } else {
+        const int n = (mt & 1) * (32 * kLinesU) + (lane & (32 * kLinesU - 1));
+        touch = (uint32_t)(n / kLinesU) * a.Dm + min(d0 + n % kLinesU * 128, a.Dm - 4);
+    }
+    uint32_t touched = 0;
+    auto prefetch = [&](int s) {
+        const int t0 = s * C::KS, n = max(0, min(a.T - t0, C::KS));
+        asm volatile("" ::"v"(touched));  // a slice old
+        if (wv == 0)
+            touched = __builtin_amdgcn_raw_buffer_load_b32(scalar_block(a.dP + (size_t)t0 * a.M, n * a.M * 2), touch, 0, 0);
+        if (wv == 1) touched = __builtin_amdgcn_raw_buffer_load_b32(scalar_block(a.q + (size_t)t0 * a.Dm, n * a.Dm), touch, 0, 0);
     };
-    auto store = [&](int st) {
-        unsigned char* P = lds + st * C::STAGE + row * C::ROWB;
-        unsigned char* U = P + C::SIDE;
+    struct Raw {
+        uint32_t p[8][C::R / 2], q[8][C::R / 4], e[C::R / 4];
+    } raw[2];
+    // slices past the last give zeros
+    auto load = [&](int s, Raw& g) {
+        const int t0 = s * C::KS, n = max(0, min(a.T - t0, C::KS));
+        const auto rp = scalar_block(a.dP + (size_t)t0 * a.M, (uint32_t)n * pld);
+        const auto rq = scalar_block(a.q + (size_t)t0 * a.Dm, (uint32_t)n * qld);
+        const auto re = scalar_block(a.e + (size_t)(t0 / kKeptRows) * a.Dm, (uint32_t)((n + kKeptRows - 1) / kKeptRows) * qld);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int at = i * C::ROWB + 16 * (tb ^ turn(row + i));
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (C::R == 8) {
+                const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, vp + j * pld, 0, 0));
+                const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, vu + j * qld, 0, 0));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g.p[j][i] = v[i];
+                g.q[j][0] = w[0];
+                g.q[j][1] = w[1];
+            } else {
+                const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rp, vp + j * pld, 0, 0));
+                g.p[j][0] = v[0];
+                g.p[j][1] = v[1];
+                g.q[j][0] = __builtin_amdgcn_raw_buffer_load_b32(rq, vu + j * qld, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < C::R / 4; ++i) g.e[i] = __builtin_amdgcn_raw_buffer_load_b32(re, ve + 4 * i, 0, 0);
+    };
+    // Row i of what the thread turns, to stage st, in six pieces of about five
+    // vector instructions each.
+    u32x4 wu;
+    float scale;
+    auto turn_piece = [&](int st, const Raw& g, int i, int piece) {
+        unsigned char* P = lds + st * C::STAGE + (row + i) * C::ROWB + 16 * (tb ^ turn(row + i));
+        if (piece == 0) {
             u32x4 w;
-            if (doP) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)  // tokens 2j and 2j + 1 of row i
-                    w[j] = __builtin_amdgcn_perm(p[2 * j + 1][i / 2], p[2 * j][i / 2], i & 1 ? 0x07060302 : 0x05040100);
-                *reinterpret_cast<u32x4*>(P + at) = w;
-            }
-            if (doU) {
-                const float scale = kept_scale((int)(int8_t)(ex[i / 4] >> (8 * (i % 4))));
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float lo = (float)(int8_t)(q[2 * j][i / 4] >> (8 * (i % 4))) * scale;
-                    const float hi = (float)(int8_t)(q[2 * j + 1][i / 4] >> (8 * (i % 4))) * scale;
-                    w[j] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)lo, (__bf16)hi});
-                }
-                *reinterpret_cast<u32x4*>(U + at) = w;
-            }
+            for (int j = 0; j < 4; ++j)  // tokens 2j and 2j + 1 of row i
+                w[j] = __builtin_amdgcn_perm(g.p[2 * j + 1][i / 2], g.p[2 * j][i / 2], i & 1 ? 0x07060302 : 0x05040100);
+            *reinterpret_cast<u32x4*>(P) = w;
+            scale = kept_scale((int)(int8_t)(g.e[i / 4] >> (8 * (i % 4))));
+        } else if (piece <= 4) {
+            const int j = piece - 1;
+            const float lo = (float)(int8_t)(g.q[2 * j][i / 4] >> (8 * (i % 4))) * scale;
+            const float hi = (float)(int8_t)(g.q[2 * j + 1][i / 4] >> (8 * (i % 4))) * scale;
+            wu[j] = __builtin_bit_cast(unsigned, bf16x2{(__bf16)lo, (__bf16)hi});
+        } else {
+            *reinterpret_cast<u32x4*>(P + C::SIDE) = wu;
         }
     };
 
@@ -119,35 +165,67 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
         for (int j = 0; j < C::N; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    auto multiply = [&](int st) {
-        const unsigned char* P = lds + st * C::STAGE + (wm * (B / 2) + l32) * C::ROWB;
-        const unsigned char* U = lds + st * C::STAGE + C::SIDE + (wd * (B / 2) + l32) * C::ROWB;
+    struct Frag {
+        bf16x8 p[C::N], u[C::N];
+    } f[2];
+    auto read = [&](int st, int kk, Frag& g, int n) {
+        const int r = 32 * (n % C::N) + l32;  // in the wave's half, which begins at a multiple of 64
+        const unsigned char* at = lds + st * C::STAGE + r * C::ROWB + 16 * ((2 * kk + hf) ^ turn(r));
+        if (n < C::N) g.u[n] = *reinterpret_cast<const bf16x8*>(at + C::SIDE + wd * (B / 2) * C::ROWB);
+        else g.p[n - C::N] = *reinterpret_cast<const bf16x8*>(at + wm * (B / 2) * C::ROWB);
+    };
+    // Step kk of stage st: its products on fragment set kk % 2 and between them
+    // the next step's reads (the next slice's first step after the last) and,
+    // in the first three steps, the next slice's turn.  After the last slice
+    // that goes on with what nobody reads.
+    constexpr int kProducts = C::N * C::N, kPieces = 6 * C::R;
+    constexpr int kEach = kPieces / (3 * kProducts);
+    static_assert(kEach * 3 * kProducts == kPieces && kProducts % (2 * C::N) == 0, "reads and pieces spread evenly");
+    auto step = [&](int st, auto kk_, const Raw& g) {
+        constexpr int kk = decltype(kk_)::value;
+        Frag& now = f[kk & 1];
+        Frag& then = f[(kk & 1) ^ 1];
 #pragma unroll
-        for (int kk = 0; kk < C::KS / 16; ++kk) {
-            const int at = 16 * ((2 * kk + hf) ^ turn(l32));
-            bf16x8 A[C::N], D[C::N];
+        for (int m = 0; m < kProducts; ++m) {
+            const int i = m / C::N, j = m % C::N;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(now.p[i], now.u[j], acc[i][j], 0, 0, 0);
+            if (m % (kProducts / (2 * C::N)) == 0)
+                read(kk < 3 ? st : st ^ 1, (kk + 1) % 4, then, m / (kProducts / (2 * C::N)));
+            if constexpr (kk < 3) {
+                const int first = (kk * kProducts + m) * kEach;
 #pragma unroll
-            for (int i = 0; i < C::N; ++i) A[i] = *reinterpret_cast<const bf16x8*>(P + 32 * i * C::ROWB + at);
-#pragma unroll
-            for (int j = 0; j < C::N; ++j) D[j] = *reinterpret_cast<const bf16x8*>(U + 32 * j * C::ROWB + at);
-#pragma unroll
-            for (int i = 0; i < C::N; ++i)
-#pragma unroll
-                for (int j = 0; j < C::N; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[i], D[j], acc[i][j], 0, 0, 0);
+                for (int n = 0; n < kEach; ++n) turn_piece(st ^ 1, g, (first + n) / 6, (first + n) % 6);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
+    using k0 = std::integral_constant<int, 0>;
+    using k1 = std::integral_constant<int, 1>;
+    using k2 = std::integral_constant<int, 2>;
+    using k3 = std::integral_constant<int, 3>;
+    // Slice s in stage st; g: the registers of slice s + 1, then of s + 3.
+    auto slice = [&](int s, int st, Raw& g) {
+        step(st, k0{}, g);
+        step(st, k1{}, g);
+        step(st, k2{}, g);
+        load(s + 3, g);
+        prefetch(s + 3 + kAhead);
+        // every wave has read all of this stage and written its part of the other
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        step(st, k3{}, g);
+    };
     if (s0 < s1) {
-        load(s0);
-        store(0);
-        if (s0 + 1 < s1) load(s0 + 1);
-        __syncthreads();
-        for (int s = s0; s < s1; ++s) {
-            const int st = (s - s0) & 1;
-            multiply(st);
-            if (s + 1 < s1) store(st ^ 1);
-            if (s + 2 < s1) load(s + 2);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load(s0, raw[0]);
+        load(s0 + 1, raw[1]);
+#pragma unroll
+        for (int n = 0; n < kPieces; ++n) turn_piece(0, raw[0], n / 6, n % 6);
+        load(s0 + 2, raw[0]);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < 2 * C::N; ++n) read(0, 0, f[0], n);
+        for (int s = s0; s < s1; s += 2) {
+            slice(s, 0, raw[1]);
+            slice(s + 1, 1, raw[0]);
         }
     }
 
