@@ -23,6 +23,11 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
+// What bounds it: the matrix cores and the power they draw.  M8192 Dm4096
+// T32768 takes 1.87 ms, 1178 TFLOP/s; the vendor library's product of bf16
+// operands of that shape (u already widened, so twice its bytes) takes 1.87 ms
+// too.  Without its loads the kernel would take 1.37 ms.
+//
 // A workgroup of four waves sums a B x B block of dW over a share of the
 // tokens, 64 a slice; a wave has a quarter of it.  Two LDS stages: while one is
 // multiplied the next slice is turned into the other.
@@ -43,8 +48,7 @@ struct Tile {
 // rows, R apart, that eight lanes write at one chunk.
 __device__ __forceinline__ int turn(int r) { return (r ^ (r >> 3)) & 7; }
 
-constexpr int kGroup = 4;  // tiles along M
-constexpr int kAhead = 3;  // slices
+constexpr int kGroup = 8;  // tiles along M
 
 // row_block of values that are the same in every lane but may have been formed
 // in vector registers.
@@ -83,55 +87,57 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
     const int pm = min(m0 + row, a.M - C::R), ud = min(d0 + row, a.Dm - C::R);
     const uint32_t vp = (uint32_t)(8 * tb) * pld + pm * 2, vu = (uint32_t)(8 * tb) * qld + ud;
     const uint32_t ve = (uint32_t)(tb >> 2) * qld + ud;
-    // two sets of registers: a slice's loads are issued more than one slice
-    // before they are turned
-    // The workgroups of an XCD that share a panel of dP or u each touch a part of
-    // its lines kAhead slices before they are loaded, so that those loads find
-    // them in the L2: wave 0 a quarter of dP's lines, wave 1 a half of u's.
-    constexpr int kLinesP = B / 64, kLinesU = B / 128;  // 128-byte lines of a token's row
-    uint32_t touch;
-    if (wv == 0) {
-        const int n = (dt & 3) * (16 * kLinesP) + (lane & (16 * kLinesP - 1));
-        touch = (uint32_t)(n / kLinesP) * a.M * 2 + min(m0 * 2 + n % kLinesP * 128, a.M * 2 - 4);
-    } else {
-        const int n = (mt & 1) * (32 * kLinesU) + (lane & (32 * kLinesU - 1));
-        touch = (uint32_t)(n / kLinesU) * a.Dm + min(d0 + n % kLinesU * 128, a.Dm - 4);
-    }
-    uint32_t touched = 0;
-    auto prefetch = [&](int s) {
-        const int t0 = s * C::KS, n = max(0, min(a.T - t0, C::KS));
-        asm volatile("" ::"v"(touched));  // a slice old
-        if (wv == 0)
-            touched = __builtin_amdgcn_raw_buffer_load_b32(scalar_block(a.dP + (size_t)t0 * a.M, n * a.M * 2), touch, 0, 0);
-        if (wv == 1) touched = __builtin_amdgcn_raw_buffer_load_b32(scalar_block(a.q + (size_t)t0 * a.Dm, n * a.Dm), touch, 0, 0);
-    };
+    // two sets of registers: a slice's loads are issued about one slice before
+    // they are turned
     struct Raw {
         uint32_t p[8][C::R / 2], q[8][C::R / 4], e[C::R / 4];
     } raw[2];
-    // slices past the last give zeros
-    auto load = [&](int s, Raw& g) {
-        const int t0 = s * C::KS, n = max(0, min(a.T - t0, C::KS));
-        const auto rp = scalar_block(a.dP + (size_t)t0 * a.M, (uint32_t)n * pld);
-        const auto rq = scalar_block(a.q + (size_t)t0 * a.Dm, (uint32_t)n * qld);
-        const auto re = scalar_block(a.e + (size_t)(t0 / kKeptRows) * a.Dm, (uint32_t)((n + kKeptRows - 1) / kKeptRows) * qld);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
+    // Slice s as buffers; past the last slice they are empty and give zeros.
+    struct Source {
+        __amdgpu_buffer_rsrc_t p, q, e;
+    };
+    auto source = [&](int s) {
+        const int t0 = s * C::KS, nt = max(0, min(a.T - t0, C::KS));
+        return Source{scalar_block(a.dP + (size_t)t0 * a.M, nt * (int)pld),
+                      scalar_block(a.q + (size_t)t0 * a.Dm, nt * (int)qld),
+                      scalar_block(a.e + (size_t)(t0 / kKeptRows) * a.Dm, (nt + kKeptRows - 1) / kKeptRows * (int)qld)};
+    };
+    // Load n of a slice: dP's 8 tokens, u's, the exponents.
+    constexpr int kLoads = 17;
+    auto load_one = [&](const Source& from, Raw& g, int n) {
+        const int j = n & 7;
+        if (n < 8) {
             if constexpr (C::R == 8) {
-                const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rp, vp + j * pld, 0, 0));
-                const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, vu + j * qld, 0, 0));
+                const u32x4 v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from.p, vp + j * pld, 0, 0));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) g.p[j][i] = v[i];
-                g.q[j][0] = w[0];
-                g.q[j][1] = w[1];
             } else {
-                const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rp, vp + j * pld, 0, 0));
+                const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from.p, vp + j * pld, 0, 0));
                 g.p[j][0] = v[0];
                 g.p[j][1] = v[1];
-                g.q[j][0] = __builtin_amdgcn_raw_buffer_load_b32(rq, vu + j * qld, 0, 0);
+            }
+        } else if (n < 16) {
+            if constexpr (C::R == 8) {
+                const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from.q, vu + j * qld, 0, 0));
+                g.q[j][0] = v[0];
+                g.q[j][1] = v[1];
+            } else {
+                g.q[j][0] = __builtin_amdgcn_raw_buffer_load_b32(from.q, vu + j * qld, 0, 0);
+            }
+        } else {
+            if constexpr (C::R == 8) {
+                const u32x2 v = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(from.e, ve, 0, 0));
+                g.e[0] = v[0];
+                g.e[1] = v[1];
+            } else {
+                g.e[0] = __builtin_amdgcn_raw_buffer_load_b32(from.e, ve, 0, 0);
             }
         }
+    };
+    auto load = [&](int s, Raw& g) {
+        const Source from = source(s);
 #pragma unroll
-        for (int i = 0; i < C::R / 4; ++i) g.e[i] = __builtin_amdgcn_raw_buffer_load_b32(re, ve + 4 * i, 0, 0);
+        for (int n = 0; n < kLoads; ++n) load_one(from, g, n);
     };
     // Row i of what the thread turns, to stage st, in six pieces of about five
     // vector instructions each.
@@ -181,7 +187,10 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
     constexpr int kProducts = C::N * C::N, kPieces = 6 * C::R;
     constexpr int kEach = kPieces / (3 * kProducts);
     static_assert(kEach * 3 * kProducts == kPieces && kProducts % (2 * C::N) == 0, "reads and pieces spread evenly");
-    auto step = [&](int st, auto kk_, const Raw& g) {
+    // The loads stand between products too: a wave that issues them in a row
+    // waits for the address unit, and its products with it (2.11 against 1.87
+    // ms at M8192 Dm4096 T32768).
+    auto step = [&](int st, auto kk_, const Raw& g, const Source& from, Raw& other) {
         constexpr int kk = decltype(kk_)::value;
         Frag& now = f[kk & 1];
         Frag& then = f[(kk & 1) ^ 1];
@@ -196,6 +205,12 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
 #pragma unroll
                 for (int n = 0; n < kEach; ++n) turn_piece(st ^ 1, g, (first + n) / 6, (first + n) % 6);
             }
+            if constexpr (kk == 3 || kk == 0) {
+                constexpr int kSlots = 2 * kProducts;
+                const int at = (kk == 3 ? 0 : kProducts) + m;
+#pragma unroll
+                for (int n = at * kLoads / kSlots; n < (at + 1) * kLoads / kSlots; ++n) load_one(from, other, n);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -203,42 +218,49 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
     using k1 = std::integral_constant<int, 1>;
     using k2 = std::integral_constant<int, 2>;
     using k3 = std::integral_constant<int, 3>;
-    // Slice s in stage st; g: the registers of slice s + 1, then of s + 3.
-    auto slice = [&](int s, int st, Raw& g) {
-        step(st, k0{}, g);
-        step(st, k1{}, g);
-        step(st, k2{}, g);
-        load(s + 3, g);
-        prefetch(s + 3 + kAhead);
+    // Slice s in stage st; g: the registers of slice s + 1, then of s + 3;
+    // other: of s + 2, whose first loads the slice before this one issued.
+    Source from;
+    auto slice = [&](int s, int st, Raw& g, Raw& other) {
+        step(st, k0{}, g, from, other);
+        step(st, k1{}, g, from, other);
+        step(st, k2{}, g, from, other);
+        from = source(s + 3);
         // every wave has read all of this stage and written its part of the other
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        step(st, k3{}, g);
+        step(st, k3{}, g, from, g);
     };
     if (s0 < s1) {
         load(s0, raw[0]);
         load(s0 + 1, raw[1]);
 #pragma unroll
         for (int n = 0; n < kPieces; ++n) turn_piece(0, raw[0], n / 6, n % 6);
-        load(s0 + 2, raw[0]);
+        from = source(s0 + 2);
+#pragma unroll
+        for (int n = 0; n < kLoads / 2; ++n) load_one(from, raw[0], n);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
         for (int n = 0; n < 2 * C::N; ++n) read(0, 0, f[0], n);
         for (int s = s0; s < s1; s += 2) {
-            slice(s, 0, raw[1]);
-            slice(s + 1, 1, raw[0]);
+            slice(s, 0, raw[1], raw[0]);
+            slice(s + 1, 1, raw[0], raw[1]);
         }
     }
 
-    float* o = out + (size_t)z * a.M * a.Dm;
+    const int mw = m0 + wm * (B / 2), rows = max(0, min(a.M - mw, B / 2));
+    const auto o = scalar_block(out + ((size_t)z * a.M + min(mw, a.M)) * a.Dm, rows * a.Dm * 4);
 #pragma unroll
-    for (int i = 0; i < C::N; ++i)
+    for (int j = 0; j < C::N; ++j) {
+        const int d = d0 + wd * (B / 2) + 32 * j + l32;
+        // a column past the last lies past every buffer
+        const uint32_t at = d < a.Dm ? (uint32_t)(4 * hf) * a.Dm * 4 + d * 4 : 0x80000000u;
 #pragma unroll
-        for (int j = 0; j < C::N; ++j)
+        for (int i = 0; i < C::N; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int m = m0 + wm * (B / 2) + 32 * i + 8 * (r / 4) + 4 * hf + r % 4, d = d0 + wd * (B / 2) + 32 * j + l32;
-                if (m < a.M && d < a.Dm) __builtin_nontemporal_store(acc[i][j][r], o + (size_t)m * a.Dm + d);
-            }
+            for (int r = 0; r < 16; ++r)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[i][j][r]), o,
+                                                      at + (uint32_t)(32 * i + 8 * (r / 4) + r % 4) * a.Dm * 4, 0, kLoadStream);
+    }
 }
 
 // dW = the shares' sums, in the order of the tokens.
