@@ -455,12 +455,12 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
 
 typedef struct pdssm_rows {
     const void* p;   /* entry (t, c) at p + t*ld + c */
-    int64_t ld;      /* entries from one row to the next, >= C */
+    int64_t ld;      /* entries from one row to the next, C <= ld <= 2^24 */
     const int8_t* e; /* the 8-bit form: exponents [ceil(T/32), C] (p: int8); else NULL */
 } pdssm_rows;
 
 typedef struct pdssm_gated_desc {
-    int32_t T, C, S; /* rows, channels, sequences; T >= 0, C >= 1, S >= 1 */
+    int32_t T, C, S; /* rows, channels, sequences; 0 <= T <= 2^30, 1 <= C <= 2^24, S >= 1 */
     uint32_t flags;  /* 0 or PDSSM_FLAG_BF16_IO */
 } pdssm_gated_desc;
 
@@ -528,8 +528,8 @@ int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const i
  * dP [T, M] bf16 (the bf16 pairs dD, db, dc of pdssm_scan_bwd are such rows,
  * M = 2 H N), q [T, Dm], e [ceil(T/32), Dm] as pdssm_pack8 writes them (no code
  * -128), dW [M, Dm] fp32.  On the matrix cores with fp32 sums: both operands
- * are exact in bf16.  T >= 0; M a multiple of 8, Dm of 16; T*M and T*Dm below 2^40
- * entries; dP, q, e and dW 16-byte aligned.  ws:
+ * are exact in bf16.  0 <= T <= 2^30; M a multiple of 8, Dm of 16, both at most
+ * 2^20; T*M and T*Dm below 2^40, M*Dm below 2^31 entries; dP, q, e and dW 16-byte aligned.  ws:
  * pdssm_project_wgrad_workspace_size bytes, 256-byte aligned.
  */
 size_t pdssm_project_wgrad_workspace_size(int32_t T, int32_t M, int32_t Dm);

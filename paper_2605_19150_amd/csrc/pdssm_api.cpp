@@ -377,11 +377,14 @@ bool misaligned4(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) % 
 static_assert(PDSSM_GATED_CHUNK == pdssm::kGatedChunk && PDSSM_KEPT_ROWS == pdssm::kKeptRows, "header constants");
 
 // ------------------------------------------------------------------ gated recurrence
+constexpr int64_t kMaxLd = 1 << 24;  // entries from row to row
+
 int check_gated(const pdssm_gated_desc* d) {
     if (!d || (d->flags & ~PDSSM_FLAG_BF16_IO) != 0) return PDSSM_ERR_INVALID_ARG;
     if (d->T < 0 || d->C < 1 || d->S < 1) return PDSSM_ERR_INVALID_ARG;
-    // row offsets are 64-bit; grids and per-chunk buffers stay below 2^31 entries
-    if ((long long)((d->T + 31LL) / 32) * ((d->C + 63) / 64) >= (1LL << 31) ||
+    // row offsets are 64-bit; offsets within a wave's 16 rows, row numbers, grids
+    // and per-chunk buffers stay below 2^31
+    if (d->T > (1 << 30) || d->C > kMaxLd || (long long)((d->T + 31LL) / 32) * ((d->C + 63) / 64) >= (1LL << 31) ||
         (long long)d->S * ((d->C + 63) / 64) >= (1LL << 31))
         return PDSSM_ERR_UNSUPPORTED;
     return PDSSM_OK;
@@ -393,7 +396,7 @@ bool misaligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>
 
 // Rows of w-byte entries that the kernels may read: not NULL unless there are none.
 bool bad_rows(const pdssm_rows* r, int T, int C, size_t w) {
-    if (!r || r->ld < C || r->ld > (1LL << 40)) return true;
+    if (!r || r->ld < C || r->ld > kMaxLd) return true;
     return T > 0 && (!r->p || misaligned_to(r->p, w));
 }
 
@@ -880,7 +883,7 @@ int pdssm_gated_bwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_
     for (const pdssm_rows* r : {x, ga, gi})
         if (bad_rows(r, T, C, wi) || (r->e != nullptr) != kept) return PDSSM_ERR_INVALID_ARG;
     if (bad_rows(dy, T, C, w) || dy->e || !rate || bad_sequences(d, cu) || (T > 0 && !saved) || !dd || ldd < C ||
-        ldd > (1LL << 40))
+        ldd > kMaxLd)
         return PDSSM_ERR_INVALID_ARG;
     for (int i = 0; i < 3; ++i)
         if (T > 0 && (!dd[i] || misaligned_to(dd[i], w))) return PDSSM_ERR_INVALID_ARG;
@@ -1010,7 +1013,7 @@ int check_wgrad(int32_t T, int32_t M, int32_t Dm) {
     if (T < 0 || M < 1 || Dm < 1) return PDSSM_ERR_INVALID_ARG;
     if (M % 8 != 0 || Dm % 16 != 0) return PDSSM_ERR_UNSUPPORTED;
     if ((long long)T * M >= (1LL << 40) || (long long)T * Dm >= (1LL << 40) || (long long)M * Dm >= (1LL << 31) ||
-        M > (1 << 20) || Dm > (1 << 20))
+        M > (1 << 20) || Dm > (1 << 20) || T > (1 << 30))
         return PDSSM_ERR_UNSUPPORTED;
     return PDSSM_OK;
 }

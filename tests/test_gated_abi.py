@@ -66,6 +66,9 @@ class Call:
     (lambda c: setattr(c.d, "C", 0), ERR_INVALID_ARG),
     (lambda c: setattr(c.d, "S", 0), ERR_INVALID_ARG),
     (lambda c: (setattr(c.d, "C", 1 << 30), setattr(c.d, "T", 1 << 30)), ERR_UNSUPPORTED),
+    (lambda c: setattr(c.d, "T", (1 << 30) + 1), ERR_UNSUPPORTED),
+    (lambda c: (setattr(c.d, "C", (1 << 24) + 1), setattr(c.d, "T", 1)), ERR_UNSUPPORTED),
+    (lambda c: setattr(c.x, "ld", (1 << 24) + 1), ERR_INVALID_ARG),
     (lambda c: setattr(c.x, "p", None), ERR_INVALID_ARG),
     (lambda c: setattr(c.ga, "ld", 64), ERR_INVALID_ARG),
     (lambda c: setattr(c.gi, "p", _at(3) + 2), ERR_INVALID_ARG),
@@ -175,7 +178,8 @@ def test_weight_gradient(lib):
     bad = ctypes.c_size_t(-1).value
     for T, M, Dm, code in ((-1, 16, 16, ERR_INVALID_ARG), (4, 0, 16, ERR_INVALID_ARG), (4, 16, 0, ERR_INVALID_ARG),
                            (4, 12, 16, ERR_UNSUPPORTED), (4, 16, 24, ERR_UNSUPPORTED), (4, 1 << 16, 1 << 16, ERR_UNSUPPORTED),
-                           ((1 << 31) - 1, 1 << 10, 16, ERR_UNSUPPORTED)):
+                           ((1 << 31) - 1, 1 << 10, 16, ERR_UNSUPPORTED), ((1 << 30) + 1, 16, 16, ERR_UNSUPPORTED),
+                           (4, 1 << 21, 16, ERR_UNSUPPORTED)):
         assert size(T, M, Dm) == bad
         assert lib.pdssm_project_wgrad(T, M, Dm, _at(1), _at(2), _at(3), _at(4), _at(5), 64 * MB, None) == code
     T, M, Dm = 5000, 16, 32
