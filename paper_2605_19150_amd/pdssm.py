@@ -26,6 +26,7 @@ Gated recurrent layers (gated_fwd and the functions after it) take rows:
   [T,C] and [ceil(T/32),C].
 """
 import ctypes
+import functools
 import math
 import os
 
@@ -116,7 +117,7 @@ def load():
     L.pdssm_project.argtypes = [I32] * 5 + [P] * 10 + [P]
     L.pdssm_project.restype = I
     U32, I64, V3 = ctypes.c_uint32, ctypes.c_int64, ctypes.POINTER(ctypes.c_void_p)
-    G, R = ctypes.POINTER(GatedDesc), ctypes.POINTER(Rows)
+    G, R = P, P  # GatedDesc and Rows, by address
     L.pdssm_gated_workspace_size.argtypes, L.pdssm_gated_workspace_size.restype = [G, I], Z
     L.pdssm_gated_fwd.argtypes = [G, R, R, R] + [P] * 6 + [V3, V3, P, Z, P, P]
     L.pdssm_gated_fwd.restype = I
@@ -639,85 +640,103 @@ def _ceil(n, k):
     return -(-n // k)
 
 
-class _On:
-    """The device and stream that a call on tensors of device dev runs on.  A
-    stream of the caller's own that is not the current one learns of every
-    tensor of the call (seen()), so that none is given to other work before it
-    has run."""
-
-    def __init__(self, dev, stream):
-        self.guard = torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else None
-        cur = torch.cuda.current_stream(dev)
-        self.stream = cur if stream is None else stream
-        self.other = self.stream if self.stream.cuda_stream != cur.cuda_stream else None
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-    def seen(self, *tensors):
-        if self.other is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.other)
-
-    def ptr(self):
-        return ctypes.c_void_p(self.stream.cuda_stream)
+def _on_its_device(f):
+    """f with the device of its first tensor as the current one, which is where
+    its kernels are launched."""
+    @functools.wraps(f)
+    def on(first, *args, **kw):
+        t = first[0] if isinstance(first, (tuple, list)) and first else first
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
+            with torch.cuda.device(t.device):
+                return f(first, *args, **kw)
+        return f(first, *args, **kw)
+    return on
 
 
-def _row_layout(t, name, dtype, shape, dev):
-    """(pointer, entries from row to row) of rows [T,C] or [B,L,C] that may be a part of wider rows."""
+# the current stream of a device as a number; torch.cuda.current_stream builds
+# an object for it, a fifth of a short call's time
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _on(stream, dev, tensors, status=None):
+    """The stream to launch on, as a number.  One of the caller's own that is not
+    the current one learns of every tensor of the call, so that none is given
+    to other work before it has run."""
+    current = _raw_stream(dev.index)
+    if stream is None or stream.cuda_stream == current:
+        return current
+    if status is not None:
+        stream.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _tensor(t, name, dtype, shape, dev):
+    """_need, quick where nothing is wrong; the address."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_cuda and t.device == dev and
+            t.is_contiguous()):
+        _need(t, name, dtype, shape, dev)
+    return t.data_ptr()
+
+
+def _rows(t, name, dtype, shape, dev):
+    """(address, entries from row to row, no exponents) of rows [T,C] or [B,L,C]
+    that may be a part of wider rows."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.device != dev or dev.type != "cuda":
+    if not t.is_cuda or t.device != dev:
         raise ValueError("%s must be on %s" % (name, dev))
-    C = shape[-1]
-    if t.stride(-1) != 1 and C > 1:
+    C, step = shape[-1], t.stride()
+    if step[-1] != 1 and C > 1:
         raise ValueError("%s: the entries of a row must be next to each other" % name)
     ld = C
     if len(shape) == 3:
         B, L = shape[0], shape[1]
         if L > 1:
-            ld = t.stride(1)
-            if B > 1 and t.stride(0) != L * ld:
+            ld = step[1]
+            if B > 1 and step[0] != L * ld:
                 raise ValueError("%s: rows must be evenly spaced over the batch" % name)
         elif B > 1:
-            ld = t.stride(0)
+            ld = step[0]
     elif shape[0] > 1:
-        ld = t.stride(0)
+        ld = step[0]
     if ld < C:
         raise ValueError("%s: rows must not overlap" % name)
-    return t.data_ptr(), ld
-
-
-def _rows(t, name, dtype, shape, dev):
-    p, ld = _row_layout(t, name, dtype, shape, dev)
-    return Rows(p, ld, None)
+    return t.data_ptr(), ld, None
 
 
 def _kept(pair, name, T, C, dev):
-    """A pair (q, e) in the 8-bit form."""
+    """(address, entries from row to row, address of the exponents) of a pair (q, e) in the 8-bit form."""
     q, e = pair
-    _need(q, name + " codes", torch.int8, (T, C), dev)
-    _need(e, name + " exponents", torch.int8, (_ceil(T, KEPT_ROWS), C), dev)
-    return Rows(q.data_ptr(), C, e.data_ptr())
+    return (_tensor(q, name + " codes", torch.int8, (T, C), dev), C,
+            _tensor(e, name + " exponents", torch.int8, (_ceil(T, KEPT_ROWS), C), dev))
+
+
+class _Args:
+    """A descriptor and up to four row tensors in memory that the library reads during the call."""
+
+    def __init__(self, T, C, S, flags, *rows):
+        self.d = GatedDesc(T, C, S, flags)
+        self.rows = (Rows * len(rows))(*rows)
+        self.at = [ctypes.addressof(self.d)]
+        base = ctypes.addressof(self.rows)
+        self.at += [base + i * ctypes.sizeof(Rows) for i in range(len(rows))]
 
 
 def _row_type(t):
     if not isinstance(t, torch.Tensor):
         raise TypeError("rows must be a torch.Tensor")
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise TypeError("rows must be float32 or bfloat16, got %s" % t.dtype)
-    return FLAG_BF16_IO if t.dtype == torch.bfloat16 else 0
+    if t.dtype is torch.bfloat16:
+        return FLAG_BF16_IO
+    if t.dtype is torch.float32:
+        return 0
+    raise TypeError("rows must be float32 or bfloat16, got %s" % t.dtype)
 
 
 def _sequences(t, cu):
@@ -734,28 +753,33 @@ def _sequences(t, cu):
         if not isinstance(cu, torch.Tensor) or cu.dim() != 1 or cu.shape[0] < 2:
             raise ValueError("cu must be [S+1] with S >= 1")
         S = cu.shape[0] - 1
-        _need(cu, "cu", torch.int32, (S + 1,), t.device)
+        _tensor(cu, "cu", torch.int32, (S + 1,), t.device)
     if C < 1 or S < 1:
         raise ValueError("rows need at least one channel and one sequence")
     return T, C, S
 
 
-def _gated_ws(d, op, dev):
-    n = load().pdssm_gated_workspace_size(ctypes.byref(d), op)
+def _gated_ws(args, op, dev):
+    n = load().pdssm_gated_workspace_size(args.at[0], op)
     if n == OP_SIZE_ERROR:
         raise PdssmError(ERR_UNSUPPORTED, "gated_workspace_size")
     return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
 
 
 def _state(t, name, S, C, dev):
-    if t is not None:
-        _need(t, name, torch.float32, (S, C), dev)
+    return None if t is None else _tensor(t, name, torch.float32, (S, C), dev)
 
 
-def _checked(status, what, dev):
-    """Synchronise and raise if a kernel reported a bad index."""
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _done(st, status, what):
+    """Raise on a refusal; with a status tensor, synchronise and raise if a kernel reported a bad index."""
+    if st != OK:
+        raise PdssmError(st, what)
     if status is not None:
-        torch.cuda.synchronize(dev)
+        torch.cuda.synchronize()
         st = int(status.item())
         if st != OK:
             raise PdssmError(st, what)
@@ -765,6 +789,11 @@ def _three(tensors):
     return (ctypes.c_void_p * 3)(*[t.data_ptr() for t in tensors])
 
 
+def _status(check, dev):
+    return torch.zeros(1, dtype=torch.int32, device=dev) if check else None
+
+
+@_on_its_device
 def gated_fwd(x, ga, gi, rate, cu=None, h0=None, hold8=False, check=True, stream=None):
     """The gated recurrence h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(gi_t) x_t
     with a_t = exp(-rate * sigmoid(ga_t)), over every sequence from its state
@@ -774,34 +803,29 @@ def gated_fwd(x, ga, gi, rate, cu=None, h0=None, hold8=False, check=True, stream
     takes in their place.  check=False neither synchronises nor reports a bad cu."""
     flags = _row_type(x)
     T, C, S = _sequences(x, cu)
-    dev = x.device
-    r = [_rows(t, n, x.dtype, x.shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
-    _need(rate, "rate", torch.float32, (C,), dev)
-    _state(h0, "h0", S, C, dev)
-    d = GatedDesc(T, C, S, flags)
-    with _On(dev, stream) as on:
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        h_final = torch.empty((S, C), dtype=torch.float32, device=dev)
-        saved = torch.empty((_ceil(T, GATED_CHUNK), C), dtype=torch.float32, device=dev)
-        kept = q = e = None
-        if hold8:
-            kept = tuple((torch.empty((T, C), dtype=torch.int8, device=dev),
-                          torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)) for _ in range(3))
-            q, e = _three([k[0] for k in kept]), _three([k[1] for k in kept])
-        ws = _gated_ws(d, OP_FWD, dev)
-        status = torch.zeros(1, dtype=torch.int32, device=dev) if check else None
-        if check and on.other is not None:
-            on.other.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
-        on.seen(x, ga, gi, rate, cu, h0, y, h_final, saved, ws, status, *([t for k in kept for t in k] if hold8 else []))
-        st = load().pdssm_gated_fwd(ctypes.byref(d), ctypes.byref(r[0]), ctypes.byref(r[1]), ctypes.byref(r[2]),
-                                    _p(rate), _p(cu), _p(h0), _p(y), _p(h_final), _p(saved), q, e, _p(ws),
-                                    ws.numel() if ws is not None else 0, _p(status), on.ptr())
-        if st != OK:
-            raise PdssmError(st, "pdssm_gated_fwd")
-        _checked(status, "pdssm_gated_fwd", dev)
+    dev, shape = x.device, x.shape
+    args = _Args(T, C, S, flags, *[_rows(t, n, x.dtype, shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))])
+    rate_at = _tensor(rate, "rate", torch.float32, (C,), dev)
+    h0_at = _state(h0, "h0", S, C, dev)
+    y = torch.empty(shape, dtype=x.dtype, device=dev)
+    h_final = torch.empty((S, C), dtype=torch.float32, device=dev)
+    saved = torch.empty((_ceil(T, GATED_CHUNK), C), dtype=torch.float32, device=dev)
+    kept = q = e = None
+    if hold8:
+        kept = tuple((torch.empty((T, C), dtype=torch.int8, device=dev),
+                      torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)) for _ in range(3))
+        q, e = _three([k[0] for k in kept]), _three([k[1] for k in kept])
+    ws = _gated_ws(args, OP_FWD, dev)
+    status = _status(check, dev)
+    s = _on(stream, dev, (x, ga, gi, rate, cu, h0, y, h_final, saved, ws, status,
+                          *([t for k in kept for t in k] if hold8 else ())), status)
+    st = load().pdssm_gated_fwd(*args.at, rate_at, _at(cu), h0_at, y.data_ptr(), h_final.data_ptr(), saved.data_ptr(), q, e,
+                                _at(ws), ws.numel() if ws is not None else 0, _at(status), s)
+    _done(st, status, "pdssm_gated_fwd")
     return (y, h_final, saved, kept) if hold8 else (y, h_final, saved)
 
 
+@_on_its_device
 def gated_bwd(x, ga, gi, rate, saved, dy, cu=None, h0=None, dh_final=None, check=True, stream=None):
     """Gradients of gated_fwd: (dx, dga, dgi, drate [C], dh0 [S,C]) from dy (rows
     as y) and dh_final [S,C] (default 0); saved, cu and h0 as in the forward.  x, ga, gi are the
@@ -810,39 +834,31 @@ def gated_bwd(x, ga, gi, rate, saved, dy, cu=None, h0=None, dh_final=None, check
     tensor [..., 3C], the gradient of a projection that makes the three."""
     flags = _row_type(dy)
     T, C, S = _sequences(dy, cu)
-    dev = dy.device
+    dev, shape = dy.device, dy.shape
     ins = ((x, "x"), (ga, "ga"), (gi, "gi"))
     eight = isinstance(x, (tuple, list))
     if any(isinstance(t, (tuple, list)) != eight for t, _ in ins):
         raise TypeError("x, ga and gi must be all rows or all pairs (q, e)")
-    r = [_kept(t, n, T, C, dev) if eight else _rows(t, n, dy.dtype, dy.shape, dev) for t, n in ins]
-    rdy = _rows(dy, "dy", dy.dtype, dy.shape, dev)
-    _need(rate, "rate", torch.float32, (C,), dev)
-    _need(saved, "saved", torch.float32, (_ceil(T, GATED_CHUNK), C), dev)
-    _state(h0, "h0", S, C, dev)
-    _state(dh_final, "dh_final", S, C, dev)
-    d = GatedDesc(T, C, S, flags)
-    with _On(dev, stream) as on:
-        rows = torch.empty((*dy.shape[:-1], 3 * C), dtype=dy.dtype, device=dev)
-        grads = rows.split(C, -1)
-        drate = torch.empty(C, dtype=torch.float32, device=dev)
-        dh0 = torch.empty((S, C), dtype=torch.float32, device=dev)
-        ws = _gated_ws(d, OP_BWD, dev)
-        status = torch.zeros(1, dtype=torch.int32, device=dev) if check else None
-        if check and on.other is not None:
-            on.other.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
-        on.seen(*([t for k in (x, ga, gi) for t in k] if eight else (x, ga, gi)), rate, saved, dy, cu, h0, dh_final,
-                rows, drate, dh0, ws, status)
-        st = load().pdssm_gated_bwd(ctypes.byref(d), ctypes.byref(r[0]), ctypes.byref(r[1]), ctypes.byref(r[2]),
-                                    _p(rate), _p(cu), _p(h0), _p(saved), ctypes.byref(rdy), _p(dh_final),
-                                    _three(grads), 3 * C, _p(drate), _p(dh0), _p(ws),
-                                    ws.numel() if ws is not None else 0, _p(status), on.ptr())
-        if st != OK:
-            raise PdssmError(st, "pdssm_gated_bwd")
-        _checked(status, "pdssm_gated_bwd", dev)
+    r = [_kept(t, n, T, C, dev) if eight else _rows(t, n, dy.dtype, shape, dev) for t, n in ins]
+    args = _Args(T, C, S, flags, *r, _rows(dy, "dy", dy.dtype, shape, dev))
+    rate_at = _tensor(rate, "rate", torch.float32, (C,), dev)
+    saved_at = _tensor(saved, "saved", torch.float32, (_ceil(T, GATED_CHUNK), C), dev)
+    h0_at, dhf_at = _state(h0, "h0", S, C, dev), _state(dh_final, "dh_final", S, C, dev)
+    rows = torch.empty((*shape[:-1], 3 * C), dtype=dy.dtype, device=dev)
+    grads = rows.split(C, -1)
+    drate = torch.empty(C, dtype=torch.float32, device=dev)
+    dh0 = torch.empty((S, C), dtype=torch.float32, device=dev)
+    ws = _gated_ws(args, OP_BWD, dev)
+    status = _status(check, dev)
+    s = _on(stream, dev, (*([t for k in (x, ga, gi) for t in k] if eight else (x, ga, gi)), rate, saved, dy, cu, h0,
+                          dh_final, rows, drate, dh0, ws, status), status)
+    st = load().pdssm_gated_bwd(*args.at[:4], rate_at, _at(cu), h0_at, saved_at, args.at[4], dhf_at, _three(grads), 3 * C,
+                                drate.data_ptr(), dh0.data_ptr(), _at(ws), ws.numel() if ws is not None else 0, _at(status), s)
+    _done(st, status, "pdssm_gated_bwd")
     return (*grads, drate, dh0)
 
 
+@_on_its_device
 def gated_step(x, ga, gi, rate, h, slots=None, out=None, y=None, check=True, stream=None):
     """One token of the gated recurrence for each row of x, ga, gi [B,C]: returns
     (h_new [S,C], y [B,C]).  h [S,C] holds the states; row b advances state
@@ -851,57 +867,49 @@ def gated_step(x, ga, gi, rate, h, slots=None, out=None, y=None, check=True, str
     y, and states that no row advances, are not written.  out [S,C] takes the new
     states; default: in place."""
     flags = _row_type(x)
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("x must be [B,C]")
-    B, C = x.shape
+    B, C = shape
     dev = x.device
-    r = [_rows(t, n, x.dtype, (B, C), dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
-    _need(rate, "rate", torch.float32, (C,), dev)
     if not isinstance(h, torch.Tensor) or h.dim() != 2:
         raise ValueError("h must be [S,C]")
     S = h.shape[0]
-    _need(h, "h", torch.float32, (S, C), dev)
-    out = h if out is None else out
-    _need(out, "out", torch.float32, (S, C), dev)
-    if slots is not None:
-        _need(slots, "slots", torch.int32, (B,), dev)
-    d = GatedDesc(B, C, S, flags)
-    with _On(dev, stream) as on:
-        if y is None:
-            y = torch.empty((B, C), dtype=x.dtype, device=dev)
-        _need(y, "y", x.dtype, (B, C), dev)
-        status = torch.zeros(1, dtype=torch.int32, device=dev) if check else None
-        if check and on.other is not None:
-            on.other.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
-        on.seen(x, ga, gi, rate, h, out, slots, y, status)
-        st = load().pdssm_gated_step(ctypes.byref(d), ctypes.byref(r[0]), ctypes.byref(r[1]), ctypes.byref(r[2]),
-                                     _p(rate), _p(slots), _p(h), _p(out), _p(y), _p(status), on.ptr())
-        if st != OK:
-            raise PdssmError(st, "pdssm_gated_step")
-        _checked(status, "pdssm_gated_step", dev)
-    return out, y
+    args = _Args(B, C, S, flags, _rows(x, "x", x.dtype, shape, dev), _rows(ga, "ga", x.dtype, shape, dev),
+                 _rows(gi, "gi", x.dtype, shape, dev))
+    rate_at = _tensor(rate, "rate", torch.float32, (C,), dev)
+    h_at = _tensor(h, "h", torch.float32, (S, C), dev)
+    out_at = h_at if out is None else _tensor(out, "out", torch.float32, (S, C), dev)
+    slots_at = None if slots is None else _tensor(slots, "slots", torch.int32, (B,), dev)
+    y_at = None if y is None else _tensor(y, "y", x.dtype, shape, dev)
+    if y is None:
+        y = torch.empty(shape, dtype=x.dtype, device=dev)
+        y_at = y.data_ptr()
+    status = _status(check, dev)
+    s = _on(stream, dev, (x, ga, gi, rate, h, out, slots, y, status), status)
+    st = load().pdssm_gated_step(*args.at, rate_at, slots_at, h_at, out_at, y_at, _at(status), s)
+    _done(st, status, "pdssm_gated_step")
+    return h if out is None else out, y
 
 
+@_on_its_device
 def pack8(u, stream=None):
     """(q, e): rows u [T,C] or [B,L,C] in the 8-bit form, q [T,C] and
     e [ceil(T/32),C] int8 with T = B*L; the value of q[t,c] is q[t,c] * 2^e[t//32,c]."""
     flags = _row_type(u)
     if u.dim() not in (2, 3):
         raise ValueError("u must be [T,C] or [B,L,C]")
-    C = u.shape[-1]
+    C, dev = u.shape[-1], u.device
     T = u.shape[0] if u.dim() == 2 else u.shape[0] * u.shape[1]
-    dev = u.device
-    r = _rows(u, "u", u.dtype, u.shape, dev)
-    with _On(dev, stream) as on:
-        q = torch.empty((T, C), dtype=torch.int8, device=dev)
-        e = torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)
-        on.seen(u, q, e)
-        st = load().pdssm_pack8(T, C, flags, ctypes.byref(r), _p(q), _p(e), on.ptr())
-        if st != OK:
-            raise PdssmError(st, "pdssm_pack8")
+    args = _Args(T, C, 1, flags, _rows(u, "u", u.dtype, u.shape, dev))
+    q = torch.empty((T, C), dtype=torch.int8, device=dev)
+    e = torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)
+    s = _on(stream, dev, (u, q, e))
+    _done(load().pdssm_pack8(T, C, flags, args.at[1], q.data_ptr(), e.data_ptr(), s), None, "pdssm_pack8")
     return q, e
 
 
+@_on_its_device
 def unpack8(pair, dtype=torch.float32, stream=None):
     """The values [T,C] that a pair (q, e) of the 8-bit form stands for, exact in float32 and bfloat16."""
     q, e = pair
@@ -911,16 +919,15 @@ def unpack8(pair, dtype=torch.float32, stream=None):
         raise ValueError("q must be [T,C]")
     T, C = q.shape
     dev = q.device
-    _kept(pair, "u", T, C, dev)
-    with _On(dev, stream) as on:
-        out = torch.empty((T, C), dtype=dtype, device=dev)
-        on.seen(q, e, out)
-        st = load().pdssm_unpack8(T, C, FLAG_BF16_IO if dtype == torch.bfloat16 else 0, _p(q), _p(e), _p(out), on.ptr())
-        if st != OK:
-            raise PdssmError(st, "pdssm_unpack8")
+    q_at, _, e_at = _kept(pair, "u", T, C, dev)
+    out = torch.empty((T, C), dtype=dtype, device=dev)
+    s = _on(stream, dev, (q, e, out))
+    _done(load().pdssm_unpack8(T, C, FLAG_BF16_IO if dtype is torch.bfloat16 else 0, q_at, e_at, out.data_ptr(), s), None,
+          "pdssm_unpack8")
     return out
 
 
+@_on_its_device
 def project_wgrad(dP, u8, stream=None):
     """dW [M,Dm] float32 = dP^T u, the weight gradient of a projection P = u W^T:
     dP bfloat16 with B*L rows of M entries in all (the bf16 pairs that
@@ -931,22 +938,20 @@ def project_wgrad(dP, u8, stream=None):
         raise ValueError("u8 must be a pair (q, e) with q [T,Dm]")
     T, Dm = q.shape
     dev = q.device
-    _kept(u8, "u", T, Dm, dev)
+    q_at, _, e_at = _kept(u8, "u", T, Dm, dev)
     if not isinstance(dP, torch.Tensor) or dP.dim() < 2:
         raise ValueError("dP must be rows [T,M] or [B,L,...]")
-    _need(dP, "dP", torch.bfloat16, dP.shape, dev)
-    lead = 1 if dP.dim() == 2 else 2  # axes that count rows
-    if math.prod(dP.shape[:lead]) != T:
+    shape = dP.shape
+    dP_at = _tensor(dP, "dP", torch.bfloat16, shape, dev)
+    lead = 1 if len(shape) == 2 else 2  # axes that count rows
+    if math.prod(shape[:lead]) != T:
         raise ValueError("dP and u8 disagree on the number of rows")
-    M = math.prod(dP.shape[lead:])
-    with _On(dev, stream) as on:
-        dW = torch.empty((M, Dm), dtype=torch.float32, device=dev)
-        n = load().pdssm_project_wgrad_workspace_size(T, M, Dm)
-        if n == OP_SIZE_ERROR:
-            raise PdssmError(ERR_UNSUPPORTED, "project_wgrad_workspace_size")
-        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
-        on.seen(dP, q, e, dW, ws)
-        st = load().pdssm_project_wgrad(T, M, Dm, _p(dP), _p(q), _p(e), _p(dW), _p(ws), n, on.ptr())
-        if st != OK:
-            raise PdssmError(st, "pdssm_project_wgrad")
+    M = math.prod(shape[lead:])
+    n = load().pdssm_project_wgrad_workspace_size(T, M, Dm)
+    if n == OP_SIZE_ERROR:
+        raise PdssmError(ERR_UNSUPPORTED, "project_wgrad_workspace_size")
+    dW = torch.empty((M, Dm), dtype=torch.float32, device=dev)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    s = _on(stream, dev, (dP, q, e, dW, ws))
+    _done(load().pdssm_project_wgrad(T, M, Dm, dP_at, q_at, e_at, dW.data_ptr(), _at(ws), n, s), None, "pdssm_project_wgrad")
     return dW
