@@ -35,9 +35,24 @@
 namespace pdssm {
 namespace {
 
-// Rows of a wave in each direction, and how many of them the compiler may work
-// on at once (more would cost registers, and with them a workgroup of the CU).
-constexpr int kFwdRows = 16, kBwdRows = 16, kTogether = 4;
+constexpr int kWaves = 8, kWaveRows = kGatedChunk / kWaves;  // of a workgroup; 64 channels wide
+// Rows the compiler may work on at once: more would cost registers, and with
+// them a workgroup of the CU.
+constexpr int kTogether = 4;
+static_assert(kKeptRows == 2 * kWaveRows, "two waves share an exponent");
+
+// How a wave's lanes lie on its 16 rows of 64 channels: V channels next to each
+// other in a lane, V groups of lanes one below the other.  The backward pass
+// takes two where the rows are bf16 and of even width and alignment: half as
+// many accesses, each of them 4 bytes a lane.  With fp32 a lane's one entry
+// has those 4 bytes already, and two cost registers that then spill (184 ->
+// 226 us at B16 L2048 C1024, bf16 134 -> 128 us).  The forward pass has one:
+// two leave room for 6 waves instead of 8 (60 -> 66 us there).
+template <int V>
+struct Shape {
+    static constexpr int ROWS = kWaveRows / V, LANES = 64 / V;
+    static constexpr int TOGETHER = kTogether / V;
+};
 
 // ------------------------------------------------------------------ workspace
 // A ticket counter for every 64 channels, kTicketStride bytes apart, then a
@@ -140,25 +155,57 @@ __device__ __forceinline__ int sequence_of(const GatedArgs& a, int t) {
 struct RowKinds {
     uint32_t used, first, last;
     int id;  // lane i + 1: sequence of row i
-    uint32_t all;
-    // rows that begin or end a sequence or are in none; most waves have no such row
-    __device__ __forceinline__ uint32_t special() const { return (all & ~used) | first | last; }
-    __device__ __forceinline__ int seq(int i) const { return readlane_i(id, i + 1); }
 };
+constexpr uint32_t kAllRows = (1u << kWaveRows) - 1;
 
-template <int ROWS>
 __device__ __forceinline__ RowKinds row_kinds(const GatedArgs& a, int row0) {
     RowKinds k;
-    constexpr uint32_t kAll = (1u << ROWS) - 1;
     const int lane = lane_id();
-    k.id = lane < ROWS + 2 ? sequence_of(a, row0 - 1 + lane) : -1;
+    k.id = lane < kWaveRows + 2 ? sequence_of(a, row0 - 1 + lane) : -1;
     const int before = __shfl_up(k.id, 1), after = __shfl_down(k.id, 1);
-    k.all = kAll;
-    k.used = (uint32_t)(__ballot(k.id >= 0) >> 1) & kAll;
-    k.first = (uint32_t)(__ballot(k.id >= 0 && k.id != before) >> 1) & kAll;
-    k.last = (uint32_t)(__ballot(k.id >= 0 && k.id != after) >> 1) & kAll;
+    k.used = (uint32_t)(__ballot(k.id >= 0) >> 1) & kAllRows;
+    k.first = (uint32_t)(__ballot(k.id >= 0 && k.id != before) >> 1) & kAllRows;
+    k.last = (uint32_t)(__ballot(k.id >= 0 && k.id != after) >> 1) & kAllRows;
     return k;
 }
+
+// A lane's part of them.  The masks with _any are those of all groups of lanes
+// laid over each other, the same in every lane: what few rows need stands in
+// branches on them that the other rows jump over.
+template <int V>
+struct LaneRows {
+    static constexpr int ROWS = Shape<V>::ROWS;
+    static constexpr uint32_t kAll = (1u << ROWS) - 1;
+    uint32_t used, first, last, unused_any, first_any, last_any;
+    int id, g;
+    __device__ __forceinline__ LaneRows(const RowKinds& k, int g_) : id(k.id), g(g_) {
+        used = k.used >> (g * ROWS) & kAll;
+        first = k.first >> (g * ROWS) & kAll;
+        last = k.last >> (g * ROWS) & kAll;
+        unused_any = first_any = last_any = 0;
+#pragma unroll
+        for (int n = 0; n < V; ++n) {
+            unused_any |= ~k.used >> (n * ROWS) & kAll;
+            first_any |= k.first >> (n * ROWS) & kAll;
+            last_any |= k.last >> (n * ROWS) & kAll;
+        }
+    }
+    // bit i of a lane's mask, formed where it is asked for (see rare)
+    static __device__ __forceinline__ bool is(uint32_t mask, int i) {
+        asm volatile("" : "+v"(mask));
+        return mask >> i & 1;
+    }
+    // s[sequence of row i][c] where wanted (0 without s), else what it was
+    __device__ __forceinline__ float state(const float* s, int i, int C, int c, bool wanted, float else_) const {
+        const int q = V == 1 ? readlane_i(id, i + 1) : __shfl(id, g * ROWS + i + 1);
+        if (wanted) else_ = s ? s[(size_t)max(q, 0) * C + c] : 0.f;
+        return else_;
+    }
+    __device__ __forceinline__ float* place(float* s, int i, int C, int c) const {
+        const int q = V == 1 ? readlane_i(id, i + 1) : __shfl(id, g * ROWS + i + 1);
+        return s + (size_t)max(q, 0) * C + c;
+    }
+};
 
 // cu is in order and in range, or the call is reported; out[s] = in[s] (0 if
 // in is null) for the sequences without rows.  By one wave for 64 channels.
@@ -180,8 +227,8 @@ __device__ void empty_sequences(const GatedArgs& a, const float* in, float* out,
 
 // ------------------------------------------------------------------ rows
 // A wave's rows as a buffer: reads behind the last row give 0, stores there
-// are dropped, and so are those of lanes past the last channel, whose offset
-// lies past every buffer.
+// are dropped, and so are those of lanes past the last channel and of rows in no
+// sequence, whose offset lies past every buffer.
 struct RowBlock {
     __amdgpu_buffer_rsrc_t r;
     uint32_t ld;    // bytes from row to row
@@ -190,10 +237,9 @@ struct RowBlock {
 };
 constexpr uint32_t kPast = 0x80000000u;  // 16 rows of at most 2^26 bytes and an entry end below it
 
-template <int ROWS>
 __device__ __forceinline__ RowBlock row_block_of(const void* p, int64_t ld, int size, int T, int C, int row0) {
     RowBlock b;
-    const int n = min(T - row0, ROWS);
+    const int n = min(T - row0, kWaveRows);
     b.ld = (uint32_t)ld * size;
     b.last = n > 0 ? (uint32_t)(n - 1) * b.ld : 0;
     b.r = row_block(static_cast<const char*>(p) + (n > 0 ? (int64_t)row0 * ld * size : 0),
@@ -201,29 +247,94 @@ __device__ __forceinline__ RowBlock row_block_of(const void* p, int64_t ld, int 
     return b;
 }
 
-template <class T>
-__device__ __forceinline__ T load_entry(const RowBlock& b, int i, uint32_t voff) {
-    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(b.r, voff, b.at(i), 0));
-    else if constexpr (sizeof(T) == 2) return (T)__builtin_amdgcn_raw_buffer_load_b16(b.r, voff, b.at(i), 0);
-    else return (T)__builtin_amdgcn_raw_buffer_load_b8(b.r, voff, b.at(i), 0);
-}
-// Nobody reads the outputs here again: stored past the caches (nontemporal),
-// 147 -> 138 us for the backward at B16 L2048 C1024 bf16.
-template <class T>
-__device__ __forceinline__ void store_entry(const RowBlock& b, int i, uint32_t voff, T v) {
-    if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), b.r, voff, b.at(i), kLoadStream);
-    else if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, b.r, voff, b.at(i), kLoadStream);
-    else __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, b.r, voff, b.at(i), kLoadStream);
+// V neighbouring entries of a row in a register, and row i of a lane's group in
+// memory.  Nobody reads the outputs here again: they are stored past the caches
+// (nontemporal), 147 -> 138 us for the backward at B16 L2048 C1024 bf16.
+template <int IO, int V>
+struct Some;
+template <>
+struct Some<kRowF32, 1> {
+    using R = float;
+    static constexpr int SIZE = 4;
+    static __device__ __forceinline__ R load(const RowBlock& b, int i, uint32_t voff) {
+        return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b.r, voff, b.at(i), 0));
+    }
+    static __device__ __forceinline__ float get(R v, int, float = 1.f) { return v; }
+    static __device__ __forceinline__ void store(const RowBlock& b, int i, uint32_t voff, float v) {
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), b.r, voff, b.at(i), kLoadStream);
+    }
+};
+template <>
+struct Some<kRowBf16, 1> {
+    using R = uint32_t;
+    static constexpr int SIZE = 2;
+    static __device__ __forceinline__ R load(const RowBlock& b, int i, uint32_t voff) {
+        return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, voff, b.at(i), 0);
+    }
+    static __device__ __forceinline__ float get(R v, int, float = 1.f) { return __uint_as_float(v << 16); }
+    static __device__ __forceinline__ void store(const RowBlock& b, int i, uint32_t voff, float v) {
+        __builtin_amdgcn_raw_buffer_store_b16(Entry<kRowBf16>::put(v), b.r, voff, b.at(i), kLoadStream);
+    }
+};
+template <>
+struct Some<kRowBf16, 2> {
+    using R = uint32_t;
+    static constexpr int SIZE = 2;
+    static __device__ __forceinline__ R load(const RowBlock& b, int i, uint32_t voff) {
+        return __builtin_amdgcn_raw_buffer_load_b32(b.r, voff, b.at(i), 0);
+    }
+    static __device__ __forceinline__ float get(R v, int n, float = 1.f) {
+        return __uint_as_float(n ? v & 0xffff0000u : v << 16);
+    }
+    static __device__ __forceinline__ void store(const RowBlock& b, int i, uint32_t voff, const float (&v)[2]) {
+        __builtin_amdgcn_raw_buffer_store_b32(f2_to_bf2(make_float2(v[0], v[1])), b.r, voff, b.at(i), kLoadStream);
+    }
+};
+template <>
+struct Some<kRowKept, 1> {
+    using R = int;
+    static constexpr int SIZE = 1;
+    static __device__ __forceinline__ R load(const RowBlock& b, int i, uint32_t voff) {
+        return (int8_t)__builtin_amdgcn_raw_buffer_load_b8(b.r, voff, b.at(i), 0);
+    }
+    static __device__ __forceinline__ int code(R v, int) { return v; }
+    static __device__ __forceinline__ float get(R v, int, float scale) { return (float)v * scale; }
+    static __device__ __forceinline__ void store(const RowBlock& b, int i, uint32_t voff, int v) {
+        __builtin_amdgcn_raw_buffer_store_b8((uint8_t)v, b.r, voff, b.at(i), kLoadStream);
+    }
+};
+template <>
+struct Some<kRowKept, 2> {
+    using R = uint32_t;
+    static constexpr int SIZE = 1;
+    static __device__ __forceinline__ R load(const RowBlock& b, int i, uint32_t voff) {
+        return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(b.r, voff, b.at(i), 0);
+    }
+    static __device__ __forceinline__ int code(R v, int n) { return (int8_t)(v >> (8 * n)); }
+    static __device__ __forceinline__ float get(R v, int n, float scale) { return (float)code(v, n) * scale; }
+};
+
+// A gate logit; in the 8-bit form with the code of a held one.
+template <int IO, int V>
+__device__ __forceinline__ float logit(typename Some<IO, V>::R v, int n, float scale) {
+    if constexpr (IO == kRowKept)
+        if (Some<IO, V>::code(v, n) == kKeptLow) return -INFINITY;
+    return Some<IO, V>::get(v, n, scale);
 }
 
-// This lane's entries of the wave's rows (rows behind the last: 0).
-template <int IO, int ROWS>
-__device__ __forceinline__ void load_rows(typename Entry<IO>::R (&v)[ROWS], const RowsIn& r, int T, int C, int row0, int c) {
-    using E = typename Entry<IO>::T;
-    const RowBlock b = row_block_of<ROWS>(r.p, r.ld, sizeof(E), T, C, row0);
+// This lane's entries of the wave's rows, group g, channels c ...
+template <int IO, int V>
+__device__ __forceinline__ void load_rows(typename Some<IO, V>::R (&v)[Shape<V>::ROWS], const RowsIn& r, int T, int C, int row0,
+                                          int g, int c) {
+    using S = Some<IO, V>;
+    const RowBlock b = row_block_of(r.p, r.ld, S::SIZE, T, C, row0);
+    const uint32_t voff = (uint32_t)(g * Shape<V>::ROWS) * b.ld + (uint32_t)c * S::SIZE;
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) v[i] = load_entry<E>(b, i, (uint32_t)c * sizeof(E));
+    for (int i = 0; i < Shape<V>::ROWS; ++i) v[i] = S::load(b, i, voff);
 }
+
+// The same entry of the other group of lanes.
+__device__ __forceinline__ float other_group(float v) { return __shfl_xor(v, 32); }
 
 // A barrier for LDS alone: __syncthreads would also wait for the stores of rows.
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -238,6 +349,16 @@ __device__ __forceinline__ int chunk_ticket(void* ws, int cb) {
     return __builtin_amdgcn_readfirstlane(mine);
 }
 
+// Whether row i is one of mask, the same in every lane; for what few rows need.
+// Tested where it is used: the compiler would form the tests of all rows at
+// once and keep them, in more scalar registers than there are (forward that
+// keeps its rows, C1024 T32768 fp32, with the backward: 310 -> 293 us).
+__device__ __forceinline__ bool rare(uint32_t mask, int i) {
+    mask = __builtin_amdgcn_readfirstlane(mask);
+    asm volatile("" : "+s"(mask));
+    return __builtin_expect(mask >> i & 1, 0);
+}
+
 // A kernel argument that stays in a scalar register from here on: past the
 // one-lane branch of the ticket the compiler has carried such values in vector
 // registers, and then loops over the lanes for every buffer access.
@@ -245,88 +366,80 @@ __device__ __forceinline__ void keep_scalar(int& v) { asm volatile("" : "+s"(v))
 
 // ------------------------------------------------------------------ forward
 template <int IO, bool KEEP>
-__global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, 6) void k_gated_fwd(GatedArgs a) {
-    using En = Entry<IO>;
-    constexpr int kRows = kFwdRows, kWaves = kGatedChunk / kRows;
-    __shared__ float2 fold[kWaves][64];
-    __shared__ int cuts[kWaves];
+__global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
+    using S = Some<IO, 1>;
+    constexpr int ROWS = kWaveRows;
+    __shared__ float fold[2][kWaves][64];  // a wave's step: A, B
     __shared__ float entry[64];
     __shared__ uint32_t tops[KEEP ? 3 : 1][kWaves][64];
-    __shared__ int some[KEEP ? kWaves : 1];
+    __shared__ int cuts[kWaves], some[kWaves];
     const int wv = wave_id(), lane = lane_id();
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
     const int cb = (blockIdx.x + blockIdx.x / NB) % NB;
     const int k = NC > 1 ? chunk_ticket(a.ws, cb) : 0;
     keep_scalar(a.T);
     keep_scalar(a.C);
-    const int row0 = k * kGatedChunk + wv * kRows;
+    const int row0 = k * kGatedChunk + wv * kWaveRows;
     const int c = cb * 64 + lane;
     const bool live = c < a.C;
     const int cc = live ? c : a.C - 1;
 
-    typename En::R x[kRows], ga[kRows], gi[kRows];
-    load_rows<IO>(ga, a.ga, a.T, a.C, row0, cc);
-    load_rows<IO>(gi, a.gi, a.T, a.C, row0, cc);
-    load_rows<IO>(x, a.x, a.T, a.C, row0, cc);
+    typename S::R x[ROWS], ga[ROWS], gi[ROWS];
+    load_rows<IO, 1>(ga, a.ga, a.T, a.C, row0, 0, cc);
+    load_rows<IO, 1>(gi, a.gi, a.T, a.C, row0, 0, cc);
+    load_rows<IO, 1>(x, a.x, a.T, a.C, row0, 0, cc);
     const float rate2 = a.rate[cc] * kLog2e;
-    const RowKinds rows = row_kinds<kRows>(a, row0);
+    const RowKinds kinds = row_kinds(a, row0);
+    const LaneRows<1> rows(kinds, 0);
     if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.h0, a.h_final, c, cb == 0);
 
     if constexpr (KEEP) {
         // the 8-bit form of the rows in sequences; held rows keep only that
         uint32_t top[3] = {0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (!(rows.used >> i & 1)) continue;
-            const float l = En::get(ga[i]);
-            const bool hold = l <= kGateHold;
-            const float v[3] = {En::get(x[i]), l, En::get(gi[i])};
+        for (int i = 0; i < ROWS; ++i) {
+            const float l = S::get(ga[i], 0);
+            bool skip = l <= kGateHold;
+            if (rare(rows.unused_any, i)) skip |= !rows.is(rows.used, i);
+            const float v[3] = {S::get(x[i], 0), l, S::get(gi[i], 0)};
 #pragma unroll
-            for (int n = 0; n < 3; ++n) top[n] = max(top[n], hold ? 0u : __float_as_uint(v[n]) & 0x7fffffffu);
+            for (int m = 0; m < 3; ++m) top[m] = max(top[m], skip ? 0u : __float_as_uint(v[m]) & 0x7fffffffu);
         }
 #pragma unroll
-        for (int n = 0; n < 3; ++n) tops[n][wv][lane] = top[n];
-        if (lane == 0) some[wv] = rows.used != 0;
+        for (int m = 0; m < 3; ++m) tops[m][wv][lane] = top[m];
+        if (lane == 0) some[wv] = kinds.used != 0;
         __syncthreads();
         float inv[3], lim[3];
+        const bool any = __builtin_amdgcn_readfirstlane(some[wv & ~1] | some[wv | 1]);
 #pragma unroll
-        for (int n = 0; n < 3; ++n) {
-            constexpr int kShare = kKeptRows / kRows;  // waves of a block
-            uint32_t all = 0;
-            bool any = false;
-#pragma unroll
-            for (int w = 0; w < kShare; ++w) {
-                all = max(all, tops[n][(wv & -kShare) + w][lane]);
-                any |= __builtin_amdgcn_readfirstlane(some[(wv & -kShare) + w]);
-            }
-            const int e = kept_exponent(all);
-            inv[n] = kept_inverse(e);
-            lim[n] = kept_limit(e);
-            if (wv % kShare == 0 && any && live) a.e[n][(size_t)(row0 / kKeptRows) * a.C + c] = (int8_t)e;
+        for (int m = 0; m < 3; ++m) {
+            const int e = kept_exponent(max(top[m], tops[m][wv ^ 1][lane]));
+            inv[m] = kept_inverse(e);
+            lim[m] = kept_limit(e);
+            if (!(wv & 1) && any && live) a.e[m][(size_t)(row0 / kKeptRows) * a.C + c] = (int8_t)e;
         }
-        const RowBlock q0 = row_block_of<kRows>(a.q[0], a.C, 1, a.T, a.C, row0);
-        const RowBlock q1 = row_block_of<kRows>(a.q[1], a.C, 1, a.T, a.C, row0);
-        const RowBlock q2 = row_block_of<kRows>(a.q[2], a.C, 1, a.T, a.C, row0);
+        RowBlock q[3];
+#pragma unroll
+        for (int m = 0; m < 3; ++m) q[m] = row_block_of(a.q[m], a.C, 1, a.T, a.C, row0);
         const uint32_t voff = live ? (uint32_t)c : kPast;
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (!(rows.used >> i & 1)) continue;
-            const float l = En::get(ga[i]);
+        for (int i = 0; i < ROWS; ++i) {
+            uint32_t to = voff;
+            if (rare(rows.unused_any, i)) to = rows.is(rows.used, i) ? voff : kPast;
+            const float l = S::get(ga[i], 0);
             const bool hold = l <= kGateHold;
-            store_entry(q0, i, voff, (int8_t)(hold ? 0 : kept_code(En::get(x[i]), inv[0], lim[0])));
-            store_entry(q1, i, voff, (int8_t)(hold ? kKeptLow : kept_code(l, inv[1], lim[1])));
-            store_entry(q2, i, voff, (int8_t)(hold ? 0 : kept_code(En::get(gi[i]), inv[2], lim[2])));
+            Some<kRowKept, 1>::store(q[0], i, to, hold ? 0 : kept_code(S::get(x[i], 0), inv[0], lim[0]));
+            Some<kRowKept, 1>::store(q[1], i, to, hold ? kKeptLow : kept_code(l, inv[1], lim[1]));
+            Some<kRowKept, 1>::store(q[2], i, to, hold ? 0 : kept_code(S::get(gi[i], 0), inv[2], lim[2]));
         }
     }
 
-    // what few rows need stands in branches that the others jump over
-    const uint32_t special = rows.special();
-    float av[kRows], bv[kRows];
-    float A = 1.f, B = 0.f;
+    const uint32_t special = rows.unused_any | rows.first_any | rows.last_any;
+    float av[ROWS], bv[ROWS], A = 1.f, B = 0.f;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const float l = En::get(ga[i]);
-        float r = sigmoid_f(l), in = sigmoid_f(En::get(gi[i])), xi = En::get(x[i]);
+    for (int i = 0; i < ROWS; ++i) {
+        const float l = S::get(ga[i], 0);
+        float r = sigmoid_f(l), in = sigmoid_f(S::get(gi[i], 0)), xi = S::get(x[i], 0);
         const bool hold = l <= kGateHold;
         if (__builtin_expect(__any(hold), 0)) {
             r = hold ? 0.f : r;  // a = 1 and beta = 0
@@ -337,227 +450,291 @@ __global__ __launch_bounds__(kGatedChunk / kFwdRows * 64, 6) void k_gated_fwd(Ga
         av[i] = d.a;
         bv[i] = __builtin_amdgcn_sqrtf(d.beta2) * in * xi;
         float h = B;
-        if (__builtin_expect(special >> i & 1, 0)) {
-            if (!(rows.used >> i & 1)) av[i] = 1.f, bv[i] = 0.f;
-            if (rows.first >> i & 1) {
-                bv[i] = fmaf(av[i], a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f, bv[i]);
-                h = 0.f;
-            }
+        if (rare(special, i)) {
+            if (!rows.is(rows.used, i)) av[i] = 1.f, bv[i] = 0.f;
+            const bool first = rows.is(rows.first, i);
+            bv[i] = fmaf(av[i], rows.state(a.h0, i, a.C, cc, first, 0.f), bv[i]);
+            h = first ? 0.f : h;
         }
         B = fmaf(av[i], h, bv[i]);
         A *= av[i];
         if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
     }
-    fold[wv][lane] = make_float2(A, B);
-    if (lane == 0) cuts[wv] = rows.first != 0;
+    fold[0][wv][lane] = A;
+    fold[1][wv][lane] = B;
+    if (lane == 0) cuts[wv] = kinds.first != 0;
     __syncthreads();
+    const uint32_t cut_waves = (uint32_t)__ballot(lane < kWaves && cuts[lane & (kWaves - 1)]);
     if (wv == 0) {
         float At = 1.f, Bt = 0.f;
-        bool cut = k == 0;  // nothing from the left reaches the last row
-#pragma unroll 4
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float2 f = fold[w][lane];
-            const bool cw = __builtin_amdgcn_readfirstlane(cuts[w]);
-            Bt = cw ? f.y : fmaf(f.x, Bt, f.y);
-            At *= f.x;
-            cut |= cw;
+            Bt = cut_waves >> w & 1 ? fold[1][w][lane] : fmaf(fold[0][w][lane], Bt, fold[1][w][lane]);
+            At *= fold[0][w][lane];
         }
+        const bool cut = k == 0 || cut_waves;  // nothing from the left reaches the last row
         uint64_t* mine = words_in(a.ws, NB) + ((size_t)k * NB + cb) * 64;
         const bool more = k + 1 < NC;
         if (more) put_word(mine + lane, cut ? state_word(Bt) : step_word(At, Bt));
         float h = 0.f;
-        if (k > 0 && !(rows.first & 1)) {
+        if (k > 0 && !(kinds.first & 1)) {
             h = chunk_entry(mine - (size_t)NB * 64, -(ptrdiff_t)NB * 64, k, a.status);
             if (more && !cut) put_word(mine + lane, state_word(fmaf(At, h, Bt)));
         }
         entry[lane] = h;
-        if (a.saved && live && (rows.used & 1)) a.saved[(size_t)k * a.C + c] = h;
+        if (a.saved && live && (kinds.used & 1)) a.saved[(size_t)k * a.C + c] = h;
     }
     __syncthreads();
     float h = entry[lane];
-    for (int w = 0; w < wv; ++w) {
-        const float2 f = fold[w][lane];
-        h = __builtin_amdgcn_readfirstlane(cuts[w]) ? f.y : fmaf(f.x, h, f.y);
-    }
-    const RowBlock y = row_block_of<kRows>(a.y, a.C, sizeof(typename En::T), a.T, a.C, row0);
-    const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
-    auto emit = [&](auto plain_) {
-        constexpr bool PLAIN = decltype(plain_)::value;
+#pragma unroll 4
+    for (int w = 0; w < wv; ++w)
+        h = cut_waves >> w & 1 ? fold[1][w][lane] : fmaf(fold[0][w][lane], h, fold[1][w][lane]);
+    const RowBlock y = row_block_of(a.y, a.C, S::SIZE, a.T, a.C, row0);
+    const uint32_t voff = live ? (uint32_t)c * S::SIZE : kPast;
+    if (special == 0) {
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            h = !PLAIN && (rows.first >> i & 1) ? bv[i] : fmaf(av[i], h, bv[i]);
-            if (PLAIN || (rows.used >> i & 1)) store_entry(y, i, voff, En::put(h));
-            if constexpr (!PLAIN)
-                if ((rows.last >> i & 1) && live && a.h_final) a.h_final[(size_t)rows.seq(i) * a.C + c] = h;
+        for (int i = 0; i < ROWS; ++i) {
+            h = fmaf(av[i], h, bv[i]);
+            S::store(y, i, voff, h);
         }
-    };
-    if (special == 0) emit(std::true_type{});
-    else emit(std::false_type{});
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        h = rows.is(rows.first, i) ? bv[i] : fmaf(av[i], h, bv[i]);
+        S::store(y, i, rows.is(rows.used, i) ? voff : kPast, h);
+        float* f = rows.place(a.h_final, i, a.C, cc);
+        if (rows.is(rows.last, i) && live && a.h_final) *f = h;
+    }
 }
 
 // ------------------------------------------------------------------ backward
 // IN: format of x, ga, gi (IO's, or the 8-bit form).
-template <int IO, int IN>
-__global__ __launch_bounds__(kGatedChunk / kBwdRows * 64, 4) void k_gated_bwd(GatedArgs a, float* part) {
-    using En = Entry<IO>;
-    constexpr int kRows = kBwdRows, kWaves = kGatedChunk / kRows;
-    __shared__ float fold[3][kWaves][64];
+template <int IO, int IN, int V>
+__global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float* part) {
+    using S = Some<IO, V>;
+    using N = Some<IN, V>;
+    constexpr int ROWS = Shape<V>::ROWS;
+    __shared__ __align__(8) float fold[3][kWaves][64];  // a wave's steps: A, B from the left, G from the right
+    __shared__ __align__(8) float entry[64];
+    __shared__ float sums[kWaves * V][64];
     __shared__ int cuts[2][kWaves];
-    __shared__ float entry[64];
     const int wv = wave_id(), lane = lane_id();
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
     const int cb = (blockIdx.x + blockIdx.x / NB) % NB;
     const int k = NC - 1 - (NC > 1 ? chunk_ticket(a.ws, cb) : 0);  // from the last chunk to the first
     keep_scalar(a.T);
     keep_scalar(a.C);
-    const int row0 = k * kGatedChunk + wv * kRows;
-    const int c = cb * 64 + lane;
+    const int row0 = k * kGatedChunk + wv * kWaveRows;
+    const int g = V == 1 ? 0 : lane / Shape<V>::LANES, lc = lane % Shape<V>::LANES * V;
+    const int c = cb * 64 + lc;
     const bool live = c < a.C;
-    const int cc = live ? c : a.C - 1;
+    const int cc = live ? c : a.C - V;
 
-    typename Entry<IN>::R xr[kRows], gar[kRows], gir[kRows];
-    typename En::R dyr[kRows];
-    load_rows<IN>(gar, a.ga, a.T, a.C, row0, cc);
-    load_rows<IN>(gir, a.gi, a.T, a.C, row0, cc);
-    load_rows<IN>(xr, a.x, a.T, a.C, row0, cc);
-    load_rows<IO>(dyr, a.dy, a.T, a.C, row0, cc);
-    float scale[3] = {1.f, 1.f, 1.f};
-    if constexpr (IN == kRowKept) {
-        const size_t o = (size_t)(min(row0, a.T - 1) / kKeptRows) * a.C + cc;
-        scale[0] = kept_scale(a.x.e[o]);
-        scale[1] = kept_scale(a.ga.e[o]);
-        scale[2] = kept_scale(a.gi.e[o]);
-    }
-    const float rate = a.rate[cc], rate2 = rate * kLog2e;
-    const float before_chunk = a.saved[(size_t)k * a.C + cc];
-    const RowKinds rows = row_kinds<kRows>(a, row0);
-    if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.dhf, a.dh0, c, cb == 0);
-
-    // gates, and the wave's two folds: states from the left, gradients from the
-    // right.  hb: the row's input term, later the state before it.  a and beta
-    // are computed anew from r wherever they are needed: with them kept, a
-    // wave's 16 rows would not leave room for a second workgroup on the CU,
-    // which is what hides this one's waits (203 us with rows halved and all
-    // kept, one workgroup a CU, at B16 L2048 C1024 bf16)
-    const uint32_t special = rows.special();
-
-    float r[kRows], in[kRows], hb[kRows];
-    float A = 1.f, B = 0.f, G = 0.f, Gend = 0.f;
+    typename N::R xr[ROWS], gar[ROWS], gir[ROWS];
+    typename S::R dyr[ROWS];
+    load_rows<IN, V>(gar, a.ga, a.T, a.C, row0, g, cc);
+    load_rows<IN, V>(gir, a.gi, a.T, a.C, row0, g, cc);
+    load_rows<IN, V>(xr, a.x, a.T, a.C, row0, g, cc);
+    load_rows<IO, V>(dyr, a.dy, a.T, a.C, row0, g, cc);
+    float scale[3][V], rate[V], rate2[V], h[V];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const float l = Entry<IN>::gate(gar[i], scale[1]);
-        r[i] = sigmoid_f(l);
-        in[i] = sigmoid_f(Entry<IN>::get(gir[i], scale[2]));
-        float ix = in[i] * Entry<IN>::get(xr[i], scale[0]);
-        const bool hold = l <= kGateHold;
-
-        r[i] = hold ? 0.f : r[i];
-        ix = hold ? 0.f : ix;
-        float h = B;
-        if (__builtin_expect(special >> i & 1, 0)) {
-            if (!(rows.used >> i & 1)) r[i] = 0.f;
-            if (rows.first >> i & 1) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
+    for (int n = 0; n < V; ++n) {
+        scale[0][n] = scale[1][n] = scale[2][n] = 1.f;
+        if constexpr (IN == kRowKept) {
+            const size_t o = (size_t)(min(row0, a.T - 1) / kKeptRows) * a.C + cc + n;
+            scale[0][n] = kept_scale(a.x.e[o]);
+            scale[1][n] = kept_scale(a.ga.e[o]);
+            scale[2][n] = kept_scale(a.gi.e[o]);
         }
-        const Decay d = decay_of(r[i], rate2);
-        hb[i] = __builtin_amdgcn_sqrtf(d.beta2) * ix;
-        B = fmaf(d.a, h, hb[i]);
-        A *= d.a;
-        // the gradient that leaves the first row: dy of each row times the a's up to it ...
-        G = fmaf(A, En::get(dyr[i]), G);
-        // ... as far as the first row that ends a sequence
-        if (__builtin_expect((rows.last & ((2u << i) - 1)) == 1u << i, 0))
-            Gend = fmaf(A, a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f, G);
-        if (i % kTogether == kTogether - 1) __builtin_amdgcn_sched_barrier(0);
+        rate[n] = a.rate[cc + n];
+        rate2[n] = rate[n] * kLog2e;
+        h[n] = a.saved[(size_t)k * a.C + cc + n];  // the state before the chunk
     }
-    if (rows.last) G = Gend;
-    fold[0][wv][lane] = A;
-    fold[1][wv][lane] = B;
-    fold[2][wv][lane] = G;
+    const RowKinds kinds = row_kinds(a, row0);
+    const LaneRows<V> rows(kinds, g);
+    if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.dhf, a.dh0, cb * 64 + lane, cb == 0);
+
+    // gates, and the two folds: states from the left, gradients from the right.
+    // hb: the row's input term, later the state before it; r = 0 where the state
+    // is held (no other logit gives it).  a and beta are computed anew from r
+    // wherever they are needed: with them kept, the 16 rows would not leave room
+    // for a second workgroup on the CU, which is what hides this one's waits (203
+    // us with half the rows and all kept, one workgroup a CU, against 149 at B16
+    // L2048 C1024 bf16).
+    float r[ROWS][V], in[ROWS][V], hb[ROWS][V], A[V], B[V], G[V], Gend[V];
+#pragma unroll
+    for (int n = 0; n < V; ++n) A[n] = 1.f, B[n] = G[n] = Gend[n] = 0.f;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+        for (int n = 0; n < V; ++n) {
+            const float l = logit<IN, V>(gar[i], n, scale[1][n]);
+            r[i][n] = sigmoid_f(l);
+            in[i][n] = sigmoid_f(N::get(gir[i], n, scale[2][n]));
+            float ix = in[i][n] * N::get(xr[i], n, scale[0][n]);
+            const bool hold = l <= kGateHold;
+            r[i][n] = hold ? 0.f : r[i][n];
+            ix = hold ? 0.f : ix;
+            float before = B[n];
+            if (rare(rows.unused_any | rows.first_any, i)) {
+                if (!rows.is(rows.used, i)) r[i][n] = 0.f;
+                before = rows.state(a.h0, i, a.C, cc + n, rows.is(rows.first, i), before);
+            }
+            const Decay d = decay_of(r[i][n], rate2[n]);
+            hb[i][n] = __builtin_amdgcn_sqrtf(d.beta2) * ix;
+            B[n] = fmaf(d.a, before, hb[i][n]);
+            A[n] *= d.a;
+            // the gradient that leaves the first row: dy of each row times the a's up to it ...
+            G[n] = fmaf(A[n], S::get(dyr[i], n), G[n]);
+            // ... as far as the first row that ends a sequence
+            if (rare(rows.last_any, i)) {
+                const bool end = rows.is(rows.last & (0u - rows.last), i);
+                const float from = rows.state(a.dhf, i, a.C, cc + n, end, 0.f);
+                if (end) Gend[n] = fmaf(A[n], from, G[n]);
+            }
+        }
+        if (i % Shape<V>::TOGETHER == Shape<V>::TOGETHER - 1) __builtin_amdgcn_sched_barrier(0);
+    }
+    // the wave's steps from its groups'; Ag, Bg: the upper group's, Al, Gl: the lower one's
+    const bool first_upper = (kinds.first & LaneRows<V>::kAll) != 0, first_lower = kinds.first >> ROWS != 0;
+    const bool last_upper = (kinds.last & LaneRows<V>::kAll) != 0, last_lower = kinds.last >> ROWS != 0;
+    float Ag[V], Bg[V], Al[V], Gl[V];
+#pragma unroll
+    for (int n = 0; n < V; ++n) {
+        if (rows.last) G[n] = Gend[n];
+        Ag[n] = Al[n] = A[n];
+        Bg[n] = B[n];
+        Gl[n] = G[n];
+        if constexpr (V == 2) {
+            const float Ao = other_group(A[n]), Bo = other_group(B[n]), Go = other_group(G[n]);
+            const float Bl = g ? B[n] : Bo, Gu = g ? Go : G[n];
+            Al[n] = g ? A[n] : Ao;
+            Ag[n] = g ? Ao : A[n];
+            Bg[n] = g ? Bo : B[n];
+            Gl[n] = g ? G[n] : Go;
+            A[n] = Al[n] * Ag[n];
+            B[n] = first_lower ? Bl : fmaf(Al[n], Bg[n], Bl);
+            G[n] = last_upper ? Gu : fmaf(Ag[n], Gl[n], Gu);
+        }
+        if (g == 0) {
+            fold[0][wv][lc + n] = A[n];
+            fold[1][wv][lc + n] = B[n];
+            fold[2][wv][lc + n] = G[n];
+        }
+    }
     if (lane == 0) {
-        cuts[0][wv] = rows.first != 0;
-        cuts[1][wv] = rows.last != 0;
+        cuts[0][wv] = kinds.first != 0;
+        cuts[1][wv] = kinds.last != 0;
     }
     __syncthreads();
+    const uint32_t first_waves = (uint32_t)__ballot(lane < kWaves && cuts[0][lane & (kWaves - 1)]);
+    const uint32_t last_waves = (uint32_t)__ballot(lane < kWaves && cuts[1][lane & (kWaves - 1)]);
     // the last wave's rows end the chunk: it finds what comes from the right
     if (wv == kWaves - 1) {
         float At = 1.f, Gt = 0.f;
-        bool cut = k == NC - 1;
 #pragma unroll 4
         for (int w = kWaves - 1; w >= 0; --w) {
-            const bool cw = __builtin_amdgcn_readfirstlane(cuts[1][w]);
-            Gt = cw ? fold[2][w][lane] : fmaf(fold[0][w][lane], Gt, fold[2][w][lane]);
+            Gt = last_waves >> w & 1 ? fold[2][w][lane] : fmaf(fold[0][w][lane], Gt, fold[2][w][lane]);
             At *= fold[0][w][lane];
-            cut |= cw;
         }
+        const bool cut = k == NC - 1 || last_waves;
         uint64_t* mine = words_in(a.ws, NB) + ((size_t)k * NB + cb) * 64;
         if (k > 0) put_word(mine + lane, cut ? state_word(Gt) : step_word(At, Gt));
         float u = 0.f;
-        if (k + 1 < NC && !(rows.last >> (kRows - 1) & 1)) {
+        if (k + 1 < NC && !(kinds.last >> (kWaveRows - 1) & 1)) {
             u = chunk_entry(mine + (size_t)NB * 64, (ptrdiff_t)NB * 64, NC - 1 - k, a.status);
             if (k > 0 && !cut) put_word(mine + lane, state_word(fmaf(At, u, Gt)));
         }
         entry[lane] = u;
     }
     // the states before the rows, while that wave may wait
-    float h = before_chunk;
-#pragma unroll 4
-    for (int w = 0; w < wv; ++w)
-        h = __builtin_amdgcn_readfirstlane(cuts[0][w]) ? fold[1][w][lane] : fmaf(fold[0][w][lane], h, fold[1][w][lane]);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        if (__builtin_expect(rows.first >> i & 1, 0)) h = a.h0 ? a.h0[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-        const float b = hb[i];
-        hb[i] = h;
-        h = fmaf(__builtin_amdgcn_exp2f(-rate2 * r[i]), h, b);
-        // what comes of these is computed again below, not kept
-        asm volatile("" : "+v"(r[i]), "+v"(xr[i]), "+v"(dyr[i]));
+    for (int n = 0; n < V; ++n) {
+#pragma unroll 4
+        for (int w = 0; w < wv; ++w)
+            h[n] = first_waves >> w & 1 ? fold[1][w][lc + n] : fmaf(fold[0][w][lc + n], h[n], fold[1][w][lc + n]);
+        if (g) h[n] = first_upper ? Bg[n] : fmaf(Ag[n], h[n], Bg[n]);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+#pragma unroll
+        for (int n = 0; n < V; ++n) {
+            if (rare(rows.first_any, i)) h[n] = rows.state(a.h0, i, a.C, cc + n, rows.is(rows.first, i), h[n]);
+            const float b = hb[i][n];
+            hb[i][n] = h[n];
+            h[n] = fmaf(__builtin_amdgcn_exp2f(-rate2[n] * r[i][n]), h[n], b);
+            asm volatile("" : "+v"(r[i][n]));  // what comes of these is computed again below, not kept
+        }
+        asm volatile("" : "+v"(xr[i]), "+v"(dyr[i]));
     }
     __syncthreads();
-    float u = entry[lane];
+    float u[V], sum[V];
+#pragma unroll
+    for (int n = 0; n < V; ++n) {
+        u[n] = entry[lc + n];
+        sum[n] = 0.f;
 #pragma unroll 4
-    for (int w = kWaves - 1; w > wv; --w)
-        u = __builtin_amdgcn_readfirstlane(cuts[1][w]) ? fold[2][w][lane] : fmaf(fold[0][w][lane], u, fold[2][w][lane]);
+        for (int w = kWaves - 1; w > wv; --w)
+            u[n] = last_waves >> w & 1 ? fold[2][w][lc + n] : fmaf(fold[0][w][lc + n], u[n], fold[2][w][lc + n]);
+        if (V == 2 && g == 0) u[n] = last_lower ? Gl[n] : fmaf(Al[n], u[n], Gl[n]);
+    }
     RowBlock out[3];
 #pragma unroll
-    for (int n = 0; n < 3; ++n) out[n] = row_block_of<kRows>(a.d[n], a.ldd, sizeof(typename En::T), a.T, a.C, row0);
-    const uint32_t voff = live ? (uint32_t)c * sizeof(typename En::T) : kPast;
-    float sum = 0.f;
+    for (int m = 0; m < 3; ++m) out[m] = row_block_of(a.d[m], a.ldd, S::SIZE, a.T, a.C, row0);
+    const uint32_t voff = live ? (uint32_t)(g * ROWS) * out[0].ld + (uint32_t)c * S::SIZE : kPast;
 #pragma unroll
-    for (int i = kRows - 1; i >= 0; --i) {
-        if (__builtin_expect(rows.last >> i & 1, 0)) u = a.dhf ? a.dhf[(size_t)rows.seq(i) * a.C + cc] : 0.f;
-        const float g = En::get(dyr[i]) + u, x = Entry<IN>::get(xr[i], scale[0]);
-        const Decay d = decay_of(r[i], rate2);
-        const float t = in[i] * __builtin_amdgcn_rsqf(d.beta2);  // i / beta
-        float dx = g * d.beta2 * t;
-        u = g * d.a;
-        float w = rate * r[i] * u * fmaf(x * d.a, t, -hb[i]);
-        float dxx = dx * x;
-        dxx = fmaf(-dxx, in[i], dxx);
-        {
-            const bool hold = r[i] == 0.f;
-            dx = hold ? 0.f : dx;
+    for (int i = ROWS - 1; i >= 0; --i) {
+        float d0[V], d1[V], d2[V];
+#pragma unroll
+        for (int n = 0; n < V; ++n) {
+            if (rare(rows.last_any, i)) u[n] = rows.state(a.dhf, i, a.C, cc + n, rows.is(rows.last, i), u[n]);
+            const float gr = S::get(dyr[i], n) + u[n], x = N::get(xr[i], n, scale[0][n]);
+            const Decay d = decay_of(r[i][n], rate2[n]);
+            const float t = in[i][n] * __builtin_amdgcn_rsqf(d.beta2);  // i / beta
+            float dx = gr * d.beta2 * t;
+            u[n] = gr * d.a;
+            float w = rate[n] * r[i][n] * u[n] * fmaf(x * d.a, t, -hb[i][n]);
+            float dxx = dx * x;
+            dxx = fmaf(-dxx, in[i][n], dxx);
+            const bool hold = r[i][n] == 0.f;
+            d0[n] = hold ? 0.f : dx;
             w = hold ? 0.f : w;
-            dxx = hold ? 0.f : dxx;
+            d2[n] = hold ? 0.f : dxx;
+            sum[n] += w;
+            d1[n] = fmaf(-w, r[i][n], w);
         }
-        sum += w;
-        if (rows.used >> i & 1) {
-            store_entry(out[0], i, voff, En::put(dx));
-            store_entry(out[1], i, voff, En::put(fmaf(-w, r[i], w)));
-            store_entry(out[2], i, voff, En::put(dxx));
+        uint32_t to = voff;
+        if (rare(rows.unused_any | rows.first_any, i)) {
+            to = rows.is(rows.used, i) ? voff : kPast;
+#pragma unroll
+            for (int n = 0; n < V; ++n) {
+                float* f = rows.place(a.dh0, i, a.C, cc + n);
+                if (rows.is(rows.first, i) && live && a.dh0) *f = u[n];
+            }
         }
-        if (__builtin_expect((rows.first >> i & 1) && live && a.dh0, 0)) a.dh0[(size_t)rows.seq(i) * a.C + c] = u;
-        if (i % kTogether == 0) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (V == 1) {
+            S::store(out[0], i, to, d0[0]);
+            S::store(out[1], i, to, d1[0]);
+            S::store(out[2], i, to, d2[0]);
+        } else {
+            S::store(out[0], i, to, d0);
+            S::store(out[1], i, to, d1);
+            S::store(out[2], i, to, d2);
+        }
+        if (i % Shape<V>::TOGETHER == 0) __builtin_amdgcn_sched_barrier(0);
     }
     if (!a.drate) return;
+#pragma unroll
+    for (int n = 0; n < V; ++n) sums[wv * V + g][lc + n] = sum[n];
     __syncthreads();
-    fold[0][wv][lane] = sum;
-    __syncthreads();
-    if (wv == 0 && live) {
+    const int ch = cb * 64 + lane;
+    if (wv == 0 && ch < a.C) {
         float all = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) all += fold[0][w][lane];
-        if (NC > 1) part[(size_t)k * a.C + c] = all;
-        else a.drate[c] = all / rate;
+        for (int w = 0; w < kWaves * V; ++w) all += sums[w][lane];
+        if (NC > 1) part[(size_t)k * a.C + ch] = all;
+        else a.drate[ch] = all / a.rate[ch];
     }
 }
 
@@ -633,6 +810,11 @@ void clear_words(const GatedArgs& a, hipStream_t s) {
 }
 }  // namespace
 
+namespace {
+// Whether rows of size-byte entries can be read two channels at a time.
+bool pairs(const void* p, int64_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % (2 * size) == 0 && ld % 2 == 0; }
+}  // namespace
+
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s) {
     const int NC = chunks_of(a.T), NB = blocks_of(a.C);
     if (NC == 0) {
@@ -640,10 +822,13 @@ hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s) {
         return hipGetLastError();
     }
     if (NC > 1) clear_words(a, s);
-    constexpr int kWaves = kGatedChunk / kFwdRows;
-    auto* f = a.io == kRowBf16 ? (a.q[0] ? k_gated_fwd<kRowBf16, true> : k_gated_fwd<kRowBf16, false>)
-                               : (a.q[0] ? k_gated_fwd<kRowF32, true> : k_gated_fwd<kRowF32, false>);
-    hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a);
+    auto go = [&](auto* f) { hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a); };
+    const bool keep = a.q[0] != nullptr;
+    if (a.io == kRowBf16) {
+        keep ? go(k_gated_fwd<kRowBf16, true>) : go(k_gated_fwd<kRowBf16, false>);
+    } else {
+        keep ? go(k_gated_fwd<kRowF32, true>) : go(k_gated_fwd<kRowF32, false>);
+    }
     return hipGetLastError();
 }
 
@@ -658,10 +843,16 @@ hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) {
         clear_words(a, s);
         part = reinterpret_cast<float*>(words_in(a.ws, NB) + words_of(a.T, a.C));
     }
-    constexpr int kWaves = kGatedChunk / kBwdRows;
-    auto* f = a.io == kRowBf16 ? (a.kept ? k_gated_bwd<kRowBf16, kRowKept> : k_gated_bwd<kRowBf16, kRowBf16>)
-                               : (a.kept ? k_gated_bwd<kRowF32, kRowKept> : k_gated_bwd<kRowF32, kRowF32>);
-    hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a, part);
+    bool two = a.io == kRowBf16 && a.C % 2 == 0 && pairs(a.dy.p, a.dy.ld, 2);
+    for (const RowsIn* r : {&a.x, &a.ga, &a.gi}) two = two && pairs(r->p, r->ld, a.kept ? 1 : 2);
+    for (const void* d : a.d) two = two && pairs(d, a.ldd, 2);
+    auto go = [&](auto* f) { hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a, part); };
+    if (a.io == kRowBf16) {
+        if (two) a.kept ? go(k_gated_bwd<kRowBf16, kRowKept, 2>) : go(k_gated_bwd<kRowBf16, kRowBf16, 2>);
+        else a.kept ? go(k_gated_bwd<kRowBf16, kRowKept, 1>) : go(k_gated_bwd<kRowBf16, kRowBf16, 1>);
+    } else {
+        a.kept ? go(k_gated_bwd<kRowF32, kRowKept, 1>) : go(k_gated_bwd<kRowF32, kRowF32, 1>);
+    }
     if (NC > 1 && a.drate) hipLaunchKernelGGL(k_gated_rate, dim3(NB), dim3(1024), 0, s, part, a.rate, a.drate, NC, a.C);
     return hipGetLastError();
 }

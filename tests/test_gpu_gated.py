@@ -181,6 +181,53 @@ def test_eight_bit_checkpoint(which, C, masked, dtype):
     _check_bwd(case, case.bwd(saved, kept), h, size, kept=want)
 
 
+@pytest.mark.parametrize("C", [2, 62, 64, 66, 192])
+@pytest.mark.parametrize("which", sorted(BOUNDS))
+def test_backward_of_paired_channels(which, C):
+    """bf16 rows of even width and alignment, where a lane of the backward pass has two channels."""
+    b = BOUNDS[which]
+    case = Case(b, C, T=b[-1] + (7 if C != 64 else 0), dtype=torch.bfloat16, wide=False, states=C != 66,
+                masked=C in (62, 192), seed=len(b) + C)
+    y, fin, saved, kept = case.fwd(hold8=True)
+    h, size = _check_fwd(case, y, fin)
+    got = case.bwd(saved)
+    _check_bwd(case, got, h, size)
+    want = G.kept(*(_np(t) for t in (case.x, case.ga, case.gi)), case.end)
+    _check_bwd(case, case.bwd(saved, kept), h, size, kept=want)
+    held = _np(case.ga)[:case.end] <= G.HOLD
+    for t in got[:3]:
+        assert (_np(t)[:case.end][held] == 0).all()
+
+
+def test_paired_channels_leave_rows_behind_alone():
+    """The same with rows behind the last sequence: neither read for a result nor written."""
+    case = Case([0, 40, 130], 66, T=300, dtype=torch.bfloat16, wide=False, seed=3)
+    outs = []
+    for junk in (0.0, math.nan):
+        for t in (case.x, case.ga, case.gi):
+            t[130:] = junk
+        case.dy[130:] = junk
+        _, _, saved, kept = case.fwd(hold8=True)
+        lib, P, p = pdssm.load(), ctypes.byref, pdssm._p
+        for eight in (False, True):
+            d = pdssm.GatedDesc(case.T, case.C, case.S, pdssm.FLAG_BF16_IO)
+            r = [pdssm.Rows(t.data_ptr(), t.stride(0), None) for t in (case.x, case.ga, case.gi)]
+            if eight:
+                r = [pdssm.Rows(q.data_ptr(), 66, e.data_ptr()) for q, e in kept]
+            ws = torch.empty(lib.pdssm_gated_workspace_size(P(d), pdssm.OP_BWD), dtype=torch.uint8, device=DEV)
+            g = [torch.full((300, 66), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(3)]
+            drate, dh0 = torch.empty(66, device=DEV), torch.empty(2, 66, device=DEV)
+            rdy = pdssm.Rows(case.dy.data_ptr(), 66, None)
+            assert lib.pdssm_gated_bwd(P(d), P(r[0]), P(r[1]), P(r[2]), p(case.rate), p(case.cu), p(case.h0), p(saved),
+                                       P(rdy), p(case.dhf), pdssm._three(g), 66, p(drate), p(dh0), p(ws), ws.numel(),
+                                       None, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == 0
+            torch.cuda.synchronize()
+            assert all((t[130:] == 7).all() for t in g)
+            outs.append([t[:130] for t in g] + [drate, dh0])
+    for a, b in zip(outs[:2], outs[2:]):
+        assert all(torch.equal(v, w) for v, w in zip(a, b))
+
+
 def test_rows_behind_and_untouched_outputs():
     """Rows behind the last sequence: no output of theirs is written, and what they hold does not matter."""
     case = Case([0, 40, 130], 65, T=300, seed=3)
