@@ -78,10 +78,14 @@ __device__ __forceinline__ void put_word(uint64_t* p, uint64_t w) {
     __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Four words a thread (n is a multiple of 64).
 __global__ __launch_bounds__(256) void k_gated_clear(void* ws, int NB, size_t n) {
+    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (i < (size_t)NB) *reinterpret_cast<unsigned*>(static_cast<char*>(ws) + i * kTicketStride) = 0;
-    if (i < n) words_in(ws, NB)[i] = kEmpty;
+    if (i * 4 >= n) return;
+    u64x2* w = reinterpret_cast<u64x2*>(words_in(ws, NB) + i * 4);
+    w[0] = w[1] = u64x2{kEmpty, kEmpty};
 }
 
 // The state (or gradient) that enters a chunk, for the 64 channels of a wave:
@@ -195,16 +199,24 @@ struct LaneRows {
         asm volatile("" : "+v"(mask));
         return mask >> i & 1;
     }
+    // Sequence of row i, 0 where it has none.  Waited for here and not behind
+    // the branch: there the wait would hold for all rows' loads and stores, of
+    // the many waves too that do not take it.
+    __device__ __forceinline__ int sequence(int i) const {
+        int q = V == 1 ? readlane_i(id, i + 1) : __shfl(id, g * ROWS + i + 1);
+        if constexpr (V == 2) asm volatile("" : "+v"(q));
+        return max(q, 0);
+    }
     // s[sequence of row i][c] where wanted (0 without s), else what it was
     __device__ __forceinline__ float state(const float* s, int i, int C, int c, bool wanted, float else_) const {
-        const int q = V == 1 ? readlane_i(id, i + 1) : __shfl(id, g * ROWS + i + 1);
-        if (wanted) else_ = s ? s[(size_t)max(q, 0) * C + c] : 0.f;
+        const int q = sequence(i);
+        if (wanted) {
+            else_ = s ? s[(size_t)q * C + c] : 0.f;
+            asm volatile("" : "+v"(else_));
+        }
         return else_;
     }
-    __device__ __forceinline__ float* place(float* s, int i, int C, int c) const {
-        const int q = V == 1 ? readlane_i(id, i + 1) : __shfl(id, g * ROWS + i + 1);
-        return s + (size_t)max(q, 0) * C + c;
-    }
+    __device__ __forceinline__ float* place(float* s, int i, int C, int c) const { return s + (size_t)sequence(i) * C + c; }
 };
 
 // cu is in order and in range, or the call is reported; out[s] = in[s] (0 if
@@ -322,16 +334,18 @@ __device__ __forceinline__ float logit(typename Some<IO, V>::R v, int n, float s
     return Some<IO, V>::get(v, n, scale);
 }
 
-// This lane's entries of the wave's rows, group g, channels c ...
+// This lane's entries of the wave's rows, channels c ...; row by row, in the
+// order of their use, so that the first row's work begins when it is there
+// (backward at B16 L2048 C1024 bf16: 124 -> 119 us).
 template <int IO, int V>
-__device__ __forceinline__ void load_rows(typename Some<IO, V>::R (&v)[Shape<V>::ROWS], const RowsIn& r, int T, int C, int row0,
-                                          int g, int c) {
+struct RowsOf {
     using S = Some<IO, V>;
-    const RowBlock b = row_block_of(r.p, r.ld, S::SIZE, T, C, row0);
-    const uint32_t voff = (uint32_t)(g * Shape<V>::ROWS) * b.ld + (uint32_t)c * S::SIZE;
-#pragma unroll
-    for (int i = 0; i < Shape<V>::ROWS; ++i) v[i] = S::load(b, i, voff);
-}
+    RowBlock b;
+    uint32_t voff;
+    __device__ __forceinline__ RowsOf(const RowsIn& r, int T, int C, int row0, int g, int c)
+        : b(row_block_of(r.p, r.ld, S::SIZE, T, C, row0)), voff((uint32_t)(g * Shape<V>::ROWS) * b.ld + (uint32_t)c * S::SIZE) {}
+    __device__ __forceinline__ typename S::R row(int i) const { return S::load(b, i, voff); }
+};
 
 // The same entry of the other group of lanes.
 __device__ __forceinline__ float other_group(float v) { return __shfl_xor(v, 32); }
@@ -385,10 +399,15 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
     const int cc = live ? c : a.C - 1;
 
     typename S::R x[ROWS], ga[ROWS], gi[ROWS];
-    load_rows<IO, 1>(ga, a.ga, a.T, a.C, row0, 0, cc);
-    load_rows<IO, 1>(gi, a.gi, a.T, a.C, row0, 0, cc);
-    load_rows<IO, 1>(x, a.x, a.T, a.C, row0, 0, cc);
     const float rate2 = a.rate[cc] * kLog2e;
+    const RowsOf<IO, 1> xs(a.x, a.T, a.C, row0, 0, cc), gas(a.ga, a.T, a.C, row0, 0, cc), gis(a.gi, a.T, a.C, row0, 0, cc);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        ga[i] = gas.row(i);
+        gi[i] = gis.row(i);
+        x[i] = xs.row(i);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     const RowKinds kinds = row_kinds(a, row0);
     const LaneRows<1> rows(kinds, 0);
     if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.h0, a.h_final, c, cb == 0);
@@ -531,12 +550,6 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
     const bool live = c < a.C;
     const int cc = live ? c : a.C - V;
 
-    typename N::R xr[ROWS], gar[ROWS], gir[ROWS];
-    typename S::R dyr[ROWS];
-    load_rows<IN, V>(gar, a.ga, a.T, a.C, row0, g, cc);
-    load_rows<IN, V>(gir, a.gi, a.T, a.C, row0, g, cc);
-    load_rows<IN, V>(xr, a.x, a.T, a.C, row0, g, cc);
-    load_rows<IO, V>(dyr, a.dy, a.T, a.C, row0, g, cc);
     float scale[3][V], rate[V], rate2[V], h[V];
 #pragma unroll
     for (int n = 0; n < V; ++n) {
@@ -550,6 +563,18 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
         rate[n] = a.rate[cc + n];
         rate2[n] = rate[n] * kLog2e;
         h[n] = a.saved[(size_t)k * a.C + cc + n];  // the state before the chunk
+    }
+    typename N::R xr[ROWS], gar[ROWS], gir[ROWS];
+    typename S::R dyr[ROWS];
+    const RowsOf<IN, V> xs(a.x, a.T, a.C, row0, g, cc), gas(a.ga, a.T, a.C, row0, g, cc), gis(a.gi, a.T, a.C, row0, g, cc);
+    const RowsOf<IO, V> dys(a.dy, a.T, a.C, row0, g, cc);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        gar[i] = gas.row(i);
+        gir[i] = gis.row(i);
+        xr[i] = xs.row(i);
+        dyr[i] = dys.row(i);
+        __builtin_amdgcn_sched_barrier(0);
     }
     const RowKinds kinds = row_kinds(a, row0);
     const LaneRows<V> rows(kinds, g);
@@ -738,18 +763,24 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
     }
 }
 
-// drate from the chunks' sums: 16 waves take every 16th chunk of 64 channels.
+// drate from the chunks' sums, 16 channels a workgroup: quarter q of wave w
+// takes every 64th chunk from 4 w + q on.
 __global__ __launch_bounds__(1024) void k_gated_rate(const float* part, const float* rate, float* drate, int NC, int C) {
-    __shared__ float sums[16][64];
-    const int wv = wave_id(), lane = lane_id(), c = blockIdx.x * 64 + lane;
+    __shared__ float sums[16][16];
+    const int wv = wave_id(), lane = lane_id(), ch = lane & 15, c = blockIdx.x * 16 + ch;
     float s = 0.f;
-    if (c < C)
-        for (int k = wv; k < NC; k += 16) s += part[(size_t)k * C + c];
-    sums[wv][lane] = s;
+    if (c < C) {
+#pragma unroll 4
+        for (int k = wv * 4 + lane / 16; k < NC; k += 64) s += part[(size_t)k * C + c];
+    }
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (lane < 16) sums[wv][ch] = s;
     __syncthreads();
-    if (wv != 0 || c >= C) return;
+    if (wv != 0 || lane >= 16 || c >= C) return;
     s = 0.f;
-    for (int w = 0; w < 16; ++w) s += sums[w][lane];
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += sums[w][ch];
     drate[c] = s / rate[c];
 }
 
@@ -805,8 +836,8 @@ size_t gated_workspace(int T, int C, int S, bool bwd) {
 namespace {
 void clear_words(const GatedArgs& a, hipStream_t s) {
     const int NB = blocks_of(a.C);
-    const size_t n = words_of(a.T, a.C);  // at least 128 for each counter
-    hipLaunchKernelGGL(k_gated_clear, dim3((n + 255) / 256), dim3(256), 0, s, a.ws, NB, n);
+    const size_t n = words_of(a.T, a.C);  // at least 128 for each counter, so there are threads for all of them
+    hipLaunchKernelGGL(k_gated_clear, dim3((n / 4 + 255) / 256), dim3(256), 0, s, a.ws, NB, n);
 }
 }  // namespace
 
@@ -853,7 +884,7 @@ hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) {
     } else {
         a.kept ? go(k_gated_bwd<kRowF32, kRowKept, 1>) : go(k_gated_bwd<kRowF32, kRowF32, 1>);
     }
-    if (NC > 1 && a.drate) hipLaunchKernelGGL(k_gated_rate, dim3(NB), dim3(1024), 0, s, part, a.rate, a.drate, NC, a.C);
+    if (NC > 1 && a.drate) hipLaunchKernelGGL(k_gated_rate, dim3((a.C + 15) / 16), dim3(1024), 0, s, part, a.rate, a.drate, NC, a.C);
     return hipGetLastError();
 }
 
