@@ -794,9 +794,20 @@ __global__ __launch_bounds__(64) void k_gated_none(GatedArgs a, const float* in,
     if (a.drate) a.drate[c] = 0.f;
 }
 
-template <int IO>
+// V entries of a row, next to each other and aligned as one.
+template <int IO, int V>
+struct alignas(V * sizeof(typename Entry<IO>::T)) Pack {
+    typename Entry<IO>::T v[V];
+};
+
+// One row b of a batch, V channels a thread.
+template <int IO, int V>
 __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
-    const int c = blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
+    using En = Entry<IO>;
+    using Row = Pack<IO, V>;
+    using State = Pack<kRowF32, V>;
+    const int c = (blockIdx.x * 256 + threadIdx.x) * V, b = blockIdx.y;
+    const bool live = c < a.C;
     int slot = b;
     if (a.slots) {
         slot = a.slots[b];
@@ -804,6 +815,19 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
             if (slot >= a.pool) report_index_error(a.status);
             return;
         }
+    }
+    auto at = [&](const RowsIn& r) {
+        return *reinterpret_cast<const Row*>(static_cast<const typename En::T*>(r.p) + (size_t)b * r.ld + c);
+    };
+    const size_t o = (size_t)slot * a.C + c;
+    Row x = {}, ga = {}, gi = {};
+    State rate = {}, h = {};
+    if (live) {
+        x = at(a.x);
+        ga = at(a.ga);
+        gi = at(a.gi);
+        rate = *reinterpret_cast<const State*>(a.rate + c);
+        h = *reinterpret_cast<const State*>(a.h_in + o);
     }
     // the first row that names a slot has it; others of the same batch are refused
     bool again = false;
@@ -813,17 +837,19 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
         report_index_error(a.status);
         return;
     }
-    if (c >= a.C) return;
-    using En = Entry<IO>;
-    auto at = [&](const RowsIn& r) { return En::get(static_cast<const typename En::T*>(r.p)[(size_t)b * r.ld + c]); };
-    const float l = at(a.ga);
-    const bool hold = l <= kGateHold;
-    const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), a.rate[c] * kLog2e);
-    const float in = hold ? 0.f : __builtin_amdgcn_sqrtf(d.beta2) * sigmoid_f(at(a.gi)) * at(a.x);
-    const size_t o = (size_t)slot * a.C + c;
-    const float h = fmaf(d.a, a.h_in[o], in);
-    a.h_out[o] = h;
-    static_cast<typename En::T*>(a.y)[(size_t)b * a.C + c] = En::put(h);
+    if (!live) return;
+    Row y;
+#pragma unroll
+    for (int n = 0; n < V; ++n) {
+        const float l = En::get(ga.v[n]);
+        const bool hold = l <= kGateHold;
+        const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), rate.v[n] * kLog2e);
+        const float in = hold ? 0.f : __builtin_amdgcn_sqrtf(d.beta2) * sigmoid_f(En::get(gi.v[n])) * En::get(x.v[n]);
+        h.v[n] = fmaf(d.a, h.v[n], in);
+        y.v[n] = En::put(h.v[n]);
+    }
+    *reinterpret_cast<State*>(a.h_out + o) = h;
+    *reinterpret_cast<Row*>(static_cast<typename En::T*>(a.y) + (size_t)b * a.C + c) = y;
 }
 
 }  // namespace
@@ -842,8 +868,10 @@ void clear_words(const GatedArgs& a, hipStream_t s) {
 }  // namespace
 
 namespace {
-// Whether rows of size-byte entries can be read two channels at a time.
-bool pairs(const void* p, int64_t ld, int size) { return reinterpret_cast<uintptr_t>(p) % (2 * size) == 0 && ld % 2 == 0; }
+// Whether rows of size-byte entries can be read n channels at a time.
+bool by(int n, const void* p, int64_t ld, int size) {
+    return reinterpret_cast<uintptr_t>(p) % (n * size) == 0 && ld % n == 0;
+}
 }  // namespace
 
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s) {
@@ -874,9 +902,9 @@ hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) {
         clear_words(a, s);
         part = reinterpret_cast<float*>(words_in(a.ws, NB) + words_of(a.T, a.C));
     }
-    bool two = a.io == kRowBf16 && a.C % 2 == 0 && pairs(a.dy.p, a.dy.ld, 2);
-    for (const RowsIn* r : {&a.x, &a.ga, &a.gi}) two = two && pairs(r->p, r->ld, a.kept ? 1 : 2);
-    for (const void* d : a.d) two = two && pairs(d, a.ldd, 2);
+    bool two = a.io == kRowBf16 && a.C % 2 == 0 && by(2, a.dy.p, a.dy.ld, 2);
+    for (const RowsIn* r : {&a.x, &a.ga, &a.gi}) two = two && by(2, r->p, r->ld, a.kept ? 1 : 2);
+    for (const void* d : a.d) two = two && by(2, d, a.ldd, 2);
     auto go = [&](auto* f) { hipLaunchKernelGGL(f, dim3((unsigned)NC * NB), dim3(kWaves * 64), 0, s, a, part); };
     if (a.io == kRowBf16) {
         if (two) a.kept ? go(k_gated_bwd<kRowBf16, kRowKept, 2>) : go(k_gated_bwd<kRowBf16, kRowBf16, 2>);
@@ -889,8 +917,15 @@ hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_gated_step(const GatedStepArgs& a, hipStream_t s) {
-    auto* f = a.io == kRowBf16 ? k_gated_step<kRowBf16> : k_gated_step<kRowF32>;
-    hipLaunchKernelGGL(f, dim3((a.C + 255) / 256, a.B), dim3(256), 0, s, a);
+    // four channels a thread where width and alignment allow: 11.5 -> 7.6 us for 512 rows of 4096 bf16 channels
+    const int size = a.io == kRowBf16 ? 2 : 4;
+    bool four = a.C % 4 == 0 && by(4, a.y, a.C, size);
+    for (const RowsIn* r : {&a.x, &a.ga, &a.gi}) four = four && by(4, r->p, r->ld, size);
+    for (const float* p : {a.rate, a.h_in, static_cast<const float*>(a.h_out)}) four = four && by(4, p, a.C, 4);
+    const int wide = four ? 1024 : 256;
+    auto* f = a.io == kRowBf16 ? (four ? k_gated_step<kRowBf16, 4> : k_gated_step<kRowBf16, 1>)
+                               : (four ? k_gated_step<kRowF32, 4> : k_gated_step<kRowF32, 1>);
+    hipLaunchKernelGGL(f, dim3((a.C + wide - 1) / wide, a.B), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

@@ -351,7 +351,18 @@ def test_no_rows():
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
 @pytest.mark.parametrize("B,C,pool", [(1, 1, 1), (3, 65, 5), (40, 300, 64), (300, 17, 300)])
 def test_one_token(B, C, pool, dtype):
-    case = Case(list(range(B + 1)), C, dtype=dtype, masked=B == 40, seed=B)
+    _one_token(B, C, pool, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("B,C,pool", [(1, 4, 1), (3, 1020, 5), (40, 1024, 64), (300, 1028, 300), (2, 66, 2)])
+def test_one_token_of_aligned_rows(B, C, pool, dtype):
+    """Where a thread has four channels, and rows of another width beside them."""
+    _one_token(B, C, pool, dtype, False)
+
+
+def _one_token(B, C, pool, dtype, wide):
+    case = Case(list(range(B + 1)), C, dtype=dtype, wide=wide, masked=B == 40, seed=B)
     order = torch.randperm(pool, generator=torch.Generator().manual_seed(B))[:B].to(torch.int32)
     h = torch.randn(pool, C, device=DEV)
     want, size = (G.gated_fwd(*case.ref()[0], case.bounds, _np(h)[order.long().numpy()], absolute=k)[0] for k in (False, True))
