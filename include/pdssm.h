@@ -448,7 +448,7 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
  * magnitude: 64 would stand for 2^128).  Both ways are exact but for that
  * rounding (at most 2^(e-1), at e = 122 2^e), also to bf16.  e = -128 marks a block
  * that held a NaN or an infinity: its values read NaN.  q = -128 is the code
- * of a held gate logit and reads -inf. */
+ * of a held gate logit and reads -inf, in such a block too. */
 #define PDSSM_GATE_HOLD (-64.0f)
 #define PDSSM_GATED_CHUNK 128 /* rows between two saved states */
 #define PDSSM_KEPT_ROWS 32    /* rows that share an exponent in the 8-bit form */
@@ -460,7 +460,9 @@ typedef struct pdssm_rows {
 } pdssm_rows;
 
 typedef struct pdssm_gated_desc {
-    int32_t T, C, S; /* rows, channels, sequences; 0 <= T <= 2^30, 1 <= C <= 2^24, S >= 1 */
+    /* rows, channels, sequences; 0 <= T <= 2^30, 1 <= C <= 2^24, 1 <= S <= 2^30
+     * and ceil(T/128) * ceil(C/64) < 2^23, else PDSSM_ERR_UNSUPPORTED */
+    int32_t T, C, S;
     uint32_t flags;  /* 0 or PDSSM_FLAG_BF16_IO */
 } pdssm_gated_desc;
 
@@ -475,8 +477,13 @@ size_t pdssm_gated_workspace_size(const pdssm_gated_desc* desc, int op);
  * pdssm_gated_bwd needs (a row whose chunk begins with a sequence's first row
  * is not read there); optional q[3], e[3]: x, ga, gi in the 8-bit form, all
  * six or none (q == e == NULL).  In a held row x and gi are kept as 0 and ga as
- * held.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned.
+ * held.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned (0: none).
  * Results are deterministic.
+ *
+ * In this call and the next, workgroups with different rows of a channel wait
+ * for each other, in an order in which each waits only for such as have begun.
+ * A wait ends after a second or more all the same: PDSSM_ERR_HIP in
+ * *dev_status, and NaN in the rows that needed the answer.
  */
 int pdssm_gated_fwd(const pdssm_gated_desc* desc, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
                     const float* rate, const int32_t* cu, const float* h0, void* y, float* h_final, float* saved,
@@ -507,7 +514,8 @@ int pdssm_gated_bwd(const pdssm_gated_desc* desc, const pdssm_rows* x, const pds
  * A row with a negative slot is skipped (padding of a batch).  A slot >= S, and a
  * slot that an earlier row of the call has named, is reported as PDSSM_ERR_INDEX
  * and its row skipped.  Skipped rows of y, and the entries of h_out of states
- * that no row advances, are not written.  h_out may be h_in.  y [T, C].
+ * that no row advances, are not written.  h_out may be h_in.  y [T, C].  T <=
+ * 65535, else PDSSM_ERR_UNSUPPORTED.
  */
 int pdssm_gated_step(const pdssm_gated_desc* desc, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
                      const float* rate, const int32_t* slots, const float* h_in, float* h_out, void* y,
@@ -516,7 +524,8 @@ int pdssm_gated_step(const pdssm_gated_desc* desc, const pdssm_rows* x, const pd
 /*
  * Rows to the 8-bit form and back.  u: rows [T, C], fp32 or, with
  * PDSSM_FLAG_BF16_IO, bf16; q [T, C], e [ceil(T/32), C]; out [T, C], fp32 or
- * bf16 by the flag.  T >= 0, C >= 1.
+ * bf16 by the flag.  0 <= T <= 2^30, 1 <= C <= 2^24, ceil(T/32) * ceil(C/64) <
+ * 2^25, else PDSSM_ERR_UNSUPPORTED.
  */
 int pdssm_pack8(int32_t T, int32_t C, uint32_t flags, const pdssm_rows* u, int8_t* q, int8_t* e, void* stream);
 int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const int8_t* e, void* out, void* stream);

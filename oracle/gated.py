@@ -111,7 +111,7 @@ def pack8(u):
 def unpack8(q, e):
     scale = np.where(e == -128, np.nan, 2.0 ** np.asarray(e, np.float64))
     v = np.asarray(q, np.float64) * np.repeat(scale, BLOCK, 0)[:q.shape[0]]
-    return np.where((q == -128) & ~np.isnan(v), -np.inf, v)
+    return np.where(q == -128, -np.inf, v)
 
 
 def kept(x, ga, gi, end):

@@ -382,10 +382,18 @@ constexpr int64_t kMaxLd = 1 << 24;  // entries from row to row
 int check_gated(const pdssm_gated_desc* d) {
     if (!d || (d->flags & ~PDSSM_FLAG_BF16_IO) != 0) return PDSSM_ERR_INVALID_ARG;
     if (d->T < 0 || d->C < 1 || d->S < 1) return PDSSM_ERR_INVALID_ARG;
-    // row offsets are 64-bit; offsets within a wave's 16 rows, row numbers, grids
-    // and per-chunk buffers stay below 2^31
-    if (d->T > (1 << 30) || d->C > kMaxLd || (long long)((d->T + 31LL) / 32) * ((d->C + 63) / 64) >= (1LL << 31) ||
-        (long long)d->S * ((d->C + 63) / 64) >= (1LL << 31))
+    // row offsets are 64-bit; offsets within a wave's 16 rows and row numbers stay
+    // below 2^31, and a launch below 2^32 threads (512 for 128 rows of 64 channels)
+    if (d->T > (1 << 30) || d->S > (1 << 30) || d->C > kMaxLd ||
+        (long long)((d->T + 127LL) / 128) * ((d->C + 63) / 64) >= (1LL << 23))
+        return PDSSM_ERR_UNSUPPORTED;
+    return PDSSM_OK;
+}
+
+// The same for the 8-bit form: 64 threads for 32 rows of 64 channels or more.
+int check_kept(int32_t T, int32_t C, uint32_t flags) {
+    if ((flags & ~PDSSM_FLAG_BF16_IO) != 0 || T < 0 || C < 1) return PDSSM_ERR_INVALID_ARG;
+    if (T > (1 << 30) || C > kMaxLd || (long long)((T + 31LL) / 32) * ((C + 63) / 64) >= (1LL << 25))
         return PDSSM_ERR_UNSUPPORTED;
     return PDSSM_OK;
 }
@@ -979,8 +987,7 @@ int pdssm_gated_step(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm
 }
 
 int pdssm_pack8(int32_t T, int32_t C, uint32_t flags, const pdssm_rows* u, int8_t* q, int8_t* e, void* stream) {
-    const pdssm_gated_desc d = {T, C, 1, flags};
-    const int st = check_gated(&d);
+    const int st = check_kept(T, C, flags);
     if (st != PDSSM_OK) return st;
     const size_t w = row_bytes(flags);
     if (bad_rows(u, T, C, w) || u->e || (T > 0 && (!q || !e))) return PDSSM_ERR_INVALID_ARG;
@@ -994,8 +1001,7 @@ int pdssm_pack8(int32_t T, int32_t C, uint32_t flags, const pdssm_rows* u, int8_
 }
 
 int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const int8_t* e, void* out, void* stream) {
-    const pdssm_gated_desc d = {T, C, 1, flags};
-    const int st = check_gated(&d);
+    const int st = check_kept(T, C, flags);
     if (st != PDSSM_OK) return st;
     const size_t w = row_bytes(flags);
     if (T > 0 && (!q || !e || !out || misaligned_to(out, w))) return PDSSM_ERR_INVALID_ARG;

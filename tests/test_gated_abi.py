@@ -67,6 +67,8 @@ class Call:
     (lambda c: setattr(c.d, "S", 0), ERR_INVALID_ARG),
     (lambda c: (setattr(c.d, "C", 1 << 30), setattr(c.d, "T", 1 << 30)), ERR_UNSUPPORTED),
     (lambda c: setattr(c.d, "T", (1 << 30) + 1), ERR_UNSUPPORTED),
+    (lambda c: setattr(c.d, "T", 1 << 30), ERR_UNSUPPORTED),  # 2^32 threads and more
+    (lambda c: setattr(c.d, "S", (1 << 30) + 1), ERR_UNSUPPORTED),
     (lambda c: (setattr(c.d, "C", (1 << 24) + 1), setattr(c.d, "T", 1)), ERR_UNSUPPORTED),
     (lambda c: setattr(c.x, "ld", (1 << 24) + 1), ERR_INVALID_ARG),
     (lambda c: setattr(c.x, "p", None), ERR_INVALID_ARG),
@@ -171,6 +173,9 @@ def test_pack_and_unpack(lib):
                  (9, 40, 0, _at(1), _at(2), _at(3) + 1), (9, 40, FLAG_BF16_IO, _at(1), _at(2), _at(3) + 1),
                  (9, 40, 2 + 4, _at(1), _at(2), _at(3)), (9, 40, 0, _at(1), _at(2), _at(1) + 356)):
         assert lib.pdssm_unpack8(*args, None) == ERR_INVALID_ARG, args[:3]
+    for T, C in (((1 << 30) + 1, 1), (1, (1 << 24) + 1), (1 << 30, 64), (1 << 24, 1 << 12)):
+        assert lib.pdssm_pack8(T, C, 0, P(Rows(_at(1), C, None)), _at(2), _at(3), None) == ERR_UNSUPPORTED
+        assert lib.pdssm_unpack8(T, C, 0, _at(1), _at(2), _at(3), None) == ERR_UNSUPPORTED
 
 
 def test_weight_gradient(lib):

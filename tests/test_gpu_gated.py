@@ -228,6 +228,29 @@ def test_paired_channels_leave_rows_behind_alone():
         assert all(torch.equal(v, w) for v, w in zip(a, b))
 
 
+def test_eight_bit_checkpoint_of_a_block_that_is_not_finite():
+    """A NaN gate makes its block of 32 rows NaN, but for the rows held in it; nothing else changes."""
+    case = Case([0, 60, 200], 66, seed=11, masked=True)
+    clean = case.fwd(hold8=True)
+    g0 = case.bwd(clean[2], clean[3])
+    used = [t for t in range(64, 96) if float(case.ga[t, 3]) > G.HOLD]
+    case.ga[used[4], 3] = math.nan
+    y, fin, saved, kept = case.fwd(hold8=True)
+    for k, (q, e) in enumerate(kept):
+        v = _np(pdssm.unpack8((q, e)))
+        assert np.array_equal(v, G.unpack8(q.cpu().numpy(), e.cpu().numpy()), equal_nan=True)
+        rest = np.ones_like(v, bool)
+        rest[64:96, 3] = k != 1
+        assert np.array_equal(v[rest], _np(pdssm.unpack8(clean[3][k]))[rest])
+    g = case.bwd(saved, kept)
+    held = _np(case.ga)[:, 3] <= G.HOLD
+    for a, b in zip(g[:3], g0[:3]):
+        a, b = _np(a), _np(b)
+        others = [c for c in range(66) if c != 3]
+        assert np.array_equal(a[:, others], b[:, others]) and (a[held, 3] == 0).all()
+        assert np.array_equal(a[:60], b[:60]) and np.isnan(a[used, 3]).all()
+
+
 def test_rows_behind_and_untouched_outputs():
     """Rows behind the last sequence: no output of theirs is written, and what they hold does not matter."""
     case = Case([0, 40, 130], 65, T=300, seed=3)
