@@ -658,15 +658,15 @@ def _on_its_device(f):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
-def _on(stream, dev, tensors, status=None):
+def _on(stream, dev, tensors):
     """The stream to launch on, as a number.  One of the caller's own that is not
-    the current one learns of every tensor of the call, so that none is given
-    to other work before it has run."""
+    the current one waits for it (the memory of the outputs may still be in use
+    there, by work of whoever had it before), and learns of every tensor of the
+    call, so that none is given to other work before it has run."""
     current = _raw_stream(dev.index)
     if stream is None or stream.cuda_stream == current:
         return current
-    if status is not None:
-        stream.wait_stream(torch.cuda.current_stream(dev))  # status is zeroed
+    stream.wait_stream(torch.cuda.current_stream(dev))
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
@@ -714,14 +714,22 @@ def _rows(t, name, dtype, shape, dev):
 def _kept(pair, name, T, C, dev):
     """(address, entries from row to row, address of the exponents) of a pair (q, e) in the 8-bit form."""
     q, e = pair
+    _int32(T, C)
     return (_tensor(q, name + " codes", torch.int8, (T, C), dev), C,
             _tensor(e, name + " exponents", torch.int8, (_ceil(T, KEPT_ROWS), C), dev))
+
+
+def _int32(*sizes):
+    """Sizes that the library takes as 32-bit numbers."""
+    if max(sizes) > 0x7fffffff:
+        raise PdssmError(ERR_UNSUPPORTED, "sizes %s" % (sizes,))
 
 
 class _Args:
     """A descriptor and up to four row tensors in memory that the library reads during the call."""
 
     def __init__(self, T, C, S, flags, *rows):
+        _int32(T, C, S)
         self.d = GatedDesc(T, C, S, flags)
         self.rows = (Rows * len(rows))(*rows)
         self.at = [ctypes.addressof(self.d)]
@@ -818,7 +826,7 @@ def gated_fwd(x, ga, gi, rate, cu=None, h0=None, hold8=False, check=True, stream
     ws = _gated_ws(args, OP_FWD, dev)
     status = _status(check, dev)
     s = _on(stream, dev, (x, ga, gi, rate, cu, h0, y, h_final, saved, ws, status,
-                          *([t for k in kept for t in k] if hold8 else ())), status)
+                          *([t for k in kept for t in k] if hold8 else ())))
     st = load().pdssm_gated_fwd(*args.at, rate_at, _at(cu), h0_at, y.data_ptr(), h_final.data_ptr(), saved.data_ptr(), q, e,
                                 _at(ws), ws.numel() if ws is not None else 0, _at(status), s)
     _done(st, status, "pdssm_gated_fwd")
@@ -851,7 +859,7 @@ def gated_bwd(x, ga, gi, rate, saved, dy, cu=None, h0=None, dh_final=None, check
     ws = _gated_ws(args, OP_BWD, dev)
     status = _status(check, dev)
     s = _on(stream, dev, (*([t for k in (x, ga, gi) for t in k] if eight else (x, ga, gi)), rate, saved, dy, cu, h0,
-                          dh_final, rows, drate, dh0, ws, status), status)
+                          dh_final, rows, drate, dh0, ws, status))
     st = load().pdssm_gated_bwd(*args.at[:4], rate_at, _at(cu), h0_at, saved_at, args.at[4], dhf_at, _three(grads), 3 * C,
                                 drate.data_ptr(), dh0.data_ptr(), _at(ws), ws.numel() if ws is not None else 0, _at(status), s)
     _done(st, status, "pdssm_gated_bwd")
@@ -886,7 +894,7 @@ def gated_step(x, ga, gi, rate, h, slots=None, out=None, y=None, check=True, str
         y = torch.empty(shape, dtype=x.dtype, device=dev)
         y_at = y.data_ptr()
     status = _status(check, dev)
-    s = _on(stream, dev, (x, ga, gi, rate, h, out, slots, y, status), status)
+    s = _on(stream, dev, (x, ga, gi, rate, h, out, slots, y, status))
     st = load().pdssm_gated_step(*args.at, rate_at, slots_at, h_at, out_at, y_at, _at(status), s)
     _done(st, status, "pdssm_gated_step")
     return h if out is None else out, y
@@ -947,6 +955,7 @@ def project_wgrad(dP, u8, stream=None):
     if math.prod(shape[:lead]) != T:
         raise ValueError("dP and u8 disagree on the number of rows")
     M = math.prod(shape[lead:])
+    _int32(M)
     n = load().pdssm_project_wgrad_workspace_size(T, M, Dm)
     if n == OP_SIZE_ERROR:
         raise PdssmError(ERR_UNSUPPORTED, "project_wgrad_workspace_size")

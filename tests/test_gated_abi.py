@@ -199,3 +199,12 @@ def test_weight_gradient(lib):
         assert lib.pdssm_project_wgrad(T, M, Dm, *good[:4], None, 64 * MB, None) == ERR_WORKSPACE
         assert lib.pdssm_project_wgrad(T, M, Dm, *good[:5], need - 1, None) == ERR_WORKSPACE
         assert lib.pdssm_project_wgrad(T, M, Dm, *good[:4], _at(5) + 64, 64 * MB, None) == ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("sizes", [((1 << 32) + 5, 4, 1), (4, (1 << 32) + 5, 1), (4, 4, (1 << 32) + 1)])
+def test_sizes_past_32_bits_are_not_cut(sizes):
+    """They would otherwise arrive in the library as their low 32 bits."""
+    with pytest.raises(pdssm.PdssmError, match="UNSUPPORTED"):
+        pdssm._Args(*sizes, 0)
+    with pytest.raises(pdssm.PdssmError, match="UNSUPPORTED"):
+        pdssm._kept((None, None), "u", *sizes[:2], None) if max(sizes[:2]) > 4 else pdssm._int32(*sizes)

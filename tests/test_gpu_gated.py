@@ -524,6 +524,21 @@ def test_on_another_stream():
     assert torch.equal(y, want[0]) and torch.equal(case.bwd(saved, stream=s)[0], outs[0][1])
 
 
+def test_another_stream_waits_for_the_current_one():
+    """The memory of the outputs may still be in use on the current stream."""
+    case = Case([0, 200], 64, seed=2)
+    case.fwd()
+    s, done = torch.cuda.Stream(), torch.cuda.Event()
+    a = torch.randn(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        b = a @ a
+    done.record()
+    case.fwd(check=False, stream=s)
+    s.synchronize()
+    assert done.query() and b.shape == a.shape
+
+
 def test_captured_and_replayed():
     """A graph of the whole set, replayed with new inputs and eager work in between."""
     case = Case([0, 130, 130, 1000], 80, T=1003, dtype=torch.bfloat16, seed=6)
