@@ -48,6 +48,12 @@ KERNEL_SOURCES = {
     "k_bwd_fused_real": ["pdssm_fused.hip", "pdssm_fused.h", "pdssm_device.h", "pdssm_io.h"],
     "k_ste_gemm": ["pdssm_ste.hip", "pdssm_internal.h", "pdssm_device.h", "pdssm_io.h"],
     "k_project_wide": ["pdssm_select.hip", "pdssm_select.h", "pdssm_project_rule.h", "pdssm_device.h", "pdssm_io.h"],
+    "k_gated_fwd": ["pdssm_gated.hip", "pdssm_gated.h", "pdssm_gated_math.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h"],
+    "k_gated_bwd": ["pdssm_gated.hip", "pdssm_gated.h", "pdssm_gated_math.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h"],
+    "k_gated_step": ["pdssm_gated.hip", "pdssm_gated.h", "pdssm_gated_math.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h"],
+    "k_pack8": ["pdssm_kept.hip", "pdssm_kept.h", "pdssm_rows.h", "pdssm_device.h"],
+    "k_unpack8": ["pdssm_kept.hip", "pdssm_kept.h", "pdssm_rows.h", "pdssm_device.h"],
+    "k_wgrad": ["pdssm_wgrad.hip", "pdssm_kept.h", "pdssm_rows.h", "pdssm_device.h"],
     "k_project_thin": ["pdssm_select.hip", "pdssm_select.h", "pdssm_project_rule.h", "pdssm_device.h", "pdssm_io.h"],
 }
 
