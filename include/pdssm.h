@@ -482,7 +482,7 @@ size_t pdssm_gated_workspace_size(const pdssm_gated_desc* desc, int op);
  *
  * In this call and the next, workgroups with different rows of a channel wait
  * for each other, in an order in which each waits only for such as have begun.
- * A wait ends after a second or more all the same: PDSSM_ERR_HIP in
+ * A wait that is not answered for seconds ends all the same: PDSSM_ERR_HIP in
  * *dev_status, and NaN in the rows that needed the answer.
  */
 int pdssm_gated_fwd(const pdssm_gated_desc* desc, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,

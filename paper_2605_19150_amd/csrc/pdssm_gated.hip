@@ -16,7 +16,7 @@
 // chunks of kGatedChunk rows without regard to where sequences begin (a row
 // that begins one drops what comes from its left), so packed sequences of any
 // lengths make equal pieces of work.  A workgroup has one chunk of 64 channels:
-// eight waves of 16 rows, a channel a lane.  A wave folds its rows into one
+// eight waves of 16 rows, a channel (or two, see Shape) a lane.  A wave folds its rows into one
 // step (A, B): h_out = A h_in + B; the wave steps are folded in LDS into the
 // chunk's; and the state that enters the chunk comes from the chunks before
 // it, whose workgroups publish their step as soon as they have it and the state
@@ -25,6 +25,14 @@
 //
 // Every fold goes in row order from left to right (the backward one from right
 // to left), whatever was known when: results do not depend on timing.
+//
+// Bound by memory, with the arithmetic close behind: six to nine hardware
+// exponentials, reciprocals and roots and about as many other operations as fit
+// under an entry's bytes.  At B16 L2048 C1024 bf16 the forward takes 56 us (270
+// MB, 4.8 TB/s; a large copy reaches 5.2), the backward 120 us with the kernels
+// around it (471 MB, 3.9 TB/s; vector units 77% busy); in fp32 both move 5 TB/s
+// and more.  Forward with the 8-bit form and backward from it, B8 L18000 C1024
+// bf16: 935 us (3.28 GB).
 #include "pdssm_gated.h"
 
 #include <type_traits>
@@ -96,9 +104,9 @@ __global__ __launch_bounds__(256) void k_gated_clear(void* ws, int NB, size_t n)
 // advances it.  Chunks are handed out in the order in which they depend on
 // each other (chunk_ticket), so the chunks waited for are running or done, the
 // first one waits for nobody, and every wait ends; a wait of kWaitLimit looks
-// (over a second) ends all the same, reports PDSSM_ERR_HIP and gives NaN.
+// (seconds) ends all the same, reports PDSSM_ERR_HIP and gives NaN.
 constexpr int kBatch = 4, kBatches = 16;  // with batches of 8 the forward at B16 L2048 C1024 bf16 takes 56.5 us, of 4 53.8, of 2 55.4
-constexpr int kWaitLimit = 1 << 20;
+constexpr int kWaitLimit = 1 << 22;
 constexpr int kErrWait = -4;  // PDSSM_ERR_HIP
 
 // Folds words d * kBatch .. of the n into h; known: h is a value; gap: an empty word.
@@ -412,7 +420,7 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
     const int cc = live ? c : a.C - 1;
 
     typename S::R x[ROWS], ga[ROWS], gi[ROWS];
-    const float rate2 = a.rate[cc] * kLog2e;
+    const float rate = a.rate[cc];
     const RowsOf<IO, 1> xs(a.x, a.T, a.C, row0, 0, cc), gas(a.ga, a.T, a.C, row0, 0, cc), gis(a.gi, a.T, a.C, row0, 0, cc);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
@@ -478,7 +486,7 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
             in = hold ? 0.f : in;
             xi = hold ? 0.f : xi;
         }
-        const Decay d = decay_of(r, rate2);
+        const Decay d = decay_of(r, rate);
         av[i] = d.a;
         bv[i] = __builtin_amdgcn_sqrtf(d.beta2) * in * xi;
         float h = B;
@@ -563,7 +571,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
     const bool live = c < a.C;
     const int cc = live ? c : a.C - V;
 
-    float scale[3][V], rate[V], rate2[V], h[V];
+    float scale[3][V], rate[V], h[V];
 #pragma unroll
     for (int n = 0; n < V; ++n) {
         scale[0][n] = scale[1][n] = scale[2][n] = 1.f;
@@ -574,7 +582,6 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
             scale[2][n] = kept_scale(a.gi.e[o]);
         }
         rate[n] = a.rate[cc + n];
-        rate2[n] = rate[n] * kLog2e;
         h[n] = a.saved[(size_t)k * a.C + cc + n];  // the state before the chunk
     }
     typename N::R xr[ROWS], gar[ROWS], gir[ROWS];
@@ -596,10 +603,10 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
     // gates, and the two folds: states from the left, gradients from the right.
     // hb: the row's input term, later the state before it; r = 0 where the state
     // is held (no other logit gives it).  a and beta are computed anew from r
-    // wherever they are needed: with them kept, the 16 rows would not leave room
-    // for a second workgroup on the CU, which is what hides this one's waits (203
-    // us with half the rows and all kept, one workgroup a CU, against 149 at B16
-    // L2048 C1024 bf16).
+    // wherever they are needed: kept, they would not leave room for a second
+    // workgroup on the CU, which is what hides this one's waits (half the rows,
+    // all kept, one workgroup a CU: 203 us, where this took 149 then, at B16 L2048
+    // C1024 bf16; all kept and spilled in part: 161 us, now 120).
     float r[ROWS][V], in[ROWS][V], hb[ROWS][V], A[V], B[V], G[V], Gend[V];
 #pragma unroll
     for (int n = 0; n < V; ++n) A[n] = 1.f, B[n] = G[n] = Gend[n] = 0.f;
@@ -619,7 +626,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
                 if (!rows.is(rows.used, i)) r[i][n] = 0.f;
                 before = rows.state(a.h0, i, a.C, cc + n, rows.is(rows.first, i), before);
             }
-            const Decay d = decay_of(r[i][n], rate2[n]);
+            const Decay d = decay_of(r[i][n], rate[n]);
             hb[i][n] = __builtin_amdgcn_sqrtf(d.beta2) * ix;
             B[n] = fmaf(d.a, before, hb[i][n]);
             A[n] *= d.a;
@@ -701,7 +708,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
             if (rare(rows.first_any, i)) h[n] = rows.state(a.h0, i, a.C, cc + n, rows.is(rows.first, i), h[n]);
             const float b = hb[i][n];
             hb[i][n] = h[n];
-            h[n] = fmaf(__builtin_amdgcn_exp2f(-rate2[n] * r[i][n]), h[n], b);
+            h[n] = fmaf(decay_of(r[i][n], rate[n]).a, h[n], b);
             asm volatile("" : "+v"(r[i][n]));  // what comes of these is computed again below, not kept
         }
         asm volatile("" : "+v"(xr[i]), "+v"(dyr[i]));
@@ -728,11 +735,11 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
         for (int n = 0; n < V; ++n) {
             if (rare(rows.last_any, i)) u[n] = rows.state(a.dhf, i, a.C, cc + n, rows.is(rows.last, i), u[n]);
             const float gr = S::get(dyr[i], n) + u[n], x = N::get(xr[i], n, scale[0][n]);
-            const Decay d = decay_of(r[i][n], rate2[n]);
+            const Decay d = decay_of(r[i][n], rate[n]);
             const float t = in[i][n] * __builtin_amdgcn_rsqf(d.beta2);  // i / beta
             float dx = gr * d.beta2 * t;
             u[n] = gr * d.a;
-            float w = rate[n] * r[i][n] * u[n] * fmaf(x * d.a, t, -hb[i][n]);
+            float w = d.s * u[n] * fmaf(x * d.a, t, -hb[i][n]);
             float dxx = dx * x;
             dxx = fmaf(-dxx, in[i][n], dxx);
             const bool hold = r[i][n] == 0.f;
@@ -856,7 +863,7 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
     for (int n = 0; n < V; ++n) {
         const float l = En::get(ga.v[n]);
         const bool hold = l <= kGateHold;
-        const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), rate.v[n] * kLog2e);
+        const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), rate.v[n]);
         const float in = hold ? 0.f : __builtin_amdgcn_sqrtf(d.beta2) * sigmoid_f(En::get(gi.v[n])) * En::get(x.v[n]);
         h.v[n] = fmaf(d.a, h.v[n], in);
         y.v[n] = En::put(h.v[n]);

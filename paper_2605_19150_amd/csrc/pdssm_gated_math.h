@@ -21,27 +21,33 @@ __device__ __forceinline__ float sigmoid_f(float v) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504088896340736f));
 }
 
-// a = e^(-s) and beta^2 = 1 - a^2 of one entry.  The latter needs care near
-// a = 1, where the difference keeps only its last bits (s is rate * r, often
-// 1e-3 and less): 1 - e^(-2s) = 2 e^(-s) sinh(s), and sinh's series converges
-// fast.  Up to s = 0.3 its first omitted term is 1.5e-7 of the sum; from there
-// on 1 - a^2 is off by 4e-7 of itself.  With v = s log2 e the powers of ln 2
-// sit in the coefficients.
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// a = e^(-s) and beta^2 = 1 - a^2 of one entry, s = rate * r.  Long memories
+// have s of 1e-3 and less, where two things need care: the difference 1 - a^2
+// keeps only its last bits, and the hardware's exponential is off by 6e-9 to
+// one side, which a recurrence adds up over the 1 / s rows that it remembers.
+// So up to s = 0.15 drop = 1 - a comes from a polynomial (4e-8 of it off, to
+// both sides), a = 1 - drop is the nearest number but for the rounding of drop,
+// and beta^2 = drop (1 + a) is off by 2e-7 of itself at most; from there on 1 - a
+// is exact to 3e-7.
 struct Decay {
-    float a;
+    float s, a;
     float beta2;   // 1 - a^2, beta squared
 };
 
-__device__ __forceinline__ Decay decay_of(float r, float rate2) {  // rate2 = rate * log2 e
+__device__ __forceinline__ Decay decay_of(float r, float rate) {
     Decay d;
-    const float v = rate2 * r, u = v * v;
-    d.a = __builtin_amdgcn_exp2f(-v);
-    // 2 ln2 (1 + (ln2 v)^2 / 6 + (ln2 v)^4 / 120)
-    const float p = fmaf(u, fmaf(u, 2.6667116e-3f, 0.11100822f), 1.3862944f);
-    d.beta2 = v < 0.43280851f ? d.a * v * p : fmaf(-d.a, d.a, 1.f);
+    d.s = rate * r;
+    const float e = __builtin_amdgcn_exp2f(d.s * -kLog2e);
+    const bool near = d.s < 0.15f;
+    float p = fmaf(d.s, -3.9347485e-2f, 0.16646752f);
+    p = fmaf(d.s, p, -0.49999511f);
+    p = fmaf(d.s, p, 1.f);
+    const float drop = near ? d.s * p : 1.f - e;
+    d.a = near ? 1.f - drop : e;
+    d.beta2 = fmaf(drop, d.a, drop);
     return d;
 }
-
-constexpr float kLog2e = 1.44269504088896340736f;
 
 }  // namespace pdssm
