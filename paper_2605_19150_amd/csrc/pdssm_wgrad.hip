@@ -65,11 +65,10 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
     const int wv = wave_id(), lane = lane_id();
     const int MT = (a.M + B - 1) / B, DT = (a.Dm + B - 1) / B, total = MT * DT;
     // consecutive workgroups go to the 8 XCDs in turn: each XCD takes a run of
-    // tiles that share their rows of dP
-    const int per = (total + 7) / 8;
-    const int z = blockIdx.y;
-    const int turnno = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || turnno >= total) return;
+    // the tiles of all shares, which have their rows of dP in common
+    const int jobs = total * Z, job = (blockIdx.x & 7) * ((jobs + 7) / 8) + (blockIdx.x >> 3);
+    if (job >= jobs) return;
+    const int z = job / total, turnno = job - z * total;
     // in turn, kGroup tiles along M before the next along Dm: a run of 32 is
     // then about square in bytes (a row of dP has twice those of u)
     const int gt = kGroup * DT, gr = turnno / gt, in = turnno - gr * gt, gm = min(kGroup, MT - gr * kGroup);
@@ -263,22 +262,34 @@ __global__ __launch_bounds__(256, B == 256 ? 1 : 2) void k_wgrad(WgradArgs a, in
     }
 }
 
-// dW = the shares' sums, in the order of the tokens.
+// dW = the shares' sums.  G threads take every Gth share of four entries, and
+// their sums are added in order.
+template <int G>
 __global__ __launch_bounds__(256) void k_wgrad_sum(const float* part, float* dW, size_t n, int Z) {
-    const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);  // n is a multiple of 128
-    if (i >= n) return;
-    float4 s = *reinterpret_cast<const float4*>(part + i);
+    constexpr int W = 256 / G;
+    __shared__ float4 sums[G][W];
+    const int g = threadIdx.x / W, l = threadIdx.x % W;
+    const size_t i = 4 * ((size_t)blockIdx.x * W + l);  // n is a multiple of 128
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4& v) { s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w); };
+    if (i < n) {
 #pragma unroll 4
-    for (int z = 1; z < Z; ++z) {
-        const float4 v = *reinterpret_cast<const float4*>(part + (size_t)z * n + i);
-        s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+        for (int z = g; z < Z; z += G) add(*reinterpret_cast<const float4*>(part + (size_t)z * n + i));
     }
+    sums[g][l] = s;
+    __syncthreads();
+    if (g != 0 || i >= n) return;
+#pragma unroll
+    for (int k = 1; k < G; ++k) add(sums[k][l]);
     *reinterpret_cast<float4*>(dW + i) = s;
 }
 
 // Tile and shares of the tokens.  The 256 tile needs half the LDS traffic of
-// the 128 one; it is taken where its tiles, or shares of at least 4 slices, fill the
-// 256 CUs.
+// the 128 one, which fills the 256 CUs with shorter shares and smaller sums of
+// them.  The larger is taken where a CU has 24 slices of it or more (T32768 M1024
+// Dm1024, 32: 88 us against 108; T8192 M2048 Dm1024, 16: 65 against 55; T1500 M8192
+// Dm1024, 12: 56 against 36), or its tiles fill the CUs without shares (T511
+// M8192 Dm2048: 28 against 31).
 struct WgradPlan {
     int B, Z;
 };
@@ -290,9 +301,13 @@ WgradPlan plan_of(int T, int M, int Dm) {
         if (z > (slices + least - 1) / least) z = (slices + least - 1) / least;
         return (int)(z < 1 ? 1 : z);
     };
-    const int z256 = shares(256, 256, 4);
-    if (tiles(256) * z256 >= 192) return {256, z256};
-    return {128, shares(128, 512, 1)};
+    // shares are whole pairs of slices (as in the kernel): no empty ones
+    auto even = [&](int z) {
+        const int share = ((slices + z - 1) / z + 1) & ~1;
+        return share ? (slices + share - 1) / share : 1;
+    };
+    if (tiles(256) >= 192 || tiles(256) * slices >= 24 * 256) return {256, even(shares(256, 256, 4))};
+    return {128, even(shares(128, 512, 1))};
 }
 
 template <int B>
@@ -301,7 +316,7 @@ hipError_t launch(const WgradArgs& a, int Z, float* out, hipStream_t s) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k_wgrad<B>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)Tile<B>::LDS);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_wgrad<B>, dim3(8 * ((total + 7) / 8), Z), dim3(256), Tile<B>::LDS, s, a, Z, out);
+    hipLaunchKernelGGL(k_wgrad<B>, dim3((unsigned)(8 * (((long long)total * Z + 7) / 8))), dim3(256), Tile<B>::LDS, s, a, Z, out);
     return hipGetLastError();
 }
 
@@ -318,7 +333,10 @@ hipError_t launch_wgrad(const WgradArgs& a, hipStream_t s) {
     hipError_t e = p.B == 256 ? launch<256>(a, p.Z, out, s) : launch<128>(a, p.Z, out, s);
     if (e != hipSuccess || p.Z == 1) return e;
     const size_t n = (size_t)a.M * a.Dm;
-    hipLaunchKernelGGL(k_wgrad_sum, dim3((n / 4 + 255) / 256), dim3(256), 0, s, out, a.dW, n, p.Z);
+    auto sum = [&](auto* f, int W) {
+        hipLaunchKernelGGL(f, dim3((unsigned)((n / 4 + W - 1) / W)), dim3(256), 0, s, out, a.dW, n, p.Z);
+    };
+    p.Z >= 8 ? sum(k_wgrad_sum<16>, 16) : sum(k_wgrad_sum<4>, 64);
     return hipGetLastError();
 }
 

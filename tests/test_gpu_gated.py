@@ -479,6 +479,12 @@ def test_weight_gradient(T, M, Dm):
     assert torch.equal(dW, pdssm.project_wgrad(dP, u8))
 
 
+@pytest.mark.parametrize("T,M,Dm", [(100, 3592, 3344), (98401, 264, 272), (131, 4096, 16)])
+def test_weight_gradient_of_many_tiles_and_many_tokens(T, M, Dm):
+    """Where the larger tile is taken, with and without shares of the tokens, and a single column of tiles."""
+    test_weight_gradient(T, M, Dm)
+
+
 def test_weight_gradient_of_values_that_are_not_finite():
     dP = torch.randn(70, 16).to(torch.bfloat16).to(DEV)
     u = torch.randn(70, 32).to(DEV)
