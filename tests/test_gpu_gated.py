@@ -661,3 +661,83 @@ def test_refused_tensors():
         pdssm.project_wgrad(torch.zeros(49, 16, dtype=torch.bfloat16, device=DEV), pdssm.pack8(torch.zeros(50, 16, device=DEV)))
     with pytest.raises(TypeError):
         pdssm.project_wgrad(torch.zeros(50, 16, device=DEV), pdssm.pack8(torch.zeros(50, 16, device=DEV)))
+
+
+def test_offsets_past_32_bits():
+    """Rows whose entries lie more than 2^31 from the first: the results of the last sequence by itself."""
+    C, T0 = 64, (1 << 25) + (1 << 17)
+    T, tail = T0 + 1000, slice(T0, None)
+    g = torch.Generator().manual_seed(21)
+    full, own = [], []
+    for _ in range(4):
+        t = torch.zeros(T, C, dtype=torch.bfloat16, device=DEV)
+        t[tail] = torch.randn(1000, C, generator=g).to(torch.bfloat16).to(DEV)
+        full.append(t)
+        own.append(t[tail].clone())
+    assert full[0].numel() > 1 << 31
+    rate = torch.full((C,), 0.05, device=DEV)
+    cu, one = (torch.tensor(v, dtype=torch.int32, device=DEV) for v in ([0, T0, T], [0, 1000]))
+    y, fin, saved, kept = pdssm.gated_fwd(*full[:3], rate, cu=cu, hold8=True)
+    y1, fin1, saved1, kept1 = pdssm.gated_fwd(*own[:3], rate, cu=one, hold8=True)
+    assert torch.equal(y[tail], y1) and torch.equal(fin[1:], fin1)
+    assert all(torch.equal(q[tail], q1) and torch.equal(e[T0 // 32:], e1) for (q, e), (q1, e1) in zip(kept, kept1))
+    for a, b in ((full[:3], own[:3]), (kept, kept1)):
+        got, want = pdssm.gated_bwd(*a, rate, saved, full[3], cu=cu), pdssm.gated_bwd(*b, rate, saved1, own[3], cu=one)
+        assert all(torch.equal(v[tail], w) for v, w in zip(got[:3], want[:3]))
+        del got
+    del kept, y
+    q, e = pdssm.pack8(full[0])
+    q1, e1 = pdssm.pack8(own[0])
+    assert torch.equal(q[tail], q1) and torch.equal(e[T0 // 32:], e1)
+    assert torch.equal(pdssm.unpack8((q, e), dtype=torch.bfloat16)[tail], pdssm.unpack8((q1, e1), dtype=torch.bfloat16))
+    u, p = _np(pdssm.unpack8((q1, e1))), _np(own[1])  # the other rows add zeros
+    _near("dW", _np(pdssm.project_wgrad(full[1], (q, e))), p.T @ u, np.abs(p).T @ np.abs(u), 1002)
+
+
+def test_a_pool_past_32_bits():
+    """A state more than 2^31 entries into the pool."""
+    C, S = 1024, (1 << 21) + 3
+    h = torch.zeros(S, C, device=DEV)
+    assert h.numel() > 1 << 31
+    g = torch.Generator().manual_seed(22)
+    x, ga, gi = (torch.randn(2, C, generator=g).to(DEV) for _ in range(3))
+    rate = torch.full((C,), 0.1, device=DEV)
+    own = torch.randn(2, C, generator=g).to(DEV)
+    h[[1, S - 1]] = own
+    _, y = pdssm.gated_step(x, ga, gi, rate, h, slots=torch.tensor([S - 1, 1], dtype=torch.int32, device=DEV))
+    want = own[[1, 0]].contiguous()
+    _, y1 = pdssm.gated_step(x, ga, gi, rate, want)
+    assert torch.equal(y, y1) and torch.equal(h[[S - 1, 1]], want)
+    assert not h[2:S - 1].any() and not h[0].any()
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with its own workspace, and two graphs replayed side by side."""
+    cases = [Case([0, 700, 701, 9000], 130, dtype=torch.bfloat16, seed=k) for k in (1, 2)]
+    want = []
+    for c in cases:
+        y, _, saved = c.fwd()
+        want.append((y, c.bwd(saved)))
+    streams, graphs, outs = [torch.cuda.Stream() for _ in cases], [], []
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                y, _, saved = c.fwd(check=False)
+                got.append((y, c.bwd(saved, check=False)))
+        torch.cuda.synchronize()
+        for (y, d), (y1, d1) in zip(got, want):
+            assert torch.equal(y, y1) and all(torch.equal(a, b) for a, b in zip(d, d1))
+    for c in cases:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            y, _, saved = c.fwd(check=False)
+            outs.append((y, c.bwd(saved, check=False)))
+    for _ in range(5):
+        for gr, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                gr.replay()
+        torch.cuda.synchronize()
+        for (y, d), (y1, d1) in zip(outs, want):
+            assert torch.equal(y, y1) and all(torch.equal(a, b) for a, b in zip(d, d1))
