@@ -821,7 +821,7 @@ int pdssm_compose_chunks(const pdssm_desc* d, const int32_t* idx, const int32_t*
 
 size_t pdssm_gated_workspace_size(const pdssm_gated_desc* d, int op) {
     if (check_gated(d) != PDSSM_OK || (op != PDSSM_OP_FWD && op != PDSSM_OP_BWD)) return (size_t)-1;
-    return pdssm::gated_workspace(d->T, d->C, d->S, op == PDSSM_OP_BWD);
+    return pdssm::gated_workspace(d->T, d->C, op == PDSSM_OP_BWD);
 }
 
 int pdssm_gated_fwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_rows* ga, const pdssm_rows* gi,
@@ -843,7 +843,7 @@ int pdssm_gated_fwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_
         for (int i = 0; i < 3; ++i)
             if (!q[i] || !e[i]) return PDSSM_ERR_INVALID_ARG;
     const bool keep = q && T > 0;
-    const size_t need = pdssm::gated_workspace(T, C, d->S, false);
+    const size_t need = pdssm::gated_workspace(T, C, false);
     if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
     if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
     if (any_overlap({{y, n * w}, {h_final, ns}, {saved, nc}, {ws, need}, {keep ? q[0] : nullptr, n},
@@ -898,7 +898,7 @@ int pdssm_gated_bwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_
     for (const void* p : {(const void*)rate, (const void*)h0, (const void*)saved, (const void*)dh_final, (const void*)drate,
                           (const void*)dh0, (const void*)dev_status})
         if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
-    const size_t need = pdssm::gated_workspace(T, C, d->S, true);
+    const size_t need = pdssm::gated_workspace(T, C, true);
     if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
     if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
     // the three gradients may be parts of one tensor of wider rows: then they

@@ -37,7 +37,7 @@ struct GatedArgs {
 };
 
 // Workspace bytes of a forward (bwd = false) or backward pass.
-size_t gated_workspace(int T, int C, int S, bool bwd);
+size_t gated_workspace(int T, int C, bool bwd);
 
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t s);
 hipError_t launch_gated_bwd(const GatedArgs& a, hipStream_t s);

@@ -29,13 +29,11 @@
 // Bound by memory, with the arithmetic close behind: six to nine hardware
 // exponentials, reciprocals and roots and about as many other operations as fit
 // under an entry's bytes.  At B16 L2048 C1024 bf16 the forward takes 56 us (270
-// MB, 4.8 TB/s; a large copy reaches 5.2), the backward 120 us with the kernels
-// around it (471 MB, 3.9 TB/s; vector units 77% busy); in fp32 both move 5 TB/s
-// and more.  Forward with the 8-bit form and backward from it, B8 L18000 C1024
-// bf16: 935 us (3.28 GB).
+// MB, 4.8 TB/s; a large copy reaches 5.2), the backward 122 us with the kernels
+// around it (471 MB, 3.9 TB/s), the vector units 69% and 67% busy; in fp32 both
+// move 5 TB/s and more.  Forward with the 8-bit form and backward from it, B8
+// L18000 C1024 bf16: 925 us (3.28 GB), the vector units 80% busy.
 #include "pdssm_gated.h"
-
-#include <type_traits>
 
 #include "pdssm_device.h"
 #include "pdssm_gated_math.h"
@@ -874,7 +872,7 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
 
 }  // namespace
 
-size_t gated_workspace(int T, int C, int S, bool bwd) {
+size_t gated_workspace(int T, int C, bool bwd) {
     if (chunks_of(T) <= 1) return 0;
     return blocks_of(C) * kTicketStride + words_of(T, C) * 8 + (bwd ? (size_t)chunks_of(T) * C * 4 : 0);
 }

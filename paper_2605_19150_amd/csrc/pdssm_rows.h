@@ -43,17 +43,13 @@ struct Entry;
 template <>
 struct Entry<kRowF32> {
     using T = float;  // in memory
-    using R = float;  // in a register
-    static __device__ __forceinline__ float get(R v, float = 1.f) { return v; }
-    static __device__ __forceinline__ float gate(R v, float) { return v; }
+    static __device__ __forceinline__ float get(T v) { return v; }
     static __device__ __forceinline__ T put(float v) { return v; }
 };
 template <>
 struct Entry<kRowBf16> {
     using T = uint16_t;
-    using R = uint32_t;
-    static __device__ __forceinline__ float get(R v, float = 1.f) { return __uint_as_float(v << 16); }
-    static __device__ __forceinline__ float gate(R v, float) { return get(v); }
+    static __device__ __forceinline__ float get(uint32_t v) { return __uint_as_float(v << 16); }
     // to nearest, ties to even: off by at most 2^-8 of the value, the one
     // rounding of an output
     static __device__ __forceinline__ T put(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
@@ -62,10 +58,8 @@ struct Entry<kRowBf16> {
 template <>
 struct Entry<kRowKept> {
     using T = int8_t;
-    using R = int;
-    static __device__ __forceinline__ float get(R v, float scale) { return (float)v * scale; }
-    // a gate logit, with the code of a held one
-    static __device__ __forceinline__ float gate(R v, float scale) { return v == kKeptLow ? -INFINITY : (float)v * scale; }
+    // with the code of a held gate logit
+    static __device__ __forceinline__ float get(int v, float scale) { return v == kKeptLow ? -INFINITY : (float)v * scale; }
 };
 
 }  // namespace pdssm
