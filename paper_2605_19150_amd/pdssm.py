@@ -29,6 +29,7 @@ import ctypes
 import functools
 import math
 import os
+import struct
 
 import torch
 
@@ -682,8 +683,7 @@ def _tensor(t, name, dtype, shape, dev):
 
 
 def _rows(t, name, dtype, shape, dev):
-    """(address, entries from row to row, no exponents) of rows [T,C] or [B,L,C]
-    that may be a part of wider rows."""
+    """pdssm_rows of rows [T,C] or [B,L,C] that may be a part of wider rows."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if t.dtype is not dtype:
@@ -708,15 +708,21 @@ def _rows(t, name, dtype, shape, dev):
         ld = step[0]
     if ld < C:
         raise ValueError("%s: rows must not overlap" % name)
-    return t.data_ptr(), ld, None
+    return _ROW.pack(t.data_ptr(), ld, 0)
 
 
 def _kept(pair, name, T, C, dev):
-    """(address, entries from row to row, address of the exponents) of a pair (q, e) in the 8-bit form."""
+    """(address of the codes, address of the exponents) of a pair (q, e) in the 8-bit form."""
     q, e = pair
     _int32(T, C)
-    return (_tensor(q, name + " codes", torch.int8, (T, C), dev), C,
+    return (_tensor(q, name + " codes", torch.int8, (T, C), dev),
             _tensor(e, name + " exponents", torch.int8, (_ceil(T, KEPT_ROWS), C), dev))
+
+
+def _kept_rows(pair, name, T, C, dev):
+    """pdssm_rows of a pair."""
+    q_at, e_at = _kept(pair, name, T, C, dev)
+    return _ROW.pack(q_at, C, e_at)
 
 
 def _int32(*sizes):
@@ -725,16 +731,14 @@ def _int32(*sizes):
         raise PdssmError(ERR_UNSUPPORTED, "sizes %s" % (sizes,))
 
 
-class _Args:
-    """A descriptor and up to four row tensors in memory that the library reads during the call."""
+# pdssm_gated_desc and pdssm_rows as bytes, which the library reads during the
+# call; ctypes structures take seven times as long to make
+_DESC, _ROW = struct.Struct("iiiI"), struct.Struct("PqP")
 
-    def __init__(self, T, C, S, flags, *rows):
-        _int32(T, C, S)
-        self.d = GatedDesc(T, C, S, flags)
-        self.rows = (Rows * len(rows))(*rows)
-        self.at = [ctypes.addressof(self.d)]
-        base = ctypes.addressof(self.rows)
-        self.at += [base + i * ctypes.sizeof(Rows) for i in range(len(rows))]
+
+def _desc(T, C, S, flags):
+    _int32(T, C, S)
+    return _DESC.pack(T, C, S, flags)
 
 
 def _row_type(t):
@@ -767,8 +771,8 @@ def _sequences(t, cu):
     return T, C, S
 
 
-def _gated_ws(args, op, dev):
-    n = load().pdssm_gated_workspace_size(args.at[0], op)
+def _gated_ws(desc, op, dev):
+    n = load().pdssm_gated_workspace_size(desc, op)
     if n == OP_SIZE_ERROR:
         raise PdssmError(ERR_UNSUPPORTED, "gated_workspace_size")
     return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
@@ -812,22 +816,23 @@ def gated_fwd(x, ga, gi, rate, cu=None, h0=None, hold8=False, check=True, stream
     flags = _row_type(x)
     T, C, S = _sequences(x, cu)
     dev, shape = x.device, x.shape
-    args = _Args(T, C, S, flags, *[_rows(t, n, x.dtype, shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))])
+    d = _desc(T, C, S, flags)
+    rows = [_rows(t, n, x.dtype, shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
     rate_at = _tensor(rate, "rate", torch.float32, (C,), dev)
     h0_at = _state(h0, "h0", S, C, dev)
-    y = torch.empty(shape, dtype=x.dtype, device=dev)
-    h_final = torch.empty((S, C), dtype=torch.float32, device=dev)
-    saved = torch.empty((_ceil(T, GATED_CHUNK), C), dtype=torch.float32, device=dev)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    h_final = rate.new_empty((S, C))
+    saved = rate.new_empty((_ceil(T, GATED_CHUNK), C))
     kept = q = e = None
     if hold8:
         kept = tuple((torch.empty((T, C), dtype=torch.int8, device=dev),
                       torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)) for _ in range(3))
         q, e = _three([k[0] for k in kept]), _three([k[1] for k in kept])
-    ws = _gated_ws(args, OP_FWD, dev)
+    ws = _gated_ws(d, OP_FWD, dev)
     status = _status(check, dev)
     s = _on(stream, dev, (x, ga, gi, rate, cu, h0, y, h_final, saved, ws, status,
                           *([t for k in kept for t in k] if hold8 else ())))
-    st = load().pdssm_gated_fwd(*args.at, rate_at, _at(cu), h0_at, y.data_ptr(), h_final.data_ptr(), saved.data_ptr(), q, e,
+    st = load().pdssm_gated_fwd(d, *rows, rate_at, _at(cu), h0_at, y.data_ptr(), h_final.data_ptr(), saved.data_ptr(), q, e,
                                 _at(ws), ws.numel() if ws is not None else 0, _at(status), s)
     _done(st, status, "pdssm_gated_fwd")
     return (y, h_final, saved, kept) if hold8 else (y, h_final, saved)
@@ -847,20 +852,21 @@ def gated_bwd(x, ga, gi, rate, saved, dy, cu=None, h0=None, dh_final=None, check
     eight = isinstance(x, (tuple, list))
     if any(isinstance(t, (tuple, list)) != eight for t, _ in ins):
         raise TypeError("x, ga and gi must be all rows or all pairs (q, e)")
-    r = [_kept(t, n, T, C, dev) if eight else _rows(t, n, dy.dtype, shape, dev) for t, n in ins]
-    args = _Args(T, C, S, flags, *r, _rows(dy, "dy", dy.dtype, shape, dev))
+    d = _desc(T, C, S, flags)
+    r = [_kept_rows(t, n, T, C, dev) if eight else _rows(t, n, dy.dtype, shape, dev) for t, n in ins]
+    dy_rows = _rows(dy, "dy", dy.dtype, shape, dev)
     rate_at = _tensor(rate, "rate", torch.float32, (C,), dev)
     saved_at = _tensor(saved, "saved", torch.float32, (_ceil(T, GATED_CHUNK), C), dev)
     h0_at, dhf_at = _state(h0, "h0", S, C, dev), _state(dh_final, "dh_final", S, C, dev)
-    rows = torch.empty((*shape[:-1], 3 * C), dtype=dy.dtype, device=dev)
+    rows = dy.new_empty((*shape[:-1], 3 * C))
     grads = rows.split(C, -1)
-    drate = torch.empty(C, dtype=torch.float32, device=dev)
-    dh0 = torch.empty((S, C), dtype=torch.float32, device=dev)
-    ws = _gated_ws(args, OP_BWD, dev)
+    drate = torch.empty_like(rate)
+    dh0 = rate.new_empty((S, C))
+    ws = _gated_ws(d, OP_BWD, dev)
     status = _status(check, dev)
     s = _on(stream, dev, (*([t for k in (x, ga, gi) for t in k] if eight else (x, ga, gi)), rate, saved, dy, cu, h0,
                           dh_final, rows, drate, dh0, ws, status))
-    st = load().pdssm_gated_bwd(*args.at[:4], rate_at, _at(cu), h0_at, saved_at, args.at[4], dhf_at, _three(grads), 3 * C,
+    st = load().pdssm_gated_bwd(d, *r, rate_at, _at(cu), h0_at, saved_at, dy_rows, dhf_at, _three(grads), 3 * C,
                                 drate.data_ptr(), dh0.data_ptr(), _at(ws), ws.numel() if ws is not None else 0, _at(status), s)
     _done(st, status, "pdssm_gated_bwd")
     return (*grads, drate, dh0)
@@ -883,19 +889,19 @@ def gated_step(x, ga, gi, rate, h, slots=None, out=None, y=None, check=True, str
     if not isinstance(h, torch.Tensor) or h.dim() != 2:
         raise ValueError("h must be [S,C]")
     S = h.shape[0]
-    args = _Args(B, C, S, flags, _rows(x, "x", x.dtype, shape, dev), _rows(ga, "ga", x.dtype, shape, dev),
-                 _rows(gi, "gi", x.dtype, shape, dev))
+    d = _desc(B, C, S, flags)
+    rows = [_rows(t, n, x.dtype, shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
     rate_at = _tensor(rate, "rate", torch.float32, (C,), dev)
     h_at = _tensor(h, "h", torch.float32, (S, C), dev)
     out_at = h_at if out is None else _tensor(out, "out", torch.float32, (S, C), dev)
     slots_at = None if slots is None else _tensor(slots, "slots", torch.int32, (B,), dev)
     y_at = None if y is None else _tensor(y, "y", x.dtype, shape, dev)
     if y is None:
-        y = torch.empty(shape, dtype=x.dtype, device=dev)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
         y_at = y.data_ptr()
     status = _status(check, dev)
     s = _on(stream, dev, (x, ga, gi, rate, h, out, slots, y, status))
-    st = load().pdssm_gated_step(*args.at, rate_at, slots_at, h_at, out_at, y_at, _at(status), s)
+    st = load().pdssm_gated_step(d, *rows, rate_at, slots_at, h_at, out_at, y_at, _at(status), s)
     _done(st, status, "pdssm_gated_step")
     return h if out is None else out, y
 
@@ -909,11 +915,12 @@ def pack8(u, stream=None):
         raise ValueError("u must be [T,C] or [B,L,C]")
     C, dev = u.shape[-1], u.device
     T = u.shape[0] if u.dim() == 2 else u.shape[0] * u.shape[1]
-    args = _Args(T, C, 1, flags, _rows(u, "u", u.dtype, u.shape, dev))
+    _int32(T, C)
+    rows = _rows(u, "u", u.dtype, u.shape, dev)
     q = torch.empty((T, C), dtype=torch.int8, device=dev)
     e = torch.empty((_ceil(T, KEPT_ROWS), C), dtype=torch.int8, device=dev)
     s = _on(stream, dev, (u, q, e))
-    _done(load().pdssm_pack8(T, C, flags, args.at[1], q.data_ptr(), e.data_ptr(), s), None, "pdssm_pack8")
+    _done(load().pdssm_pack8(T, C, flags, rows, q.data_ptr(), e.data_ptr(), s), None, "pdssm_pack8")
     return q, e
 
 
@@ -927,8 +934,8 @@ def unpack8(pair, dtype=torch.float32, stream=None):
         raise ValueError("q must be [T,C]")
     T, C = q.shape
     dev = q.device
-    q_at, _, e_at = _kept(pair, "u", T, C, dev)
-    out = torch.empty((T, C), dtype=dtype, device=dev)
+    q_at, e_at = _kept(pair, "u", T, C, dev)
+    out = torch.empty_like(q, dtype=dtype)
     s = _on(stream, dev, (q, e, out))
     _done(load().pdssm_unpack8(T, C, FLAG_BF16_IO if dtype is torch.bfloat16 else 0, q_at, e_at, out.data_ptr(), s), None,
           "pdssm_unpack8")
@@ -946,7 +953,7 @@ def project_wgrad(dP, u8, stream=None):
         raise ValueError("u8 must be a pair (q, e) with q [T,Dm]")
     T, Dm = q.shape
     dev = q.device
-    q_at, _, e_at = _kept(u8, "u", T, Dm, dev)
+    q_at, e_at = _kept(u8, "u", T, Dm, dev)
     if not isinstance(dP, torch.Tensor) or dP.dim() < 2:
         raise ValueError("dP must be rows [T,M] or [B,L,...]")
     shape = dP.shape

@@ -205,6 +205,6 @@ def test_weight_gradient(lib):
 def test_sizes_past_32_bits_are_not_cut(sizes):
     """They would otherwise arrive in the library as their low 32 bits."""
     with pytest.raises(pdssm.PdssmError, match="UNSUPPORTED"):
-        pdssm._Args(*sizes, 0)
+        pdssm._desc(*sizes, 0)
     with pytest.raises(pdssm.PdssmError, match="UNSUPPORTED"):
         pdssm._kept((None, None), "u", *sizes[:2], None) if max(sizes[:2]) > 4 else pdssm._int32(*sizes)
