@@ -740,7 +740,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
             float w = d.s * u[n] * fmaf(x * d.a, t, -hb[i][n]);
             float dxx = dx * x;
             dxx = fmaf(-dxx, in[i][n], dxx);
-            const bool hold = r[i][n] == 0.f;
+            const bool hold = d.beta2 < 1.17549435e-38f;  // r = 0; roots know no smaller numbers either
             d0[n] = hold ? 0.f : dx;
             w = hold ? 0.f : w;
             d2[n] = hold ? 0.f : dxx;

@@ -12,7 +12,8 @@ namespace pdssm {
 // A gate logit at or under this one holds the state: a = 1, no input and no
 // gradient, whatever the other rows hold (padding: the type's lowest value or
 // -inf).  sigmoid(-64) is 1.6e-28, so s = rate * r stays a normal number for
-// every gate that is not held.
+// every gate that is not held and every rate from 1e-10 on; where it does not,
+// a = 1 and beta = 0, and the gradients are those of a held row.
 constexpr float kGateHold = -64.f;
 
 __device__ __forceinline__ float sigmoid_f(float v) {

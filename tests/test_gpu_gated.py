@@ -425,6 +425,27 @@ def test_one_token_refused_and_skipped_rows():
     assert torch.equal(h[2], alone[2])  # the first of the two rows that named slot 2
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_rates_that_hardly_move(dtype):
+    """s = rate * r from 1 down to 1e-50: below the smallest normal number a row counts as held, and nothing is NaN."""
+    case = Case([0, 300], 64, dtype=dtype, wide=False, seed=12)
+    case.rate = 10.0 ** torch.linspace(0, -22, 64).to(DEV)
+    case.ga[::3] = -60.0
+    y, fin, saved = case.fwd()
+    h, size = _check_fwd(case, y, fin)
+    got = case.bwd(saved)
+    dx, dga, dgi, drate, dh0 = map(_np, got)
+    for t in (dx, dga, dgi, drate, dh0):
+        assert np.isfinite(t).all()
+    args, h0 = case.ref()
+    want = G.gated_bwd(*args, case.bounds, G.states_before(h, case.bounds, h0), _np(case.dy), _np(case.dhf))
+    # a row that counts as held has beta < 1.1e-19: its gradients are that small
+    g = np.abs(_np(case.dy)).sum(0) + np.abs(_np(case.dhf))[0]
+    for name, t in (("dx", dx), ("dgi", dgi)):
+        assert (np.abs(t - want[name]) <= (2.0 ** -8 if dtype == torch.bfloat16 else 0) * np.abs(want[name]) +
+                4 * (300 + 16) * U * g * (1 + np.abs(_np(case.x))) + 1.1e-19 * g).all()
+
+
 def test_steps_equal_the_sequence():
     """Prefill, then token by token: the states and outputs of one long run."""
     case = Case([0, 200], 70, seed=4)
