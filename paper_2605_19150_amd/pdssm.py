@@ -27,6 +27,7 @@ Gated recurrent layers (gated_fwd and the functions after it) take rows:
 """
 import ctypes
 import functools
+import inspect
 import math
 import os
 import struct
@@ -642,15 +643,19 @@ def _ceil(n, k):
 
 
 def _on_its_device(f):
-    """f with the device of its first tensor as the current one, which is where
-    its kernels are launched."""
+    """f with the device of its first argument, by place or by name, as the
+    current one, which is where its kernels are launched."""
+    name = next(iter(inspect.signature(f).parameters))
+
     @functools.wraps(f)
-    def on(first, *args, **kw):
-        t = first[0] if isinstance(first, (tuple, list)) and first else first
+    def on(*args, **kw):
+        t = args[0] if args else kw.get(name)
+        if isinstance(t, (tuple, list)) and t:
+            t = t[0]
         if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != torch.cuda.current_device():
             with torch.cuda.device(t.device):
-                return f(first, *args, **kw)
-        return f(first, *args, **kw)
+                return f(*args, **kw)
+        return f(*args, **kw)
     return on
 
 

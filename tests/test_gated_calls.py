@@ -1,0 +1,30 @@
+"""How the binding of the gated operators is called (no GPU): what it checks
+before it reaches the library."""
+import inspect
+
+import pytest
+import torch
+
+from paper_2605_19150_amd import pdssm
+
+FUNCTIONS = [pdssm.gated_fwd, pdssm.gated_bwd, pdssm.gated_step, pdssm.pack8, pdssm.unpack8, pdssm.project_wgrad]
+
+
+@pytest.mark.parametrize("f", FUNCTIONS, ids=lambda f: f.__name__)
+def test_every_argument_by_its_name(f):
+    """Both forms of a call end at the same check: these tensors are not on a GPU."""
+    rows, pair = torch.zeros(1, 4, 16), (torch.zeros(4, 16, dtype=torch.int8), torch.zeros(1, 16, dtype=torch.int8))
+    special = dict(rate=torch.zeros(16), saved=torch.zeros(1, 16), h=torch.zeros(4, 16), pair=pair, u8=pair,
+                   dP=torch.zeros(4, 8, dtype=torch.bfloat16))
+    names = [p.name for p in inspect.signature(f).parameters.values() if p.default is p.empty]
+    kw = {n: special.get(n, rows[0] if f is pdssm.gated_step else rows) for n in names}
+    with pytest.raises(ValueError, match="must be on") as by_place:
+        f(*kw.values())
+    with pytest.raises(ValueError, match="must be on") as by_name:
+        f(**kw)
+    assert str(by_place.value) == str(by_name.value)
+
+
+def test_a_call_without_arguments_names_them():
+    with pytest.raises(TypeError, match="'u'"):
+        pdssm.pack8()
