@@ -668,9 +668,14 @@ def _on(stream, dev, tensors):
     """The stream to launch on, as a number.  One of the caller's own that is not
     the current one waits for it (the memory of the outputs may still be in use
     there, by work of whoever had it before), and learns of every tensor of the
-    call, so that none is given to other work before it has run."""
+    call, so that none is given to other work before it has run.  A stream of
+    another device is refused."""
     current = _raw_stream(dev.index)
-    if stream is None or stream.cuda_stream == current:
+    if stream is None:
+        return current
+    if stream.device != dev:
+        raise ValueError("stream must be one of %s" % dev)
+    if stream.cuda_stream == current:
         return current
     stream.wait_stream(torch.cuda.current_stream(dev))
     for t in tensors:

@@ -28,3 +28,26 @@ def test_every_argument_by_its_name(f):
 def test_a_call_without_arguments_names_them():
     with pytest.raises(TypeError, match="'u'"):
         pdssm.pack8()
+
+
+class _Stream:
+    """As much of a torch.cuda.Stream as the binding looks at."""
+
+    def __init__(self, device, cuda_stream):
+        self.device, self.cuda_stream = torch.device(device), cuda_stream
+
+    def wait_stream(self, other):
+        self.waited = other
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    """A kernel launched there would run on that device, on memory of this one."""
+    monkeypatch.setattr(pdssm, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: "current")
+    dev = torch.device("cuda", 0)
+    for raw in (0, 4096):  # the default stream of every device has the number 0
+        with pytest.raises(ValueError, match="stream"):
+            pdssm._on(_Stream("cuda:1", raw), dev, ())
+    own = _Stream("cuda:0", 4096)
+    assert pdssm._on(own, dev, ()) == 4096 and own.waited == "current"
+    assert pdssm._on(_Stream("cuda:0", 0), dev, ()) == 0 and pdssm._on(None, dev, ()) == 0
