@@ -438,8 +438,9 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
  * lowest value) holds the state: a = 1, no input whatever x and gi are (inf
  * and NaN too), and zero gradients of that row.
  *
- * rate [C] must be positive and finite (other values give NaN, in that
- * channel only).  A row with rate * r below 6e-39 counts as held.
+ * rate [C] must be positive and finite: any other value (0, infinity, NaN)
+ * gives NaN in that channel's rows, held ones too, in the states and gradients
+ * behind them and in drate, and in no other channel.  A row with rate * r below 6e-39 counts as held.
  *
  * The 8-bit form of rows [T, C]: whole numbers q [T, C] int8 and exponents
  * e [ceil(T/32), C] int8, value q[t,c] * 2^e[t/32,c], with the smallest

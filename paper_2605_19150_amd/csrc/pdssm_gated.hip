@@ -418,7 +418,7 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
     const int cc = live ? c : a.C - 1;
 
     typename S::R x[ROWS], ga[ROWS], gi[ROWS];
-    const float rate = a.rate[cc];
+    const float rate_in = a.rate[cc];
     const RowsOf<IO, 1> xs(a.x, a.T, a.C, row0, 0, cc), gas(a.ga, a.T, a.C, row0, 0, cc), gis(a.gi, a.T, a.C, row0, 0, cc);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
@@ -429,6 +429,7 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
     }
     const RowKinds kinds = row_kinds(a, row0);
     const LaneRows<1> rows(kinds, 0);
+    const float rate = rate_of(rate_in);  // looked at behind the rows' loads: it would hold them up
     if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.h0, a.h_final, c, cb == 0);
 
     if constexpr (KEEP) {
@@ -596,6 +597,8 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
     }
     const RowKinds kinds = row_kinds(a, row0);
     const LaneRows<V> rows(kinds, g);
+#pragma unroll
+    for (int n = 0; n < V; ++n) rate[n] = rate_of(rate[n]);
     if (k == 0 && wv == kWaves - 1) empty_sequences(a, a.dhf, a.dh0, cb * 64 + lane, cb == 0);
 
     // gates, and the two folds: states from the left, gradients from the right.
@@ -777,7 +780,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
 #pragma unroll
         for (int w = 0; w < kWaves * V; ++w) all += sums[w][lane];
         if (NC > 1) part[(size_t)k * a.C + ch] = all;
-        else a.drate[ch] = all / a.rate[ch];
+        else a.drate[ch] = all / rate_of(a.rate[ch]);
     }
 }
 
@@ -799,7 +802,7 @@ __global__ __launch_bounds__(1024) void k_gated_rate(const float* part, const fl
     s = 0.f;
 #pragma unroll
     for (int w = 0; w < 16; ++w) s += sums[w][ch];
-    drate[c] = s / rate[c];
+    drate[c] = s / rate_of(rate[c]);
 }
 
 // No rows at all: out = in for every sequence, and a zero rate gradient.
@@ -861,7 +864,7 @@ __global__ __launch_bounds__(256) void k_gated_step(GatedStepArgs a) {
     for (int n = 0; n < V; ++n) {
         const float l = En::get(ga.v[n]);
         const bool hold = l <= kGateHold;
-        const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), rate.v[n]);
+        const Decay d = decay_of(hold ? 0.f : sigmoid_f(l), rate_of(rate.v[n]));
         const float in = hold ? 0.f : __builtin_amdgcn_sqrtf(d.beta2) * sigmoid_f(En::get(gi.v[n])) * En::get(x.v[n]);
         h.v[n] = fmaf(d.a, h.v[n], in);
         y.v[n] = En::put(h.v[n]);

@@ -24,6 +24,14 @@ __device__ __forceinline__ float sigmoid_f(float v) {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// A channel's rate.  One that is not positive and finite is no rate of this
+// recurrence: as a NaN it makes s, a and beta of every row NaN, also where r is
+// 0.  (Left as it is, 0 would hold the state, infinity give y = i x, and a
+// negative one a beta^2 below 0, which the backward pass takes for a held row.)
+__device__ __forceinline__ float rate_of(float rate) {
+    return rate > 0.f && rate < INFINITY ? rate : __uint_as_float(0x7fc00000u);
+}
+
 // a = e^(-s) and beta^2 = 1 - a^2 of one entry, s = rate * r.  Long memories
 // have s of 1e-3 and less, where two things need care: the difference 1 - a^2
 // keeps only its last bits, and the hardware's exponential is off by 6e-9 to
