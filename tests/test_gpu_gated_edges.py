@@ -53,3 +53,96 @@ def test_rates_that_are_not_positive_and_finite(bounds, dtype, C):
     _, y1 = pdssm.gated_step(case.x, case.ga, case.gi, good, h0)
     for v, v0 in ((h, h0), (ys, y1)):
         assert torch.isnan(v[:, bad]).all() and torch.equal(v[:, rest], v0[:, rest])
+
+
+# ---- very many sequences ---------------------------------------------------
+
+def test_very_many_sequences():
+    """2^17 sequences, most without rows, between long ones: their states, a bound out of order among the last, and
+    no more time than their share of the memory takes."""
+    T, S, C = 1 << 17, 1 << 17, 64
+    g = torch.Generator().manual_seed(31)
+    x, ga, gi, dy = (torch.randn(T, C, generator=g).to(torch.bfloat16).to(DEV) for _ in range(4))
+    rate = torch.full((C,), 0.05, device=DEV)
+    cuts = sorted(np.random.default_rng(31).choice(S, 40, replace=False).tolist())  # sequences that have rows
+    n = np.zeros(S, np.int64)
+    n[cuts] = T // 40
+    cu = torch.from_numpy(np.concatenate([[0], np.cumsum(n)]).astype(np.int32)).to(DEV)
+    few = torch.tensor([0, *(T // 40 * (k + 1) for k in range(40))], dtype=torch.int32, device=DEV)
+    h0, dhf = (torch.randn(S, C, generator=g).to(DEV) for _ in range(2))
+    at = torch.tensor(cuts, device=DEV)
+    rest = torch.ones(S, dtype=torch.bool, device=DEV)
+    rest[at] = False
+    few0, fewf = h0[at].contiguous(), dhf[at].contiguous()
+
+    y, fin, saved = pdssm.gated_fwd(x, ga, gi, rate, cu=cu, h0=h0)
+    y1, fin1, saved1 = pdssm.gated_fwd(x, ga, gi, rate, cu=few, h0=few0)
+    end = T // 40 * 40
+    assert torch.equal(y[:end], y1[:end]) and torch.equal(fin[at], fin1) and torch.equal(fin[rest], h0[rest])
+    d = pdssm.gated_bwd(x, ga, gi, rate, saved, dy, cu=cu, h0=h0, dh_final=dhf)
+    d1 = pdssm.gated_bwd(x, ga, gi, rate, saved1, dy, cu=few, h0=few0, dh_final=fewf)
+    assert all(torch.equal(a[:end], b[:end]) for a, b in zip(d[:3], d1[:3])) and torch.equal(d[3], d1[3])
+    assert torch.equal(d[4][at], d1[4]) and torch.equal(d[4][rest], dhf[rest])
+    for place in (S - 1, S, S // 2 + 17):
+        bad = cu.clone()
+        bad[place] = T + 1
+        with pytest.raises(pdssm.PdssmError, match="INDEX"):
+            pdssm.gated_fwd(x, ga, gi, rate, cu=bad, h0=h0)
+        with pytest.raises(pdssm.PdssmError, match="INDEX"):
+            pdssm.gated_bwd(x, ga, gi, rate, saved, dy, cu=bad, h0=h0, dh_final=dhf)
+
+    def took(f):
+        best = math.inf
+        for _ in range(6):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            f()
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    def fwd(cu, h0):
+        return took(lambda: pdssm.gated_fwd(x, ga, gi, rate, cu=cu, h0=h0, check=False))
+
+    def bwd(cu, h0, dhf, saved):
+        return took(lambda: pdssm.gated_bwd(x, ga, gi, rate, saved, dy, cu=cu, h0=h0, dh_final=dhf, check=False))
+
+    # 2^17 states of 64 channels are 32 MB to read and as many to write, about as much as the rows; by one wave they took
+    # a hundred times as long
+    times = fwd(cu, h0), fwd(few, few0), bwd(cu, h0, dhf, saved), bwd(few, few0, fewf, saved1)
+    print("forward %.3f (few sequences: %.3f), backward %.3f (%.3f) ms" % times)
+    assert times[0] < 10 * times[1] and times[2] < 10 * times[3]
+
+
+@pytest.mark.parametrize("T,S", [(0, 3000), (5, 1000), (128, 700), (129, 513), (3000, 20000)])
+def test_more_sequences_than_rows(T, S):
+    C = 70
+    g = torch.Generator().manual_seed(S)
+    x, ga, gi, dy = (torch.randn(T, C, generator=g).to(DEV) for _ in range(4))
+    cu = torch.cat([torch.tensor([0]), torch.randint(0, T + 1, (S - 1,), generator=g).sort().values, torch.tensor([T])])
+    h0, dhf = (torch.randn(S, C, generator=g).to(DEV) for _ in range(2))
+    rate = torch.full((C,), 0.3, device=DEV)
+    cud = cu.to(torch.int32).to(DEV)
+    _, fin, saved = pdssm.gated_fwd(x, ga, gi, rate, cu=cud, h0=h0)
+    got = pdssm.gated_bwd(x, ga, gi, rate, saved, dy, cu=cud, h0=h0, dh_final=dhf)
+    none = (cu.diff() == 0).to(DEV)
+    assert torch.equal(fin[none], h0[none]) and torch.equal(got[4][none], dhf[none])
+    args = [_np(t) for t in (x, ga, gi, rate)]
+    n = int(cu.diff().max())
+    h, want = G.gated_fwd(*args, cu.tolist(), _np(h0))
+    size, fin_size = G.gated_fwd(*args, cu.tolist(), _np(h0), absolute=True)
+    _near("h_final", _np(fin), want, fin_size, 2 * n + 32)
+    before = G.states_before(h, cu.tolist(), _np(h0))
+    w = G.gated_bwd(*args, cu.tolist(), before, _np(dy), _np(dhf))
+    m = G.gated_bwd(*args, cu.tolist(), np.abs(before), _np(dy), _np(dhf), absolute=True)
+    _near("dh0", _np(got[4]), w["dh0"], m["dh0"], 4 * n + 64)
+    _near("dx", _np(got[0]), w["dx"], m["dx"], 4 * n + 64)
+
+
+def test_many_sequences_of_length_zero():
+    z, rate, h0 = torch.empty(2500, 0, 70, device=DEV), torch.ones(70, device=DEV), torch.randn(2500, 70, device=DEV)
+    _, fin, saved = pdssm.gated_fwd(z, z, z, rate, h0=h0)
+    assert torch.equal(fin, h0)
+    got = pdssm.gated_bwd(z, z, z, rate, saved, z, dh_final=h0)
+    assert torch.equal(got[4], h0) and (got[3] == 0).all()
