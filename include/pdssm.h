@@ -431,7 +431,9 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
  * Otherwise cu [S+1] int32 on the device, cu[0] = 0 <= cu[1] <= ... <= cu[S]
  * <= T, sequence s has rows cu[s] .. cu[s+1]-1, and may have none (h_final =
  * h0, dh0 = dh_final).  Rows behind cu[S] are not used, and their outputs not
- * written.  A cu that breaks the rule is reported as PDSSM_ERR_INDEX in
+ * written; with PDSSM_FLAG_ZERO_REST in desc->flags they are zero (in the 8-bit
+ * form zeros at the lowest exponent, -126), so that a sum over all T rows, such
+ * as pdssm_project_wgrad's, is one over the sequences.  A cu that breaks the rule is reported as PDSSM_ERR_INDEX in
  * *dev_status; every access stays in bounds and the results mean nothing.
  *
  * Held rows.  A logit ga <= PDSSM_GATE_HOLD (so also -inf and the type's
@@ -450,6 +452,7 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
  * rounding (at most 2^(e-1), at e = 122 2^e), also to bf16.  e = -128 marks a block
  * that held a NaN or an infinity: its values read NaN.  q = -128 is the code
  * of a held gate logit and reads -inf, in such a block too. */
+#define PDSSM_FLAG_ZERO_REST 8u /* pdssm_gated_fwd and pdssm_gated_bwd */
 #define PDSSM_GATE_HOLD (-64.0f)
 #define PDSSM_GATED_CHUNK 128 /* rows between two saved states */
 #define PDSSM_KEPT_ROWS 32    /* rows that share an exponent in the 8-bit form */
@@ -464,7 +467,7 @@ typedef struct pdssm_gated_desc {
     /* rows, channels, sequences; 0 <= T <= 2^30, 1 <= C <= 2^24, 1 <= S <= 2^30
      * and ceil(T/128) * ceil(C/64) < 2^23, else PDSSM_ERR_UNSUPPORTED */
     int32_t T, C, S;
-    uint32_t flags;  /* 0 or PDSSM_FLAG_BF16_IO */
+    uint32_t flags;  /* PDSSM_FLAG_BF16_IO | PDSSM_FLAG_ZERO_REST, or one of them, or 0 */
 } pdssm_gated_desc;
 
 /* Workspace bytes of pdssm_gated_fwd (PDSSM_OP_FWD) or pdssm_gated_bwd
@@ -537,7 +540,8 @@ int pdssm_unpack8(int32_t T, int32_t C, uint32_t flags, const int8_t* q, const i
  *   dW[m, d] = sum_t dP[t, m] * u[t, d],   u = q * 2^e.
  * dP [T, M] bf16 (the bf16 pairs dD, db, dc of pdssm_scan_bwd are such rows,
  * M = 2 H N), q [T, Dm], e [ceil(T/32), Dm] as pdssm_pack8 writes them (no code
- * -128), dW [M, Dm] fp32.  On the matrix cores with fp32 sums: both operands
+ * -128), dW [M, Dm] fp32.  All T rows count, also such as lie behind the last
+ * of packed sequences (PDSSM_FLAG_ZERO_REST).  On the matrix cores with fp32 sums: both operands
  * are exact in bf16.  0 <= T <= 2^30; M a multiple of 8, Dm of 16, both at most
  * 2^20; T*M and T*Dm below 2^40, M*Dm below 2^31 entries; dP, q, e and dW 16-byte aligned.  ws:
  * pdssm_project_wgrad_workspace_size bytes, 256-byte aligned.

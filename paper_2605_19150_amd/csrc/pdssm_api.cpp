@@ -380,7 +380,7 @@ static_assert(PDSSM_GATED_CHUNK == pdssm::kGatedChunk && PDSSM_KEPT_ROWS == pdss
 constexpr int64_t kMaxLd = 1 << 24;  // entries from row to row
 
 int check_gated(const pdssm_gated_desc* d) {
-    if (!d || (d->flags & ~PDSSM_FLAG_BF16_IO) != 0) return PDSSM_ERR_INVALID_ARG;
+    if (!d || (d->flags & ~(PDSSM_FLAG_BF16_IO | PDSSM_FLAG_ZERO_REST)) != 0) return PDSSM_ERR_INVALID_ARG;
     if (d->T < 0 || d->C < 1 || d->S < 1) return PDSSM_ERR_INVALID_ARG;
     // row offsets are 64-bit; offsets within a wave's 16 rows and row numbers stay
     // below 2^31, and a launch below 2^32 threads (512 for 128 rows of 64 channels)
@@ -858,6 +858,7 @@ int pdssm_gated_fwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_
     a.S = d->S;
     a.L = cu ? 0 : T / d->S;
     a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.zero_rest = (d->flags & PDSSM_FLAG_ZERO_REST) != 0;
     a.x = rows_in(x);
     a.ga = rows_in(ga);
     a.gi = rows_in(gi);
@@ -930,6 +931,7 @@ int pdssm_gated_bwd(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm_
     a.S = d->S;
     a.L = cu ? 0 : T / d->S;
     a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.zero_rest = (d->flags & PDSSM_FLAG_ZERO_REST) != 0;
     a.kept = kept;
     a.x = rows_in(x);
     a.ga = rows_in(ga);
@@ -956,6 +958,7 @@ int pdssm_gated_step(const pdssm_gated_desc* d, const pdssm_rows* x, const pdssm
     if (st != PDSSM_OK) return st;
     const int B = d->T, C = d->C;
     const size_t w = row_bytes(d->flags), ns = (size_t)d->S * C * 4;
+    if (d->flags & PDSSM_FLAG_ZERO_REST) return PDSSM_ERR_INVALID_ARG;
     if (B > 65535) return PDSSM_ERR_UNSUPPORTED;  // grid
     for (const pdssm_rows* r : {x, ga, gi})
         if (bad_rows(r, B, C, w) || r->e) return PDSSM_ERR_INVALID_ARG;

@@ -11,7 +11,11 @@ namespace pdssm {
 
 constexpr int kGatedChunk = 128;  // rows between two saved states
 struct GatedArgs {
-    int T, C, S;
+    int T, C;
+    // one word: with a scalar register more than 80 the forward has three workgroups
+    // on a CU in place of four (54 -> 57 us at B16 L2048 C1024 bf16)
+    unsigned S : 31;
+    unsigned zero_rest : 1;  // outputs of rows behind the last sequence are zero; else they are not written
     int L;               // rows of a sequence where cu is null
     int io;              // format of y, dy, dx, dga, dgi; and of x, ga, gi unless kept
     int kept;            // backward: x, ga, gi are in the 8-bit form

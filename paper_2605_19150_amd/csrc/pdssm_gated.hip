@@ -433,6 +433,8 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
     const RowKinds kinds = row_kinds(a, row0);
     const LaneRows<1> rows(kinds, 0);
     const float rate = rate_of(rate_in);  // looked at behind the rows' loads: it would hold them up
+    // whether row i, in no sequence, is written all the same: a zero
+    auto rest = [&](int i) { return a.zero_rest && row0 + i < a.T; };
     if constexpr (KEEP) {
         // the 8-bit form of the rows in sequences; held rows keep only that
         uint32_t top[3] = {0, 0, 0};
@@ -456,7 +458,7 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
             const int e = kept_exponent(max(top[m], tops[m][wv ^ 1][lane]));
             inv[m] = kept_inverse(e);
             lim[m] = kept_limit(e);
-            if (!(wv & 1) && any && live) a.e[m][(size_t)(row0 / kKeptRows) * a.C + c] = (int8_t)e;
+            if (!(wv & 1) && (any || rest(0)) && live) a.e[m][(size_t)(row0 / kKeptRows) * a.C + c] = (int8_t)e;
         }
         RowBlock q[3];
 #pragma unroll
@@ -465,12 +467,16 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             uint32_t to = voff;
-            if (rare(rows.unused_any, i)) to = rows.is(rows.used, i) ? voff : kPast;
             const float l = S::get(ga[i], 0);
             const bool hold = l <= kGateHold;
-            Some<kRowKept, 1>::store(q[0], i, to, hold ? 0 : kept_code(S::get(x[i], 0), inv[0], lim[0]));
-            Some<kRowKept, 1>::store(q[1], i, to, hold ? kKeptLow : kept_code(l, inv[1], lim[1]));
-            Some<kRowKept, 1>::store(q[2], i, to, hold ? 0 : kept_code(S::get(gi[i], 0), inv[2], lim[2]));
+            int code[3] = {hold ? 0 : kept_code(S::get(x[i], 0), inv[0], lim[0]), hold ? kKeptLow : kept_code(l, inv[1], lim[1]),
+                           hold ? 0 : kept_code(S::get(gi[i], 0), inv[2], lim[2])};
+            if (rare(rows.unused_any, i) && !rows.is(rows.used, i)) {
+                to = rest(i) ? voff : kPast;
+                code[0] = code[1] = code[2] = 0;
+            }
+#pragma unroll
+            for (int m = 0; m < 3; ++m) Some<kRowKept, 1>::store(q[m], i, to, code[m]);
         }
     }
 
@@ -541,7 +547,8 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             h = rows.is(rows.first, i) ? bv[i] : fmaf(av[i], h, bv[i]);
-            S::store(y, i, rows.is(rows.used, i) ? voff : kPast, h);
+            const bool used = rows.is(rows.used, i);
+            S::store(y, i, used || rest(i) ? voff : kPast, used ? h : 0.f);
             float* f = rows.place(a.h_final, i, a.C, cc);
             if (rows.is(rows.last, i) && live && a.h_final) *f = h;
         }
@@ -770,6 +777,13 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
         }
         if (i % Shape<V>::TOGETHER == 0) __builtin_amdgcn_sched_barrier(0);
     }
+    // the rows behind the last sequence are zero if the caller asks for it (the
+    // stores above drop them)
+    if (a.zero_rest && a.cu)
+        for (int t = max(row0, a.cu[a.S]); t < min(a.T, row0 + kWaveRows); ++t)
+#pragma unroll
+            for (int m = 0; m < 3; ++m)
+                if (cb * 64 + lane < a.C) static_cast<typename Entry<IO>::T*>(a.d[m])[t * a.ldd + cb * 64 + lane] = 0;
     empty_sequences(a, a.dhf, a.dh0, cb * 64 + lane, cb == 0, (NC - 1 - k) * kWaves + wv, (int64_t)NC * kWaves);
     if (!a.drate) return;
 #pragma unroll

@@ -22,7 +22,8 @@ Gated recurrent layers (gated_fwd and the functions after it) take rows:
   x, ga, gi, dy [B,L,C] for B sequences of one length, or [T,C] with the
   sequences' bounds cu [S+1] int32; float32 or bfloat16, any strides between
   rows, entries of a row next to each other.  rate [C] and the states
-  [S,C] are float32.  Activations in the 8-bit form are pairs (q, e): int8
+  [S,C] are float32.  What is returned for rows behind the last sequence
+  (cu[S] < T) is zero.  Activations in the 8-bit form are pairs (q, e): int8
   [T,C] and [ceil(T/32),C].
 """
 import ctypes
@@ -42,6 +43,7 @@ OP_FWD, OP_BWD, OP_COMPOSE, OP_STE_GRADS = 1, 2, 3, 4
 FLAG_PREPARED = 1
 FLAG_BF16_IO = 2
 FLAG_REAL_IO = 4
+FLAG_ZERO_REST = 8  # gated_fwd, gated_bwd: rows behind the last sequence are written, as zeros
 
 
 class PdssmError(RuntimeError):
@@ -822,9 +824,12 @@ def gated_fwd(x, ga, gi, rate, cu=None, h0=None, hold8=False, check=True, stream
     in h0 [S,C] (default 0).  Returns (y, h_final [S,C], saved
     [ceil(T/128),C]), y = h in the rows' type and shape; with hold8=True also
     ((q, e) of x, of ga, of gi): the inputs in the 8-bit form, which gated_bwd
-    takes in their place.  check=False neither synchronises nor reports a bad cu."""
+    takes in their place.  Rows behind the last sequence are zero, in the 8-bit
+    form too.  check=False neither synchronises nor reports a bad cu."""
     flags = _row_type(x)
     T, C, S = _sequences(x, cu)
+    if cu is not None:
+        flags |= FLAG_ZERO_REST
     dev, shape = x.device, x.shape
     d = _desc(T, C, S, flags)
     rows = [_rows(t, n, x.dtype, shape, dev) for t, n in ((x, "x"), (ga, "ga"), (gi, "gi"))]
@@ -854,9 +859,12 @@ def gated_bwd(x, ga, gi, rate, saved, dy, cu=None, h0=None, dh_final=None, check
     as y) and dh_final [S,C] (default 0); saved, cu and h0 as in the forward.  x, ga, gi are the
     forward's rows, or all three the pairs (q, e) that it returned with
     hold8=True.  dx, dga and dgi, in dy's type and shape, are the three parts of one
-    tensor [..., 3C], the gradient of a projection that makes the three."""
+    tensor [..., 3C], the gradient of a projection that makes the three; rows
+    behind the last sequence are zero in them, so project_wgrad may sum over all."""
     flags = _row_type(dy)
     T, C, S = _sequences(dy, cu)
+    if cu is not None:
+        flags |= FLAG_ZERO_REST
     dev, shape = dy.device, dy.shape
     ins = ((x, "x"), (ga, "ga"), (gi, "gi"))
     eight = isinstance(x, (tuple, list))
@@ -957,7 +965,9 @@ def project_wgrad(dP, u8, stream=None):
     """dW [M,Dm] float32 = dP^T u, the weight gradient of a projection P = u W^T:
     dP bfloat16 with B*L rows of M entries in all (the bf16 pairs that
     scan_bwd returns, [B,L,H,N,2], are rows of 2*H*N), u8 the activations u in
-    the 8-bit form (pack8)."""
+    the 8-bit form (pack8).  All rows count: where sequences are packed, those
+    behind the last one have to be zero in one of the two and finite in the other
+    (gated_fwd and gated_bwd return zeros there)."""
     q, e = u8
     if not isinstance(q, torch.Tensor) or q.dim() != 2:
         raise ValueError("u8 must be a pair (q, e) with q [T,Dm]")

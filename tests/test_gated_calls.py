@@ -1,5 +1,6 @@
 """How the binding of the gated operators is called (no GPU): what it checks
 before it reaches the library."""
+import ctypes
 import inspect
 
 import pytest
@@ -51,3 +52,16 @@ def test_a_stream_of_another_device_is_refused(monkeypatch):
     own = _Stream("cuda:0", 4096)
     assert pdssm._on(own, dev, ()) == 4096 and own.waited == "current"
     assert pdssm._on(_Stream("cuda:0", 0), dev, ()) == 0 and pdssm._on(None, dev, ()) == 0
+
+
+def test_flags_of_the_passes_and_the_step():
+    """Zeros behind the last sequence are for the two passes; the step has no such rows."""
+    lib = pdssm.load()
+    bad = ctypes.c_size_t(-1).value
+    for flags in (pdssm.FLAG_ZERO_REST, pdssm.FLAG_ZERO_REST | pdssm.FLAG_BF16_IO):
+        d, r = pdssm._DESC.pack(4, 16, 4, flags), pdssm._ROW.pack(1 << 32, 16, 0)
+        for op in (pdssm.OP_FWD, pdssm.OP_BWD):
+            assert lib.pdssm_gated_workspace_size(d, op) != bad
+        far = [(1 << 33) + (k << 26) for k in range(5)]
+        assert lib.pdssm_gated_step(d, r, r, r, far[0], None, far[1], far[2], far[3], None, None) == pdssm.ERR_INVALID_ARG
+    assert lib.pdssm_gated_workspace_size(pdssm._DESC.pack(4, 16, 4, 16), pdssm.OP_FWD) == bad

@@ -55,6 +55,70 @@ def test_rates_that_are_not_positive_and_finite(bounds, dtype, C):
         assert torch.isnan(v[:, bad]).all() and torch.equal(v[:, rest], v0[:, rest])
 
 
+# ---- rows behind the last sequence -----------------------------------------
+
+@pytest.mark.parametrize("dtype,C", [(torch.float32, 33), (torch.bfloat16, 65), (torch.bfloat16, 66), (torch.float32, 64)])
+@pytest.mark.parametrize("bounds,T", [([0, 40, 130], 300), ([0, 128], 129), ([0, 5], 6), ([0, 96, 96], 256), ([0, 0], 40),
+                                      ([0, 0, 0], 300), ([0, 31], 500)])
+def test_rows_behind_the_last_sequence_are_zero(bounds, T, dtype, C):
+    """The binding's outputs there, whatever the inputs and the memory held."""
+    case = Case(bounds, C, T=T, dtype=dtype, wide=C % 2 == 1, seed=T)
+    end, first = bounds[-1], -(-bounds[-1] // 32)
+    for t in (case.x, case.ga, case.gi, case.dy):
+        t[end:] = math.nan
+    n = T * C
+    _dirty(n, 2 * n, 4 * n, 6 * n, 12 * n, -(-T // 32) * C)
+    y, fin, saved, kept = case.fwd(hold8=True)
+    assert (y[end:] == 0).all()
+    for q, e in kept:
+        assert (q[end:] == 0).all() and (e[first:] == -126).all()
+        assert (pdssm.unpack8((q, e))[end:] == 0).all()
+    for k in (None, kept):
+        _dirty(6 * n, 12 * n)
+        got = case.bwd(saved, k)
+        assert all((t[end:] == 0).all() for t in got[:3])
+    y, _, saved = case.fwd()
+    assert (y[end:] == 0).all()
+    if end:
+        h, size = _check_fwd(case, y, fin)
+        _check_bwd(case, case.bwd(saved), h, size)
+
+
+def test_weight_gradient_of_packed_rows():
+    """The gradients and the kept rows as they are returned, rows behind the last sequence included."""
+    case = Case([0, 130, 130, 1000], 80, T=1500, dtype=torch.bfloat16, wide=False, seed=6)
+    for t in (case.x, case.ga, case.gi, case.dy):
+        t[1000:] = math.nan
+    _dirty(1500 * 240 * 2, 1500 * 80)
+    y, fin, saved, kept = case.fwd(hold8=True)
+    _dirty(1500 * 240 * 2)
+    dP = torch.cat(case.bwd(saved, kept)[:3], 1)
+    p, u = _np(dP)[:1000], G.unpack8(*(t.cpu().numpy() for t in kept[0]))[:1000]
+    # 1500 products, a rounding each; the last 500 are zero
+    _near("dW", _np(pdssm.project_wgrad(dP, kept[0])), p.T @ u, np.abs(p).T @ np.abs(u), 1502)
+
+
+def test_captured_set_with_its_weight_gradient():
+    """Every output of a replayed graph, the weight gradient too."""
+    case = Case([0, 130, 130, 1000], 80, T=1003, dtype=torch.bfloat16, seed=6)
+    _all_ops(case)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = _all_ops(case)
+    for _ in range(4):
+        case.x.copy_(torch.randn_like(case.x))
+        case.dy.copy_(torch.randn_like(case.dy))
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        _dirty(1003 * 240 * 2, 1003 * 80)
+        want = _all_ops(case)
+        torch.cuda.synchronize()
+        for n, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), n
+
+
 # ---- very many sequences ---------------------------------------------------
 
 def test_very_many_sequences():
