@@ -114,14 +114,28 @@ def unpack8(q, e):
     return np.where(q == -128, -np.inf, v)
 
 
+OPEN = 31.75  # the least that a block with a gate logit of +inf reaches: the sigmoid is 1 in 32 bits
+
+
 def kept(x, ga, gi, end):
     """The values of x, ga, gi that the forward's 8-bit form stands for: rows up
-    to `end`, held rows kept as 0, held, 0; rows behind as 0."""
+    to `end`, held rows kept as 0, held, 0; a logit of +inf as the largest code
+    of a block that reaches OPEN, -inf (gi) as itself; rows behind as 0."""
     held = np.asarray(ga[:end], np.float64) <= HOLD
     out = []
-    for v, low in ((x, 0.0), (ga, -np.inf), (gi, 0.0)):
+    for k, v in enumerate((x, ga, gi)):
         w = np.where(held, 0.0, np.asarray(v[:end], np.float64))
-        w = np.where(held, low, unpack8(*pack8(w)))
+        low = held if k == 1 else np.zeros_like(held)
+        top = np.zeros_like(held)
+        if k > 0:
+            top = w == np.inf
+            w = np.where(top, OPEN, w)
+        if k == 2:
+            low = w == -np.inf
+            w = np.where(low, 0.0, w)
+        q, e = pack8(w)
+        q[top] = 127
+        w = np.where(low, -np.inf, unpack8(q, e))
         full = np.zeros(x.shape)
         full[:end] = w
         out.append(full)

@@ -271,6 +271,9 @@ __device__ __forceinline__ RowBlock row_block_of(const void* p, int64_t ld, int 
 // V neighbouring entries of a row in a register, and row i of a lane's group in
 // memory.  Nobody reads the outputs here again: they are stored past the caches
 // (nontemporal), 147 -> 138 us for the backward at B16 L2048 C1024 bf16.
+// What a gate logit of +inf counts as in the exponent of its block of the 8-bit
+// form: its sigmoid, 1 - 1.6e-14, is 1 in 32 bits, and it is 127 * 2^-2.
+constexpr float kOpen = 31.75f;
 template <int IO, int V>
 struct Some;
 template <>
@@ -335,7 +338,7 @@ struct Some<kRowKept, 2> {
     static __device__ __forceinline__ float get(R v, int n, float scale) { return (float)code(v, n) * scale; }
 };
 
-// A gate logit; in the 8-bit form with the code of a held one.
+// A gate logit; in the 8-bit form with the code of -inf.
 template <int IO, int V>
 __device__ __forceinline__ float logit(typename Some<IO, V>::R v, int n, float scale) {
     if constexpr (IO == kRowKept)
@@ -447,17 +450,35 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
 #pragma unroll
             for (int m = 0; m < 3; ++m) top[m] = max(top[m], skip ? 0u : __float_as_uint(v[m]) & 0x7fffffffu);
         }
+        // An infinite gate is no reason to lose the block: +inf, in both gates,
+        // gets the largest code, of at least kOpen, and an input gate's -inf a
+        // code of its own and no part in the exponent.  The few waves that have
+        // one read their rows again: the registers of all others stay as they are.
+        constexpr uint32_t kInf = 0x7f800000u;
+        if (__builtin_expect(__any(top[1] == kInf || top[2] == kInf), 0)) {
+            const RowsOf<IO, 1> ls(a.ga, a.T, a.C, row0, 0, cc), ns(a.gi, a.T, a.C, row0, 0, cc);
+            auto counts = [](float v) { return __float_as_uint(v == INFINITY ? kOpen : v) & 0x7fffffffu; };
+            top[1] = top[2] = 0;
+#pragma unroll 1
+            for (int i = 0; i < ROWS; ++i) {
+                const float l = S::get(ls.row(i), 0), n = S::get(ns.row(i), 0);
+                if (l <= kGateHold || !(rows.used >> i & 1)) continue;
+                top[1] = max(top[1], counts(l));
+                if (n != -INFINITY) top[2] = max(top[2], counts(n));
+            }
+        }
 #pragma unroll
         for (int m = 0; m < 3; ++m) tops[m][wv][lane] = top[m];
         if (lane == 0) some[wv] = kinds.used != 0;
         __syncthreads();
-        float inv[3], lim[3];
+        float inv[3], lim[3], low = 0.f;
         const bool any = __builtin_amdgcn_readfirstlane(some[wv & ~1] | some[wv | 1]);
 #pragma unroll
         for (int m = 0; m < 3; ++m) {
             const int e = kept_exponent(max(top[m], tops[m][wv ^ 1][lane]));
             inv[m] = kept_inverse(e);
             lim[m] = kept_limit(e);
+            if (m == 2) low = kept_low(e);
             if (!(wv & 1) && (any || rest(0)) && live) a.e[m][(size_t)(row0 / kKeptRows) * a.C + c] = (int8_t)e;
         }
         RowBlock q[3];
@@ -470,7 +491,7 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
             const float l = S::get(ga[i], 0);
             const bool hold = l <= kGateHold;
             int code[3] = {hold ? 0 : kept_code(S::get(x[i], 0), inv[0], lim[0]), hold ? kKeptLow : kept_code(l, inv[1], lim[1]),
-                           hold ? 0 : kept_code(S::get(gi[i], 0), inv[2], lim[2])};
+                           hold ? 0 : kept_code_or_low(S::get(gi[i], 0), inv[2], low, lim[2])};
             if (rare(rows.unused_any, i) && !rows.is(rows.used, i)) {
                 to = rest(i) ? voff : kPast;
                 code[0] = code[1] = code[2] = 0;
@@ -624,7 +645,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void k_gated_bwd(GatedArgs a, float
         for (int n = 0; n < V; ++n) {
             const float l = logit<IN, V>(gar[i], n, scale[1][n]);
             r[i][n] = sigmoid_f(l);
-            in[i][n] = sigmoid_f(N::get(gir[i], n, scale[2][n]));
+            in[i][n] = sigmoid_f(logit<IN, V>(gir[i], n, scale[2][n]));
             float ix = in[i][n] * N::get(xr[i], n, scale[0][n]);
             const bool hold = l <= kGateHold;
             r[i][n] = hold ? 0.f : r[i][n];

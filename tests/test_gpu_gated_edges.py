@@ -210,3 +210,53 @@ def test_many_sequences_of_length_zero():
     assert torch.equal(fin, h0)
     got = pdssm.gated_bwd(z, z, z, rate, saved, z, dh_final=h0)
     assert torch.equal(got[4], h0) and (got[3] == 0).all()
+
+
+# ---- infinite gates --------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,C", [(torch.float32, 65), (torch.bfloat16, 65), (torch.bfloat16, 66)])
+def test_infinite_gates_in_the_eight_bit_form(dtype, C):
+    """A gate that is open or an input that is masked altogether has the finite gradients of the plain rows, and leaves
+    its neighbours' as good as they are without it."""
+    case = Case([0, 60, 300, 470], C, T=475, dtype=dtype, wide=C % 2 == 1, masked=True, seed=C)
+    pick = torch.Generator().manual_seed(5)
+    # rows whose values count: held ones may hold anything
+    live = torch.from_numpy(_np(case.ga) > G.HOLD).to(DEV)
+    for t, v, share in ((case.gi, -math.inf, 0.2), (case.gi, math.inf, 0.02), (case.ga, math.inf, 0.02)):
+        at = (torch.rand(case.T, C, generator=pick) < share).to(DEV) & live
+        t[at] = v
+    y, fin, saved, kept = case.fwd(hold8=True)
+    h, size = _check_fwd(case, y, fin)
+    plain = case.bwd(saved)
+    want = G.kept(*(_np(t) for t in (case.x, case.ga, case.gi)), case.end)
+    blocks = -(-case.end // 32)
+    for (q, e), w in zip(kept, want):
+        assert np.array_equal(G.unpack8(q.cpu().numpy()[:case.end], e.cpu().numpy()[:blocks]), w[:case.end])
+        assert np.array_equal(_np(pdssm.unpack8((q, e)))[:case.end], w[:case.end])
+    got = case.bwd(saved, kept)
+    for t in (*plain, *got):
+        rows = case.end if t.shape[0] == case.T else t.shape[0]
+        assert torch.isfinite(t[:rows]).all()
+    # the kept value of an open gate is 31.75 or more, where the sigmoid is 1 in 32 bits as it is at infinity
+    args = [w.copy() for w in want]
+    for w, t in ((args[1], case.ga), (args[2], case.gi)):
+        w[_np(t) == math.inf] = math.inf
+    _check_bwd(case, got, h, size, kept=args)
+    shut = _np(case.gi)[:case.end] == -math.inf
+    shut &= _np(case.ga)[:case.end] > G.HOLD
+    assert shut.sum() > 1000 and all((_np(got[k])[:case.end][shut] == 0).all() for k in (0, 2))
+
+
+def test_infinite_gates_beside_a_nan():
+    """A block with a NaN is marked whatever else it holds, and infinite inputs mark theirs as before."""
+    case = Case([0, 200], 66, seed=11)
+    case.gi[40, 3], case.gi[41, 3], case.ga[70, 5], case.ga[71, 5] = math.nan, -math.inf, math.nan, math.inf
+    case.x[100, 7], case.gi[0, 9] = math.inf, -math.inf
+    _, _, _, kept = case.fwd(hold8=True)
+    bad = [(100, 7), (70, 5), (40, 3)]
+    for (q, e), (t, c) in zip(kept, bad):
+        v = _np(pdssm.unpack8((q, e)))
+        block = np.zeros_like(v, bool)
+        block[t // 32 * 32:t // 32 * 32 + 32, c] = True
+        assert np.isnan(v[block]).all() and not np.isnan(v[~block]).any()
+        assert (e[:, c].cpu().numpy() == -128).sum() == 1
