@@ -65,3 +65,10 @@ def test_flags_of_the_passes_and_the_step():
         far = [(1 << 33) + (k << 26) for k in range(5)]
         assert lib.pdssm_gated_step(d, r, r, r, far[0], None, far[1], far[2], far[3], None, None) == pdssm.ERR_INVALID_ARG
     assert lib.pdssm_gated_workspace_size(pdssm._DESC.pack(4, 16, 4, 16), pdssm.OP_FWD) == bad
+
+
+def test_packed_arguments_are_the_structures():
+    """The binding packs pdssm_gated_desc and pdssm_rows itself; the ctypes structures say the same."""
+    assert pdssm._DESC.pack(1000, 65, 7, 10) == bytes(pdssm.GatedDesc(1000, 65, 7, 10))
+    assert pdssm._ROW.pack(1 << 40, 77, 1 << 33) == bytes(pdssm.Rows(1 << 40, 77, 1 << 33))
+    assert pdssm._ROW.pack(1 << 40, 77, 0) == bytes(pdssm.Rows(1 << 40, 77, None))

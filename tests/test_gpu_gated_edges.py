@@ -260,3 +260,19 @@ def test_infinite_gates_beside_a_nan():
         block[t // 32 * 32:t // 32 * 32 + 32, c] = True
         assert np.isnan(v[block]).all() and not np.isnan(v[~block]).any()
         assert (e[:, c].cpu().numpy() == -128).sum() == 1
+
+
+# ---- weight gradient -------------------------------------------------------
+
+@pytest.mark.parametrize("T,M,Dm", [(98401, 264, 272), (6200, 4096, 1024), (131072, 512, 512), (100, 3592, 3344),
+                                    (5000, 520, 64), (20000, 64, 32), (3000, 2048, 2048), (1600, 1024, 1040), (777, 40, 48)])
+def test_weight_gradient_whose_sums_are_exact(T, M, Dm):
+    """Whole numbers, so that every partial sum is one below 2^24: a share of the tokens that is lost, counted twice or
+    cut at the wrong row changes the result.  Both tiles, with and without shares, few and many of them."""
+    g = torch.Generator(device=DEV).manual_seed(T)
+    dP = torch.randint(-3, 4, (T, M), generator=g, device=DEV)
+    u = torch.randint(-5, 6, (T, Dm), generator=g, device=DEV)
+    u8 = pdssm.pack8(u.to(torch.bfloat16))
+    assert torch.equal(pdssm.unpack8(u8), u.float()) and 15 * T < 1 << 24
+    want = dP.double().t().contiguous() @ u.double()
+    assert torch.equal(pdssm.project_wgrad(dP.to(torch.bfloat16), u8).double(), want)
