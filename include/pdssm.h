@@ -451,8 +451,8 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
  * magnitude: 64 would stand for 2^128).  Both ways are exact but for that
  * rounding (at most 2^(e-1), at e = 122 2^e), also to bf16.  e = -128 marks a block
  * that held a NaN or an infinity: its values read NaN.  q = -128 reads -inf, in
- * such a block too: the code of a held gate logit, and of an input gate's -inf
- * (which has no part in the exponent) where pdssm_gated_fwd writes the form. */
+ * such a block too: the code of a held gate logit, and of an input gate that is
+ * shut, where pdssm_gated_fwd writes the form. */
 #define PDSSM_FLAG_ZERO_REST 8u /* pdssm_gated_fwd and pdssm_gated_bwd */
 #define PDSSM_GATE_HOLD (-64.0f)
 #define PDSSM_GATED_CHUNK 128 /* rows between two saved states */
@@ -482,11 +482,13 @@ size_t pdssm_gated_workspace_size(const pdssm_gated_desc* desc, int op);
  * pdssm_gated_bwd needs (a row whose chunk begins with a sequence's first row
  * is not read there); optional q[3], e[3]: x, ga, gi in the 8-bit form, all
  * six or none (q == e == NULL).  In a held row x and gi are kept as 0 and ga as
- * held.  In the others a logit of +inf is kept as the largest code of a block
- * that reaches 31.75, whose sigmoid is 1 in 32 bits, and -inf in gi as that, so
- * such gates have the gradients of the plain rows; a NaN in a block, or an infinite x, makes the block NaN, and with it the
- * gradients of its channel from the block back to the sequence's first row and on
- * to the end of the chunk.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned (0: none).
+ * held.  In the others logits count for the exponent with 31.75 at most, where
+ * the sigmoid is 1 in 32 bits, and those of gi from -89 down, where it is 0, not at
+ * all; what then lies past the codes, infinities too, is kept as the largest one,
+ * or in gi as -inf.  So masks and open gates have the gradients of the plain rows
+ * and cost their neighbours nothing.  A NaN, or an
+ * infinite x, makes its block NaN, and with it gradients of its channel in the
+ * sequences that have rows in the block.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned (0: none).
  * Results are deterministic.
  *
  * In this call and the next, workgroups with different rows of a channel wait

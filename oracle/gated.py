@@ -114,28 +114,28 @@ def unpack8(q, e):
     return np.where(q == -128, -np.inf, v)
 
 
-OPEN = 31.75  # the least that a block with a gate logit of +inf reaches: the sigmoid is 1 in 32 bits
+OPEN, SHUT = 31.75, -89.0  # in 32 bits the sigmoid is 1 from OPEN up and 0 from SHUT down
 
 
 def kept(x, ga, gi, end):
     """The values of x, ga, gi that the forward's 8-bit form stands for: rows up
-    to `end`, held rows kept as 0, held, 0; a logit of +inf as the largest code
-    of a block that reaches OPEN, -inf (gi) as itself; rows behind as 0."""
+    to `end`, held rows kept as 0, held, 0; logits past OPEN as the largest code
+    of a block that reaches OPEN; gi from SHUT down as -inf where its code is past
+    -127; rows behind as 0."""
     held = np.asarray(ga[:end], np.float64) <= HOLD
     out = []
     for k, v in enumerate((x, ga, gi)):
-        w = np.where(held, 0.0, np.asarray(v[:end], np.float64))
-        low = held if k == 1 else np.zeros_like(held)
-        top = np.zeros_like(held)
-        if k > 0:
-            top = w == np.inf
-            w = np.where(top, OPEN, w)
-        if k == 2:
-            low = w == -np.inf
-            w = np.where(low, 0.0, w)
+        v = np.where(held, 0.0, np.asarray(v[:end], np.float64))
+        low = held if k == 1 else v <= SHUT if k == 2 else np.zeros_like(held)
+        w = np.where(low, 0.0, v if k == 0 else np.where(v > OPEN, OPEN, v))
         q, e = pack8(w)
-        q[top] = 127
-        w = np.where(low, -np.inf, unpack8(q, e))
+        step = np.repeat(2.0 ** e.astype(np.float64), BLOCK, 0)[:end]
+        if k > 0:
+            q = np.where(v > OPEN, np.minimum(np.rint(np.minimum(v, 1e9) / step), 127), q)
+        if k == 2:
+            q = np.where(low, np.maximum(np.rint(np.maximum(v, -1e9) / step), -128), q)
+        w = unpack8(q, e)
+        w = np.where(held, -np.inf if k == 1 else 0.0, w)
         full = np.zeros(x.shape)
         full[:end] = w
         out.append(full)

@@ -271,9 +271,10 @@ __device__ __forceinline__ RowBlock row_block_of(const void* p, int64_t ld, int 
 // V neighbouring entries of a row in a register, and row i of a lane's group in
 // memory.  Nobody reads the outputs here again: they are stored past the caches
 // (nontemporal), 147 -> 138 us for the backward at B16 L2048 C1024 bf16.
-// What a gate logit of +inf counts as in the exponent of its block of the 8-bit
-// form: its sigmoid, 1 - 1.6e-14, is 1 in 32 bits, and it is 127 * 2^-2.
-constexpr float kOpen = 31.75f;
+// In 32 bits the sigmoid is 1 from kOpen = 127 * 2^-2 up (1 - 1.6e-14) and 0
+// from kShut down (its reciprocal is past the largest number): what the 8-bit
+// form keeps of logits further out need not tell them apart.
+constexpr float kOpen = 31.75f, kShut = -89.f;
 template <int IO, int V>
 struct Some;
 template <>
@@ -450,21 +451,23 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
 #pragma unroll
             for (int m = 0; m < 3; ++m) top[m] = max(top[m], skip ? 0u : __float_as_uint(v[m]) & 0x7fffffffu);
         }
-        // An infinite gate is no reason to lose the block: +inf, in both gates,
-        // gets the largest code, of at least kOpen, and an input gate's -inf a
-        // code of its own and no part in the exponent.  The few waves that have
-        // one read their rows again: the registers of all others stay as they are.
-        constexpr uint32_t kInf = 0x7f800000u;
-        if (__builtin_expect(__any(top[1] == kInf || top[2] == kInf), 0)) {
+        // A gate far out is no reason to lose the codes of its block: past kOpen,
+        // +inf too, both gates count as kOpen and get the largest code at most,
+        // and an input gate from kShut down (-inf, the type's lowest value) has
+        // no part in the exponent and gets the code that reads -inf, or its own.
+        // The few waves that have one read their rows again: the registers of
+        // all others stay as they are.
+        constexpr uint32_t kOpenBits = 0x41fe0000u;
+        if (__builtin_expect(__any(top[1] > kOpenBits || top[2] > kOpenBits), 0)) {
             const RowsOf<IO, 1> ls(a.ga, a.T, a.C, row0, 0, cc), ns(a.gi, a.T, a.C, row0, 0, cc);
-            auto counts = [](float v) { return __float_as_uint(v == INFINITY ? kOpen : v) & 0x7fffffffu; };
+            auto counts = [](float v) { return __float_as_uint(v > kOpen ? kOpen : v) & 0x7fffffffu; };
             top[1] = top[2] = 0;
 #pragma unroll 1
             for (int i = 0; i < ROWS; ++i) {
                 const float l = S::get(ls.row(i), 0), n = S::get(ns.row(i), 0);
                 if (l <= kGateHold || !(rows.used >> i & 1)) continue;
                 top[1] = max(top[1], counts(l));
-                if (n != -INFINITY) top[2] = max(top[2], counts(n));
+                if (!(n <= kShut)) top[2] = max(top[2], counts(n));
             }
         }
 #pragma unroll

@@ -15,7 +15,7 @@ namespace pdssm {
 // and q * 2^e, seven bits and a sign, is exact in bf16.  A value is off by at
 // most 2^(e-1), 1/127 of the block's largest magnitude.
 constexpr int kKeptPoison = -128;  // exponent of a block that held a NaN or an infinity: its values read NaN
-constexpr int kKeptLow = -128;     // code of a held gate logit and of an input gate's -inf: reads -inf
+constexpr int kKeptLow = -128;     // code of a held gate logit and of a shut input gate: reads -inf
 
 // Exponent for the largest magnitude of a block, given as its bits (which
 // order as the magnitudes do, NaN above infinity).
@@ -37,10 +37,9 @@ __device__ __forceinline__ float kept_limit(int e) { return e == 122 ? 63.f : 12
 __device__ __forceinline__ int kept_code(float v, float inverse, float limit) {
     return (int)__builtin_rintf(__builtin_amdgcn_fmed3f(v * inverse, -limit, limit));
 }
-// The same where the block's exponent is that of its finite entries: -inf gets
-// kKeptLow, which no finite one comes to (at the two exponents of other limits
-// -inf is as good as the largest code: no sigmoid knows them apart).
-__device__ __forceinline__ float kept_low(int e) { return e == 122 || e == kKeptPoison ? -kept_limit(e) : (float)kKeptLow; }
+// The same where some entries have no part in the block's exponent: they may
+// come to kKeptLow, which no other does.
+__device__ __forceinline__ float kept_low(int e) { return e == kKeptPoison ? -127.f : (float)kKeptLow; }
 __device__ __forceinline__ int kept_code_or_low(float v, float inverse, float low, float limit) {
     return (int)__builtin_rintf(__builtin_amdgcn_fmed3f(v * inverse, low, limit));
 }

@@ -247,6 +247,37 @@ def test_infinite_gates_in_the_eight_bit_form(dtype, C):
     assert shut.sum() > 1000 and all((_np(got[k])[:case.end][shut] == 0).all() for k in (0, 2))
 
 
+@pytest.mark.parametrize("dtype,C", [(torch.float32, 65), (torch.bfloat16, 65), (torch.bfloat16, 66)])
+@pytest.mark.parametrize("shut", ["lowest", -1e9, -1e4, -100.0, -89.0])
+def test_gates_far_out_in_the_eight_bit_form(shut, dtype, C):
+    """An input masked with the type's lowest value or any other that shuts its gate, and gates wide open, do not cost
+    the logits beside them their codes."""
+    case = Case([0, 60, 300, 470], C, T=475, dtype=dtype, wide=C % 2 == 1, seed=C)
+    clean = [_np(t) for t in (case.ga, case.gi)]
+    v = torch.finfo(dtype).min if shut == "lowest" else shut
+    pick = torch.Generator().manual_seed(6)
+    far = []
+    for t, v, share in ((case.ga, -v, 0.02), (case.gi, -v, 0.02), (case.gi, v, 0.2)):
+        at = (torch.rand(case.T, C, generator=pick) < share).to(DEV)
+        t[at] = v
+        far.append(_np(at) > 0)
+    y, fin, saved, kept = case.fwd(hold8=True)
+    h, size = _check_fwd(case, y, fin)
+    want = G.kept(*(_np(t) for t in (case.x, case.ga, case.gi)), case.end)
+    got = []
+    for (q, e), w in zip(kept, want):
+        got.append(_np(pdssm.unpack8((q, e))))
+        assert np.array_equal(got[-1][:case.end], w[:case.end])
+    # half a step of a block that reaches 31.75, and 2^-7 of what the largest of the others is
+    for v, c, out in ((got[1], clean[0], far[0]), (got[2], clean[1], far[1] | far[2])):
+        ok = ~out[:case.end]
+        assert np.abs(v[:case.end] - c[:case.end])[ok].max() <= 0.125
+    args = [w.copy() for w in want]
+    for w, out in ((args[1], far[0]), (args[2], far[1] & ~far[2])):
+        w[:case.end][out[:case.end]] = math.inf  # 1 in 32 bits, as there
+    _check_bwd(case, case.bwd(saved, kept), h, size, kept=args)
+
+
 def test_infinite_gates_beside_a_nan():
     """A block with a NaN is marked whatever else it holds, and infinite inputs mark theirs as before."""
     case = Case([0, 200], 66, seed=11)
