@@ -442,7 +442,8 @@ int pdssm_compose_chunks(const pdssm_desc* desc, const int32_t* idx, const int32
  *
  * rate [C] must be positive and finite: any other value (0, infinity, NaN)
  * gives NaN in that channel's rows, held ones too, in the states and gradients
- * behind them and in drate, and in no other channel.  A row with rate * r below 6e-39 counts as held.
+ * behind them and in drate, and in no other channel.  A row with rate * r below
+ * 6e-39 has the gradients of a held one.
  *
  * The 8-bit form of rows [T, C]: whole numbers q [T, C] int8 and exponents
  * e [ceil(T/32), C] int8, value q[t,c] * 2^e[t/32,c], with the smallest
@@ -486,9 +487,9 @@ size_t pdssm_gated_workspace_size(const pdssm_gated_desc* desc, int op);
  * the sigmoid is 1 in 32 bits, and those of gi from -89 down, where it is 0, not at
  * all; what then lies past the codes, infinities too, is kept as the largest one,
  * or in gi as -inf.  So masks and open gates have the gradients of the plain rows
- * and cost their neighbours nothing.  A NaN, or an
- * infinite x, makes its block NaN, and with it gradients of its channel in the
- * sequences that have rows in the block.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned (0: none).
+ * and cost their neighbours nothing.  A NaN, or an infinite x, makes its block NaN,
+ * and with it gradients of its channel in the sequences that have rows in the
+ * block.  ws: pdssm_gated_workspace_size bytes, 256-byte aligned (0: none).
  * Results are deterministic.
  *
  * In this call and the next, workgroups with different rows of a channel wait
@@ -509,7 +510,9 @@ int pdssm_gated_fwd(const pdssm_gated_desc* desc, const pdssm_rows* x, const pds
  * In: x, ga, gi rows, or all three in the 8-bit form; rate, cu, h0 as in the
  * forward; saved, from it; dy rows; dh_final [S, C] (optional).  The states
  * are recomputed within each chunk from the saved one, with the values of the
- * 8-bit form where that is given.
+ * 8-bit form where that is given.  1 - r and 1 - i are taken from the rounded
+ * gates, so dga and dgi are off by up to 2^-24 of w and of dx x beside their own
+ * rounding: logits past 17 give 0.
  * Out: d[0..2] = dx, dga, dgi, rows of ldd entries (>= C; parts of one wider
  * row tensor when ldd > C); optional drate [C] and dh0 [S, C].
  */

@@ -28,11 +28,12 @@
 //
 // Bound by memory, with the arithmetic close behind: six to nine hardware
 // exponentials, reciprocals and roots and about as many other operations as fit
-// under an entry's bytes.  At B16 L2048 C1024 bf16 the forward takes 56 us (270
-// MB, 4.8 TB/s; a large copy reaches 5.2), the backward 122 us with the kernels
-// around it (471 MB, 3.9 TB/s), the vector units 69% and 67% busy; in fp32 both
-// move 5 TB/s and more.  Forward with the 8-bit form and backward from it, B8
-// L18000 C1024 bf16: 925 us (3.28 GB), the vector units 80% busy.
+// under an entry's bytes.  At B16 L2048 C1024 bf16 a forward call takes 59 us
+// (270 MB, 4.6 TB/s; a large copy reaches 5.2), a backward call 122 us (471 MB,
+// 3.9 TB/s), the vector units about 70% busy; in fp32 the kernels take about 100
+// and 180 us (539 and 942 MB, 5.2 to 5.4 TB/s).  Forward with the 8-bit form and
+// backward from it, B8 L18000 C1024 bf16: 915 us (3.28 GB), the vector units 80%
+// busy.
 #include "pdssm_gated.h"
 
 #include "pdssm_device.h"
@@ -247,9 +248,11 @@ __device__ void empty_sequences(const GatedArgs& a, const float* in, float* out,
 }
 
 // ------------------------------------------------------------------ rows
-// A wave's rows as a buffer: reads behind the last row give 0, stores there
-// are dropped, and so are those of lanes past the last channel and of rows in no
-// sequence, whose offset lies past every buffer.
+// A wave's rows as a buffer.  A row behind the last one is, to the first group of
+// lanes, the last one again (the scalar offset ends there), to the second one
+// past the buffer, which reads 0: either way a row in no sequence, which the
+// masks of RowKinds leave out.  Stores of such rows, and of lanes past the last
+// channel, get an offset past every buffer and are dropped.
 struct RowBlock {
     __amdgpu_buffer_rsrc_t r;
     uint32_t ld;    // bytes from row to row

@@ -3,8 +3,9 @@
 // where rows allow 16-byte accesses, 16 lanes side by side and four groups of 8
 // rows, which agree on the largest magnitudes by two lane exchanges; else 64
 // channels side by side, all 32 rows in each lane.  The rows stay in registers
-// between the magnitude and the codes.  T32768 C4096 bf16 takes 92 us to the form
-// and 63 us back, 4.4 and 6.5 TB/s (a large copy reaches 5.2).
+// between the magnitude and the codes.  T32768 C4096 bf16 takes 89 to 99 us to
+// the form and 63 to 65 back (407 MB: 4.1 to 4.6 and 6.3 to 6.5 TB/s; a large copy
+// reaches 5.2), fp32 138 to 151 and 107 to 109 (675 MB).
 #include "pdssm_device.h"
 #include "pdssm_rows.h"
 

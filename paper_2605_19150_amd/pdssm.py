@@ -20,11 +20,14 @@ Straight-through surrogate gradients (Sec. 3.1 Prop. 2): q [B,L,H,K] float32,
   dense dictionary M [H,K,N,N] float32.
 Gated recurrent layers (gated_fwd and the functions after it) take rows:
   x, ga, gi, dy [B,L,C] for B sequences of one length, or [T,C] with the
-  sequences' bounds cu [S+1] int32; float32 or bfloat16, any strides between
-  rows, entries of a row next to each other.  rate [C] and the states
-  [S,C] are float32.  What is returned for rows behind the last sequence
+  sequences' bounds cu [S+1] int32; float32 or bfloat16, rows at one pitch
+  (parts of wider rows, not the first rows of each of several longer sequences)
+  of at most 2^24 entries, entries of a row next to each other.  rate [C] and
+  the states [S,C] are float32.  What is returned for rows behind the last sequence
   (cu[S] < T) is zero.  Activations in the 8-bit form are pairs (q, e): int8
-  [T,C] and [ceil(T/32),C].
+  [T,C] and [ceil(T/32),C].  These functions run on the current stream of the
+  tensors' device, or on the one given as stream, behind what the current stream
+  has to do; who reads the results on another stream has to wait for that one.
 """
 import ctypes
 import functools
