@@ -861,7 +861,7 @@ __global__ __launch_bounds__(64) void k_gated_none(GatedArgs a, const float* in,
     if (c >= a.C) return;
     if (!a.cu && out)
         for (int s = blockIdx.y; s < a.S; s += gridDim.y) out[(size_t)s * a.C + c] = in ? in[(size_t)s * a.C + c] : 0.f;
-    if (a.drate && blockIdx.y == 0) a.drate[c] = 0.f;
+    if (a.drate && blockIdx.y == 0) a.drate[c] = 0.f / rate_of(a.rate[c]);
 }
 
 // V entries of a row, next to each other and aligned as one.

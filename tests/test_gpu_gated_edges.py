@@ -55,6 +55,18 @@ def test_rates_that_are_not_positive_and_finite(bounds, dtype, C):
         assert torch.isnan(v[:, bad]).all() and torch.equal(v[:, rest], v0[:, rest])
 
 
+def test_bad_rates_without_rows():
+    """drate says so where no row does: in chunks of a call whose sequences are all empty, and in a call without rows."""
+    rate = torch.tensor([0.5, 0.0, -1.0, math.inf, math.nan], device=DEV)
+    for T in (0, 100, 300):
+        z, cu = torch.randn(T, 5, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+        h0 = torch.randn(2, 5, device=DEV)
+        _, fin, saved = pdssm.gated_fwd(z, z, z, rate, cu=cu, h0=h0)
+        got = pdssm.gated_bwd(z, z, z, rate, saved, z, cu=cu, h0=h0, dh_final=h0)
+        assert torch.equal(fin, h0) and torch.equal(got[4], h0)
+        assert got[3][0] == 0 and torch.isnan(got[3][1:]).all()
+
+
 # ---- rows behind the last sequence -----------------------------------------
 
 @pytest.mark.parametrize("dtype,C", [(torch.float32, 33), (torch.bfloat16, 65), (torch.bfloat16, 66), (torch.float32, 64)])
