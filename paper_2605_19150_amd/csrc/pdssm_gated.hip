@@ -561,7 +561,8 @@ __global__ __launch_bounds__(kWaves * 64, 6) void k_gated_fwd(GatedArgs a) {
             if (more && !cut) put_word(mine + lane, state_word(fmaf(At, h, Bt)));
         }
         entry[lane] = h;
-        if (a.saved && live && (kinds.used & 1)) a.saved[(size_t)k * a.C + c] = h;
+        const bool used = kinds.used & 1;
+        if (a.saved && live && (used || rest(0))) a.saved[(size_t)k * a.C + c] = used ? h : 0.f;
     }
     __syncthreads();
     float h = entry[lane];

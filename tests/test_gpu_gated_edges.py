@@ -79,9 +79,9 @@ def test_rows_behind_the_last_sequence_are_zero(bounds, T, dtype, C):
     for t in (case.x, case.ga, case.gi, case.dy):
         t[end:] = math.nan
     n = T * C
-    _dirty(n, 2 * n, 4 * n, 6 * n, 12 * n, -(-T // 32) * C)
+    _dirty(n, 2 * n, 4 * n, 6 * n, 12 * n, -(-T // 32) * C, -(-T // 128) * C * 4)
     y, fin, saved, kept = case.fwd(hold8=True)
-    assert (y[end:] == 0).all()
+    assert (y[end:] == 0).all() and (saved[-(-end // 128):] == 0).all()
     for q, e in kept:
         assert (q[end:] == 0).all() and (e[first:] == -126).all()
         assert (pdssm.unpack8((q, e))[end:] == 0).all()
