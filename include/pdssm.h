@@ -560,6 +560,132 @@ size_t pdssm_project_wgrad_workspace_size(int32_t T, int32_t M, int32_t Dm);
 int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, const int8_t* q, const int8_t* e,
                         float* dW, void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Linear attention with a decay for each head.  A layer whose state is a
+ * matrix: head h has the state S [Dk, Dv] and, with a = exp(-rate[h]),
+ *
+ *   S_t = a S_{t-1} + k_t v_t^T,      o_t = scale * S_t^T q_t,
+ *
+ * that is o_t = scale * sum_{j<=t} a^(t-j) (q_t . k_j) v_j.  The operators below
+ * run it over whole sequences (in chunks, on the matrix cores), forward and
+ * backward, and one token at a time.
+ *
+ * Rows.  q, k [T, heads, Dk] and v [T, heads, Dv], o and do [T, H, Dv]: fp32, or
+ * bf16 with PDSSM_FLAG_BF16_IO in desc->flags.  Inputs may be parts of wider
+ * rows, and a stride may be 0 (rows that are alike): pdssm_heads.  There are H
+ * states, decays and output heads; q, k and v have Hq, Hk and Hv heads, which divide
+ * H, and head h reads head h / (H / Hq) of q, and so on: keys and values that
+ * query heads share, or queries and keys that heads of values share.  The gradient of a shared
+ * head is the sum over those that read it.  Any Dk and Dv from 1 to 256, alignment
+ * of an entry; 16-byte aligned rows of multiples of 16 bytes are the fast ones.
+ * States (h0, h_final, dh_final, dh0) are fp32 [S, H, Dk, Dv], and so are rate and all
+ * sums.  With bf16 rows the products run on bf16 numbers: the rows, which are
+ * exact in it, and states, weighted rows and weighted scores each as the sum of two such numbers,
+ * off by at most 2^-17 of themselves.  Outputs are rounded once, to nearest even.
+ *
+ * Sequences are as for the gated layers: S of T / S rows each, or cu [S+1], and
+ * some may have no rows (h_final = h0, dh0 = dh_final, zeros where those are NULL).
+ * Output rows behind the last sequence are zeros.  A cu that breaks the rule is reported as PDSSM_ERR_INDEX
+ * in *dev_status; every access stays in bounds and the results mean nothing.
+ *
+ * rate [H] must not be negative and must be finite, 0 is no decay: any other value gives
+ * NaN in that head's rows and states, and in no other head.  The rates are
+ * constants of the layer: there is no gradient of them.
+ *
+ * A row depends on no later one, whatever that holds, NaN and infinities too
+ * (and the gradient of a row on no earlier do): rows that hold such values are computed one
+ * by one, with those behind them in their segment, many times slower.
+ *
+ * Results are deterministic, but depend in their last bits on how many rows and
+ * heads a call has: long sequences of few heads are cut into segments. */
+typedef struct pdssm_heads {
+    const void* p;  /* entry (t, head, d) at p + t*ld + head*hs + d */
+    int64_t ld;     /* entries from one row to the next, 0 <= ld <= 2^24 */
+    int64_t hs;     /* entries from one head to the next, 0 <= hs <= 2^40 */
+} pdssm_heads;
+
+typedef struct pdssm_attn_desc {
+    /* rows, sequences; heads of the states, of q, k and v; entries of q and k, of v.
+     * 0 <= T <= 2^30, 1 <= S <= 2^30, 1 <= H <= 65535, and launches below 2^32
+     * threads, else PDSSM_ERR_UNSUPPORTED */
+    int32_t T, S, H, Hq, Hk, Hv, Dk, Dv;
+    float scale;     /* finite */
+    uint32_t flags;  /* PDSSM_FLAG_BF16_IO or 0 */
+} pdssm_attn_desc;
+
+/* Workspace bytes of pdssm_decay_attn_fwd (PDSSM_OP_FWD) or pdssm_decay_attn_bwd
+ * (PDSSM_OP_BWD); packed: whether the call has a cu.  (size_t)-1 if desc or op is
+ * invalid or the sizes are not supported. */
+size_t pdssm_decay_attn_workspace_size(const pdssm_attn_desc* desc, int packed, int op);
+
+/*
+ * Forward.  In: q, k, v; rate; cu and h0 (optional).  Out: o; optional h_final.
+ * ws: pdssm_decay_attn_workspace_size bytes, 256-byte aligned (0: none).
+ */
+int pdssm_decay_attn_fwd(const pdssm_attn_desc* desc, const pdssm_heads* q, const pdssm_heads* k, const pdssm_heads* v,
+                         const float* rate, const int32_t* cu, const float* h0, void* o, float* h_final, void* ws,
+                         size_t ws_bytes, int* dev_status, void* stream);
+
+/*
+ * Backward: the vector-Jacobian product of the forward, from its inputs.  With
+ * G_t = scale q_t do_t^T + a G_{t+1} (dh_final behind a sequence's last row),
+ *   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t,   dh0 = a G_1.
+ * In: q, k, v, rate, cu, h0 as in the forward; dout rows; dh_final (optional).
+ * Out: dq [T, Hq, Dk], dk [T, Hk, Dk], dv [T, Hv, Dv], dense; optional dh0.
+ */
+int pdssm_decay_attn_bwd(const pdssm_attn_desc* desc, const pdssm_heads* q, const pdssm_heads* k, const pdssm_heads* v,
+                         const pdssm_heads* dout, const float* rate, const int32_t* cu, const float* h0, const float* dh_final,
+                         void* dq, void* dk, void* dv, float* dh0, void* ws, size_t ws_bytes, int* dev_status, void* stream);
+
+/*
+ * One token of each of desc->T sequences (generation), in fp32: desc->S is the number of
+ * states in the pool h_in, h_out [S, H, Dk, Dv].  slots, skipped rows, errors and
+ * h_out as for pdssm_gated_step.  o [T, H, Dv].  T <= 65535, else
+ * PDSSM_ERR_UNSUPPORTED.
+ */
+int pdssm_decay_attn_step(const pdssm_attn_desc* desc, const pdssm_heads* q, const pdssm_heads* k, const pdssm_heads* v,
+                          const float* rate, const int32_t* slots, const float* h_in, float* h_out, void* o, int* dev_status,
+                          void* stream);
+
+/* ------------------------------------------------------------------------
+ * Group norm of rows, channels last, with an activation or a gate behind it, as
+ * it ends a layer of heads.  Each row's C channels are G groups of neighbours,
+ * and with a group's mean and variance (of that row alone: a token depends on no other)
+ *
+ *   u = (x - mean) / sqrt(var + eps) * weight + bias,
+ *   y = f(u), or with a gate u * f(gate),   f(z) = z or silu(z) = z sigmoid(z).
+ *
+ * x, gate, y, dy and the gradients are rows [T, C], fp32 or with
+ * PDSSM_FLAG_BF16_IO bf16; inputs may be parts of wider rows.  weight and bias [C]
+ * are fp32, NULL stands for ones and zeros; all arithmetic is fp32, row outputs are
+ * rounded once.  A silu whose argument is under -88 (also -inf and the
+ * type's lowest value: a shut gate) is 0, and its slope too; a NaN or an infinity
+ * in x gives NaN in its group's row and in no other, in the gradients of weight and bias in its
+ * columns of the group.  0 <= T <= 2^30, 1 <= C <= 2^24, min(T, 512) * G < 2^24,
+ * else PDSSM_ERR_UNSUPPORTED.  Results are deterministic. */
+#define PDSSM_ACT_NONE 0
+#define PDSSM_ACT_SILU 1
+
+typedef struct pdssm_norm_desc {
+    int32_t T, C, G; /* rows, channels, groups (G divides C) */
+    int32_t act;     /* PDSSM_ACT_NONE or PDSSM_ACT_SILU */
+    float eps;       /* finite, not negative */
+    uint32_t flags;  /* PDSSM_FLAG_BF16_IO or 0 */
+} pdssm_norm_desc;
+
+int pdssm_group_norm(const pdssm_norm_desc* desc, const pdssm_rows* x, const pdssm_rows* gate, const float* weight,
+                     const float* bias, void* y, void* stream);
+
+/*
+ * Its gradients: dx, and with a gate dgate [T, C]; optional dweight and dbias [C]
+ * fp32 (sums over all rows; ws: pdssm_group_norm_workspace_size bytes, 256-byte
+ * aligned, if there is one of them).
+ */
+size_t pdssm_group_norm_workspace_size(const pdssm_norm_desc* desc);
+int pdssm_group_norm_bwd(const pdssm_norm_desc* desc, const pdssm_rows* x, const pdssm_rows* gate, const pdssm_rows* dy,
+                         const float* weight, const float* bias, void* dx, void* dgate, float* dweight, float* dbias, void* ws,
+                         size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

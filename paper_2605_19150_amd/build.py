@@ -14,6 +14,10 @@ LIB = os.path.join(PKG, "libpdssm.so")
 # state size N so that the sizes build in parallel.
 SOURCES = [("pdssm_fused.hip", ["-DPDSSM_N=%d" % n], "pdssm_fused_n%d" % n)
            for n in (64, 128, 256, 32, 16, 8)] + [
+    # and the attention scan once per length of a head's rows
+    ("pdssm_attn_scan.hip", ["-DPDSSM_DC=%d" % n], "pdssm_attn_scan_d%d" % n) for n in (256, 128, 64)] + [
+    ("pdssm_attn.hip", [], "pdssm_attn"),
+    ("pdssm_norm.hip", [], "pdssm_norm"),
     ("pdssm_chunked.hip", [], "pdssm_chunked"),
     ("pdssm_ste.hip", [], "pdssm_ste"),
     ("pdssm_decode.hip", [], "pdssm_decode"),

@@ -7,11 +7,15 @@
 
 #include <initializer_list>
 
+#include <math.h>
+
+#include "pdssm_attn.h"
 #include "pdssm_decode.h"
 #include "pdssm_select.h"
 #include "pdssm_fused.h"
 #include "pdssm_gated.h"
 #include "pdssm_internal.h"
+#include "pdssm_norm.h"
 
 namespace {
 
@@ -418,6 +422,59 @@ pdssm::RowsIn rows_in(const pdssm_rows* r) { return {r->p, r->ld, r->e}; }
 // The layout of sequences: equal lengths, or cu.
 bool bad_sequences(const pdssm_gated_desc* d, const int32_t* cu) {
     return cu ? misaligned4(cu) : d->T % d->S != 0;
+}
+
+// ------------------------------------------------------------------ attention with a decay for each head
+int check_attn(const pdssm_attn_desc* d) {
+    if (!d || (d->flags & ~PDSSM_FLAG_BF16_IO) != 0 || !(fabsf(d->scale) < INFINITY)) return PDSSM_ERR_INVALID_ARG;
+    if (d->T < 0 || d->S < 1 || d->H < 1 || d->Dk < 1 || d->Dv < 1) return PDSSM_ERR_INVALID_ARG;
+    for (int n : {d->Hq, d->Hk, d->Hv})
+        if (n < 1 || d->H % n != 0) return PDSSM_ERR_INVALID_ARG;
+    if (d->T > (1 << 30) || d->S > (1 << 30) || d->H > 65535 || d->Dk > pdssm::kAttnMaxDim || d->Dv > pdssm::kAttnMaxDim)
+        return PDSSM_ERR_UNSUPPORTED;
+    return PDSSM_OK;
+}
+
+constexpr int64_t kMaxStride = 1LL << 40;  // entries; offsets of rows stay below 2^63 bytes with it
+
+// Heads' rows that the kernels may read: not NULL unless there are none.
+bool bad_heads(const pdssm_heads* r, int T, size_t w) {
+    if (!r || r->ld < 0 || r->ld > kMaxLd || r->hs < 0 || r->hs > kMaxStride) return true;
+    return T > 0 && (!r->p || misaligned_to(r->p, w));
+}
+Range heads_range(const pdssm_heads* r, int T, int heads, int D, size_t w) {
+    return {r->p, T > 0 ? ((size_t)(T - 1) * r->ld + (size_t)(heads - 1) * r->hs + D) * w : 0};
+}
+pdssm::HeadsIn heads_in(const pdssm_heads* r, int H, int heads) { return {r->p, r->ld, r->hs, H / heads}; }
+
+// What both directions have.
+pdssm::AttnArgs attn_args(const pdssm_attn_desc* d, bool packed) {
+    pdssm::AttnArgs a = {};
+    a.T = d->T;
+    a.S = d->S;
+    a.H = d->H;
+    a.Dk = d->Dk;
+    a.Dv = d->Dv;
+    a.L = packed ? 0 : d->T / d->S;
+    a.io = d->flags & PDSSM_FLAG_BF16_IO ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.scale = d->scale;
+    a.q.share = d->H / d->Hq;
+    a.k.share = d->H / d->Hk;
+    a.v.share = d->H / d->Hv;
+    static const int32_t some = 0;
+    a.cu = packed ? &some : nullptr;  // only whether there is one counts for the sizes
+    return a;
+}
+
+size_t attn_state_bytes(const pdssm_attn_desc* d) { return (size_t)d->S * d->H * d->Dk * d->Dv * 4; }
+
+// ------------------------------------------------------------------ group norm
+int check_norm(const pdssm_norm_desc* d) {
+    if (!d || (d->flags & ~PDSSM_FLAG_BF16_IO) != 0 || (d->act != PDSSM_ACT_NONE && d->act != PDSSM_ACT_SILU))
+        return PDSSM_ERR_INVALID_ARG;
+    if (d->T < 0 || d->C < 1 || d->G < 1 || d->C % d->G != 0 || !(d->eps >= 0.f && d->eps < INFINITY)) return PDSSM_ERR_INVALID_ARG;
+    if (d->T > (1 << 30) || d->C > kMaxLd || !pdssm::norm_fits(d->T, d->C, d->G)) return PDSSM_ERR_UNSUPPORTED;
+    return PDSSM_OK;
 }
 
 }  // namespace
@@ -1046,6 +1103,205 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
         return PDSSM_ERR_INVALID_ARG;
     pdssm::WgradArgs a = {T, M, Dm, dP, q, e, dW, ws};
     return pdssm::launch_wgrad(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+size_t pdssm_decay_attn_workspace_size(const pdssm_attn_desc* d, int packed, int op) {
+    if (check_attn(d) != PDSSM_OK || (op != PDSSM_OP_FWD && op != PDSSM_OP_BWD)) return (size_t)-1;
+    const pdssm::AttnArgs a = attn_args(d, packed != 0);
+    if (!pdssm::attn_fits(a, op == PDSSM_OP_BWD)) return (size_t)-1;
+    return pdssm::attn_workspace(a, op == PDSSM_OP_BWD);
+}
+
+int pdssm_decay_attn_fwd(const pdssm_attn_desc* d, const pdssm_heads* q, const pdssm_heads* k, const pdssm_heads* v,
+                         const float* rate, const int32_t* cu, const float* h0, void* o, float* h_final, void* ws,
+                         size_t ws_bytes, int* dev_status, void* stream) {
+    const int st = check_attn(d);
+    if (st != PDSSM_OK) return st;
+    const int T = d->T;
+    const size_t w = row_bytes(d->flags), ns = attn_state_bytes(d);
+    for (const pdssm_heads* r : {q, k, v})
+        if (bad_heads(r, T, w)) return PDSSM_ERR_INVALID_ARG;
+    if (!rate || (!cu && T % d->S != 0) || (T > 0 && (!o || misaligned_to(o, w)))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)rate, (const void*)cu, (const void*)h0, (const void*)h_final, (const void*)dev_status})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    pdssm::AttnArgs a = attn_args(d, cu != nullptr);
+    if (!pdssm::attn_fits(a, false)) return PDSSM_ERR_UNSUPPORTED;
+    const size_t need = pdssm::attn_workspace(a, false);
+    if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
+    if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{o, (size_t)T * d->H * d->Dv * w}, {h_final, ns}, {ws, need}},
+                    {heads_range(q, T, d->Hq, d->Dk, w), heads_range(k, T, d->Hk, d->Dk, w), heads_range(v, T, d->Hv, d->Dv, w),
+                     {rate, (size_t)d->H * 4}, {cu, ((size_t)d->S + 1) * 4}, {h0, ns}}))
+        return PDSSM_ERR_INVALID_ARG;
+    a.q = heads_in(q, d->H, d->Hq);
+    a.k = heads_in(k, d->H, d->Hk);
+    a.v = heads_in(v, d->H, d->Hv);
+    a.rate = rate;
+    a.cu = cu;
+    a.h0 = h0;
+    a.status = dev_status;
+    a.ws = ws;
+    a.o = o;
+    a.h_final = h_final;
+    return pdssm::launch_attn_fwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+int pdssm_decay_attn_bwd(const pdssm_attn_desc* d, const pdssm_heads* q, const pdssm_heads* k, const pdssm_heads* v,
+                         const pdssm_heads* dout, const float* rate, const int32_t* cu, const float* h0, const float* dh_final,
+                         void* dq, void* dk, void* dv, float* dh0, void* ws, size_t ws_bytes, int* dev_status, void* stream) {
+    const int st = check_attn(d);
+    if (st != PDSSM_OK) return st;
+    const int T = d->T;
+    const size_t w = row_bytes(d->flags), ns = attn_state_bytes(d);
+    for (const pdssm_heads* r : {q, k, v, dout})
+        if (bad_heads(r, T, w)) return PDSSM_ERR_INVALID_ARG;
+    if (!rate || (!cu && T % d->S != 0)) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)dq, (const void*)dk, (const void*)dv})
+        if (T > 0 && (!p || misaligned_to(p, w))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)rate, (const void*)cu, (const void*)h0, (const void*)dh_final, (const void*)dh0,
+                          (const void*)dev_status})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    pdssm::AttnArgs a = attn_args(d, cu != nullptr);
+    if (!pdssm::attn_fits(a, true)) return PDSSM_ERR_UNSUPPORTED;
+    const size_t need = pdssm::attn_workspace(a, true);
+    if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
+    if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{dq, (size_t)T * d->Hq * d->Dk * w}, {dk, (size_t)T * d->Hk * d->Dk * w}, {dv, (size_t)T * d->Hv * d->Dv * w},
+                     {dh0, ns}, {ws, need}},
+                    {heads_range(q, T, d->Hq, d->Dk, w), heads_range(k, T, d->Hk, d->Dk, w), heads_range(v, T, d->Hv, d->Dv, w),
+                     heads_range(dout, T, d->H, d->Dv, w), {rate, (size_t)d->H * 4}, {cu, ((size_t)d->S + 1) * 4}, {h0, ns},
+                     {dh_final, ns}}))
+        return PDSSM_ERR_INVALID_ARG;
+    a.q = heads_in(q, d->H, d->Hq);
+    a.k = heads_in(k, d->H, d->Hk);
+    a.v = heads_in(v, d->H, d->Hv);
+    a.dout = heads_in(dout, d->H, d->H);
+    a.rate = rate;
+    a.cu = cu;
+    a.h0 = h0;
+    a.status = dev_status;
+    a.ws = ws;
+    a.dhf = dh_final;
+    a.dq = dq;
+    a.dk = dk;
+    a.dv = dv;
+    a.dh0 = dh0;
+    return pdssm::launch_attn_bwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+int pdssm_decay_attn_step(const pdssm_attn_desc* d, const pdssm_heads* q, const pdssm_heads* k, const pdssm_heads* v,
+                          const float* rate, const int32_t* slots, const float* h_in, float* h_out, void* o, int* dev_status,
+                          void* stream) {
+    const int st = check_attn(d);
+    if (st != PDSSM_OK) return st;
+    const int B = d->T;
+    const size_t w = row_bytes(d->flags), ns = attn_state_bytes(d), no = (size_t)B * d->H * d->Dv * w;
+    if (B > 65535 || !pdssm::attn_step_fits(B, d->H, d->Dv)) return PDSSM_ERR_UNSUPPORTED;  // grid
+    for (const pdssm_heads* r : {q, k, v})
+        if (bad_heads(r, B, w)) return PDSSM_ERR_INVALID_ARG;
+    if (!slots && B > d->S) return PDSSM_ERR_INVALID_ARG;
+    if (!rate || !h_in || !h_out || (B > 0 && (!o || misaligned_to(o, w)))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)rate, (const void*)slots, (const void*)h_in, (const void*)h_out, (const void*)dev_status})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{h_out, ns}, {o, no}},
+                    {heads_range(q, B, d->Hq, d->Dk, w), heads_range(k, B, d->Hk, d->Dk, w), heads_range(v, B, d->Hv, d->Dv, w),
+                     {rate, (size_t)d->H * 4}, {slots, (size_t)B * 4}}) ||
+        overlap({h_in, ns}, {o, no}) || (h_in != h_out && overlap({h_in, ns}, {h_out, ns})))
+        return PDSSM_ERR_INVALID_ARG;
+    if (B == 0) return PDSSM_OK;
+    pdssm::AttnStepArgs a = {};
+    a.B = B;
+    a.pool = d->S;
+    a.H = d->H;
+    a.Dk = d->Dk;
+    a.Dv = d->Dv;
+    a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.scale = d->scale;
+    a.q = heads_in(q, d->H, d->Hq);
+    a.k = heads_in(k, d->H, d->Hk);
+    a.v = heads_in(v, d->H, d->Hv);
+    a.rate = rate;
+    a.slots = slots;
+    a.h_in = h_in;
+    a.h_out = h_out;
+    a.o = o;
+    a.status = dev_status;
+    return pdssm::launch_attn_step(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+int pdssm_group_norm(const pdssm_norm_desc* d, const pdssm_rows* x, const pdssm_rows* gate, const float* weight,
+                     const float* bias, void* y, void* stream) {
+    const int st = check_norm(d);
+    if (st != PDSSM_OK) return st;
+    const int T = d->T, C = d->C;
+    const size_t w = row_bytes(d->flags), nc = (size_t)C * 4;
+    if (bad_rows(x, T, C, w) || x->e || (gate && (bad_rows(gate, T, C, w) || gate->e))) return PDSSM_ERR_INVALID_ARG;
+    if (T > 0 && (!y || misaligned_to(y, w))) return PDSSM_ERR_INVALID_ARG;
+    if (misaligned4(weight) || misaligned4(bias)) return PDSSM_ERR_INVALID_ARG;
+    const pdssm_rows none = {nullptr, C, nullptr};
+    if (!gate) gate = &none;
+    if (any_overlap({{y, (size_t)T * C * w}}, {rows_range(x, T, C, w), rows_range(gate, T, C, w), {weight, nc}, {bias, nc}}))
+        return PDSSM_ERR_INVALID_ARG;
+    pdssm::NormArgs a = {};
+    a.T = T;
+    a.C = C;
+    a.G = d->G;
+    a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.silu = d->act == PDSSM_ACT_SILU;
+    a.eps = d->eps;
+    a.x = rows_in(x);
+    a.gate = rows_in(gate);
+    a.w = weight;
+    a.b = bias;
+    a.y = y;
+    return pdssm::launch_norm_fwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
+}
+
+size_t pdssm_group_norm_workspace_size(const pdssm_norm_desc* d) {
+    return check_norm(d) == PDSSM_OK ? pdssm::norm_workspace(d->T, d->C, d->G) : (size_t)-1;
+}
+
+int pdssm_group_norm_bwd(const pdssm_norm_desc* d, const pdssm_rows* x, const pdssm_rows* gate, const pdssm_rows* dy,
+                         const float* weight, const float* bias, void* dx, void* dgate, float* dweight, float* dbias, void* ws,
+                         size_t ws_bytes, void* stream) {
+    const int st = check_norm(d);
+    if (st != PDSSM_OK) return st;
+    const int T = d->T, C = d->C;
+    const size_t w = row_bytes(d->flags), nc = (size_t)C * 4, n = (size_t)T * C * w;
+    if (bad_rows(x, T, C, w) || x->e || bad_rows(dy, T, C, w) || dy->e || (gate && (bad_rows(gate, T, C, w) || gate->e)))
+        return PDSSM_ERR_INVALID_ARG;
+    if (T > 0 && (!dx || misaligned_to(dx, w) || (gate && (!dgate || misaligned_to(dgate, w))))) return PDSSM_ERR_INVALID_ARG;
+    for (const void* p : {(const void*)weight, (const void*)bias, (const void*)dweight, (const void*)dbias})
+        if (misaligned4(p)) return PDSSM_ERR_INVALID_ARG;
+    const pdssm_rows none = {nullptr, C, nullptr};
+    if (!gate) {
+        gate = &none;
+        dgate = nullptr;
+    }
+    const size_t need = dweight || dbias ? pdssm::norm_workspace(T, C, d->G) : 0;
+    if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
+    if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
+    if (any_overlap({{dx, n}, {dgate, n}, {dweight, nc}, {dbias, nc}, {ws, need}},
+                    {rows_range(x, T, C, w), rows_range(gate, T, C, w), rows_range(dy, T, C, w), {weight, nc}, {bias, nc}}))
+        return PDSSM_ERR_INVALID_ARG;
+    pdssm::NormArgs a = {};
+    a.T = T;
+    a.C = C;
+    a.G = d->G;
+    a.io = w == 2 ? pdssm::kRowBf16 : pdssm::kRowF32;
+    a.silu = d->act == PDSSM_ACT_SILU;
+    a.eps = d->eps;
+    a.x = rows_in(x);
+    a.gate = rows_in(gate);
+    a.dy = rows_in(dy);
+    a.w = weight;
+    a.b = bias;
+    a.dx = dx;
+    a.dgate = dgate;
+    a.dw = dweight;
+    a.db = dbias;
+    a.part = static_cast<float*>(ws);
+    return pdssm::launch_norm_bwd(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PDSSM_OK : PDSSM_ERR_HIP;
 }
 
 }  // extern "C"

@@ -1,0 +1,393 @@
+// pdssm_attn.hip -- linear attention with a decay for each head: the launches
+// of whole sequences, and the step of one token.
+//
+// With S_t = a S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t and G_t the gradient
+// that reaches S_t (G_t = scale q_t do_t^T + a G_{t+1}) the gradients are
+//   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t:
+// the forward scan with (do, v, k) in the places of (q, k, v), and two scans from the
+// last row to the first with (v, do, q) and (k, q, do).  One kernel has all four
+// (pdssm_attn_scan.hip); the three of a backward pass run in one launch where
+// their rows have one length, as neighbours that share what they read.
+//
+// Where sequences and heads are too few to fill the card a sequence is cut into
+// segments: a first launch adds up what the rows of each segment do to the state
+// (it reads k and v once more), k_segments joins them, and the scan begins every
+// segment from its state.  Nothing waits for another workgroup, sums have one order.
+#include <math.h>
+
+#include "pdssm_attn.h"
+#include "pdssm_device.h"
+#include "pdssm_rows.h"
+
+namespace pdssm {
+
+namespace {
+
+constexpr int kFill = 512;      // workgroups that fill the card: two on each of 256 CUs
+constexpr int kSegmentMin = 256;  // rows below which a segment is not worth its state
+
+struct Plan {
+    int seg_rows, items;
+    int64_t slots;  // states that segments begin with; 0: no sequence is cut
+};
+
+int slices(int cols, bool wide) { return (cols + (wide ? 127 : 63)) / (wide ? 128 : 64); }
+bool wide_cols(const AttnArgs& a, bool bwd) { return (bwd ? max(a.Dk, a.Dv) : a.Dv) > 64 && max(a.Dk, a.Dv) <= 128; }
+int members(const AttnArgs& a, bool bwd) {
+    const bool wide = wide_cols(a, bwd);
+    return bwd ? 2 * slices(a.Dk, wide) + slices(a.Dv, wide) : slices(a.Dv, wide);
+}
+
+Plan plan(const AttnArgs& a, bool bwd) {
+    const int chunk = a.io == kRowBf16 ? 64 : 32;
+    const int64_t heads = (int64_t)a.H * members(a, bwd);
+    Plan p = {};
+    if (!a.cu) {
+        const int64_t whole = a.S * heads;
+        int64_t n = whole >= kFill ? 1 : min((kFill + whole - 1) / whole, max((int64_t)a.L / kSegmentMin, (int64_t)1));
+        const int64_t rows = (max(a.L, 1) + n - 1) / n;
+        p.seg_rows = (int)((rows + chunk - 1) / chunk * chunk);
+        n = max((a.L + p.seg_rows - 1) / p.seg_rows, 1);
+        p.items = (int)(n * a.S);
+        p.slots = n > 1 ? a.T / p.seg_rows + 1 : 0;
+    } else {
+        // lengths are not known here: segments of what a workgroup has if all rows are shared out
+        int64_t rows = max((int64_t)kSegmentMin, (a.T * heads + kFill - 1) / kFill);
+        rows = min(rows, (int64_t)max(a.T, 1));
+        p.seg_rows = (int)((rows + chunk - 1) / chunk * chunk);
+        p.items = a.T / p.seg_rows + a.S;
+        p.slots = a.T > p.seg_rows ? a.T / p.seg_rows + 1 : 0;
+    }
+    return p;
+}
+
+size_t aligned(size_t n) { return (n + 255) / 256 * 256; }
+
+struct Space {
+    size_t states, dq, dk, dv, all;  // bytes of a set of states, of gradients for each state's head
+};
+Space space(const AttnArgs& a, const Plan& p, bool bwd) {
+    Space s = {};
+    s.states = aligned((size_t)p.slots * a.H * a.Dk * a.Dv * 4);
+    s.all = s.states * (bwd ? 2 : 1);
+    if (bwd) {
+        auto part = [&](const HeadsIn& x, int D) { return x.share > 1 ? aligned((size_t)a.T * a.H * D * 4) : 0; };
+        s.dq = part(a.q, a.Dk);
+        s.dk = part(a.k, a.Dk);
+        s.dv = part(a.v, a.Dv);
+        s.all += s.dq + s.dk + s.dv;
+    }
+    return s;
+}
+
+// From what the segments add to the states that they begin with.  x: those of the
+// sequences' first rows.  A workgroup has a part of one state of the sequence whose
+// second segment has the slot.
+__global__ __launch_bounds__(256) void k_segments(AttnScan a, int64_t slots) {
+    const AttnRole& R = a.role[blockIdx.z];
+    const int h = blockIdx.y, parts = (a.state + 255) / 256;
+    const int64_t slot = blockIdx.x / parts;
+    const int e = (int)(blockIdx.x % parts) * 256 + threadIdx.x;
+    int s;
+    int64_t begin, len;
+    if (a.cu) {
+        int lo = 0, n = a.S;
+        const int64_t row = slot * a.seg_rows;
+        while (n > 1) {  // the last sequence that begins at or before the slot's row
+            const int step = (n + 255) / 256, at = lo + (int)threadIdx.x * step;
+            const bool in = (int)threadIdx.x * step < n && min(max(a.cu[at], 0), a.T) <= row;
+            const int k = max(__syncthreads_count(in) - 1, 0);
+            n = min(step, n - k * step);
+            lo += k * step;
+        }
+        s = lo;
+        begin = min(max(a.cu[s], 0), a.T);
+        len = min(max(a.cu[s + 1], (int)begin), a.T) - begin;
+    } else {
+        s = (int)min(slot * a.seg_rows / a.L, (int64_t)a.S - 1);
+        begin = (int64_t)s * a.L;
+        len = a.L;
+    }
+    if (begin / a.seg_rows != slot - 1 || len <= a.seg_rows || e >= a.state) return;
+    const float rate = a.rate[h];
+    const float keep = rate >= 0.f && rate < INFINITY ? (float)exp(-(double)rate * a.seg_rows) : NAN;
+    float x = R.x0 ? R.x0[((size_t)s * a.H + h) * a.state + e] : 0.f;
+    const int n = (int)((len + a.seg_rows - 1) / a.seg_rows);
+    float* p = const_cast<float*>(R.seg) + ((size_t)slot * a.H + h) * a.state + e;
+    const size_t next = (size_t)a.H * a.state;
+    for (int seg = 1; seg < n; ++seg, p += next) *p = x = keep * x + *p;
+}
+
+// The gradient of a shared head: the sum over the states' heads that read it.
+template <int IO>
+__global__ __launch_bounds__(256) void k_share(const float* part, typename Entry<IO>::T* out, int64_t T, const int* cu, int S,
+                                               int heads, int share, int D) {
+    const int64_t rest = cu ? min((int64_t)max(cu[S], 0), T) : T, n = T * heads * D;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / D / heads;
+        float sum = 0.f;
+        if (row < rest) {
+            const float* p = part + (i / D) * share * D + i % D;
+            for (int r = 0; r < share; ++r) sum += p[(int64_t)r * D];
+        }
+        out[i] = Entry<IO>::put(sum);
+    }
+}
+
+__global__ __launch_bounds__(256) void k_bounds(const int* cu, int S, int T, int* status) {
+    bool bad = false;
+    for (int s = threadIdx.x; s <= S; s += 256) bad |= s == 0 ? cu[0] != 0 : cu[s] < cu[s - 1];
+    bad |= cu[S] > T;
+    if (bad) report_index_error(status);
+}
+
+hipError_t scan(const AttnScan& a, bool full, bool wide, hipStream_t s) {
+    const int Dc = a.role[0].Dc;
+    if (Dc <= 64) return launch_attn_scan<64>(a, full, wide, s);
+    if (Dc <= 128) return launch_attn_scan<128>(a, full, wide, s);
+    return launch_attn_scan<256>(a, full, wide, s);
+}
+int length_class(int Dc) { return Dc <= 64 ? 0 : Dc <= 128 ? 1 : 2; }
+
+AttnScan scan_args(const AttnArgs& a, const Plan& p) {
+    AttnScan n = {};
+    n.T = a.T;
+    n.S = a.S;
+    n.H = a.H;
+    n.L = a.L;
+    n.io = a.io;
+    n.seg_rows = p.seg_rows;
+    n.items = p.items;
+    n.state = a.Dk * a.Dv;
+    n.scale = a.scale;
+    n.rate = a.rate;
+    n.cu = a.cu;
+    n.groups = (int64_t)p.items * a.H;
+    return n;
+}
+
+void add_role(AttnScan& n, const AttnRole& r, bool wide) {
+    AttnRole& to = n.role[n.roles++];
+    to = r;
+    to.slices = slices(r.Do, wide);
+    n.members += to.slices;
+}
+
+// The states that segments begin with, of the roles in n.
+hipError_t begin_segments(const AttnScan& n, const Plan& p, bool wide, hipStream_t s) {
+    hipError_t e = scan(n, false, wide, s);
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)(p.slots * ((n.state + 255) / 256)), n.H, n.roles);
+    hipLaunchKernelGGL(k_segments, grid, dim3(256), 0, s, n, p.slots);
+    return hipGetLastError();
+}
+
+hipError_t check_bounds(const AttnArgs& a, hipStream_t s) {
+    if (!a.cu || !a.status) return hipSuccess;
+    hipLaunchKernelGGL(k_bounds, dim3(1), dim3(256), 0, s, a.cu, a.S, a.T, a.status);
+    return hipGetLastError();
+}
+
+template <int IO>
+hipError_t add_shared(const AttnArgs& a, const float* part, void* out, const HeadsIn& x, int D, hipStream_t s) {
+    const int64_t n = (int64_t)a.T * (a.H / x.share) * D;
+    if (x.share == 1 || n == 0) return hipSuccess;
+    const unsigned blocks = (unsigned)min((n + 255) / 256, (int64_t)8192);
+    hipLaunchKernelGGL(k_share<IO>, dim3(blocks), dim3(256), 0, s, part, static_cast<typename Entry<IO>::T*>(out), (int64_t)a.T, a.cu,
+                       a.S, a.H / x.share, x.share, D);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attn_workspace(const AttnArgs& a, bool bwd) { return space(a, plan(a, bwd), bwd).all; }
+
+bool attn_fits(const AttnArgs& a, bool bwd) {
+    const Plan p = plan(a, bwd);
+    const int64_t parts = ((int64_t)a.Dk * a.Dv + 255) / 256;
+    return ((int64_t)p.items * a.H + 7) * members(a, bwd) < (1 << 24) && p.slots * parts * a.H * 2 < (1 << 24);
+}
+
+hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s) {
+    const Plan p = plan(a, false);
+    const bool wide = wide_cols(a, false);
+    hipError_t e = check_bounds(a, s);
+    if (e != hipSuccess) return e;
+    AttnRole r = {};
+    r.q = a.q;
+    r.k = a.k;
+    r.v = a.v;
+    r.out = a.o;
+    r.x0 = a.h0;
+    r.seg = static_cast<const float*>(a.ws);
+    r.fin = a.h_final;
+    r.keep = a.h0;
+    r.Dc = a.Dk;
+    r.Do = a.Dv;
+    r.rs = a.Dv;
+    r.cs = 1;
+    AttnScan n = scan_args(a, p);
+    add_role(n, r, wide);
+    if (p.slots && (e = begin_segments(n, p, wide, s)) != hipSuccess) return e;
+    return scan(n, true, wide, s);
+}
+
+hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t s) {
+    const Plan p = plan(a, true);
+    const Space sp = space(a, p, true);
+    const bool wide = wide_cols(a, true);
+    hipError_t e = check_bounds(a, s);
+    if (e != hipSuccess) return e;
+    char* ws = static_cast<char*>(a.ws);
+    float* S = reinterpret_cast<float*>(ws);
+    float* G = reinterpret_cast<float*>(ws + sp.states);
+    ws += 2 * sp.states;
+    float* part[3] = {reinterpret_cast<float*>(ws), reinterpret_cast<float*>(ws + sp.dq), reinterpret_cast<float*>(ws + sp.dq + sp.dk)};
+    AttnRole dq = {}, dk = {}, dv = {}, fs = {};
+    dq.q = a.dout;
+    dq.k = a.v;
+    dq.v = a.k;
+    dq.out32 = a.q.share > 1;
+    dq.out = dq.out32 ? part[0] : a.dq;
+    dq.x0 = a.h0;
+    dq.seg = S;
+    dq.Dc = a.Dv;
+    dq.Do = a.Dk;
+    dq.rs = 1;
+    dq.cs = a.Dv;
+    dk = dq;
+    dk.q = a.v;
+    dk.k = a.dout;
+    dk.v = a.q;
+    dk.out32 = a.k.share > 1;
+    dk.out = dk.out32 ? part[1] : a.dk;
+    dk.x0 = a.dhf;
+    dk.seg = G;
+    dk.late = 1;
+    dv.q = a.k;
+    dv.k = a.q;
+    dv.v = a.dout;
+    dv.out32 = a.v.share > 1;
+    dv.out = dv.out32 ? part[2] : a.dv;
+    dv.x0 = a.dhf;
+    dv.seg = G;
+    dv.fin = a.dh0;
+    dv.keep = a.dhf;
+    dv.Dc = a.Dk;
+    dv.Do = a.Dv;
+    dv.rs = a.Dv;
+    dv.cs = 1;
+    dv.late = 1;
+    if (p.slots) {
+        fs = dv;  // the forward's states
+        fs.k = a.k;
+        fs.v = a.v;
+        fs.x0 = a.h0;
+        fs.seg = S;
+        fs.late = 0;
+        AttnScan n = scan_args(a, p);
+        add_role(n, fs, wide);
+        add_role(n, dv, wide);
+        if ((e = begin_segments(n, p, wide, s)) != hipSuccess) return e;
+    }
+    AttnScan n = scan_args(a, p);
+    add_role(n, dq, wide);
+    add_role(n, dk, wide);
+    if (length_class(a.Dk) == length_class(a.Dv)) {
+        add_role(n, dv, wide);
+    } else {
+        AttnScan m = scan_args(a, p);
+        add_role(m, dv, wide);
+        if ((e = scan(m, true, wide, s)) != hipSuccess) return e;
+    }
+    if ((e = scan(n, true, wide, s)) != hipSuccess) return e;
+    auto* add = a.io == kRowBf16 ? add_shared<kRowBf16> : add_shared<kRowF32>;
+    if ((e = add(a, part[0], a.dq, a.q, a.Dk, s)) != hipSuccess) return e;
+    if ((e = add(a, part[1], a.dk, a.k, a.Dk, s)) != hipSuccess) return e;
+    return add(a, part[2], a.dv, a.v, a.Dv, s);
+}
+
+// ---- one token -------------------------------------------------------------------------------------------------------
+
+namespace {
+
+// S' = a S + k v^T, o = scale S'^T q: the state is read and written once, and nothing
+// else counts.  TX threads beside each other have V columns each, 256 / TX rows are under way at a time.
+template <int IO, int V, int TX>
+__global__ __launch_bounds__(256) void k_attn_step(AttnStepArgs a) {
+    using En = Entry<IO>;
+    using T = typename En::T;
+    constexpr int TY = 256 / TX;
+    __shared__ float qs[kAttnMaxDim], ks[kAttnMaxDim];
+    __shared__ float sum[TY][TX * V + 1];
+    const int parts = (a.Dv + TX * V - 1) / (TX * V);
+    const int h = blockIdx.x / parts, b = blockIdx.y, tx = threadIdx.x % TX, ty = threadIdx.x / TX;
+    const int o = ((int)(blockIdx.x % parts) * TX + tx) * V;
+    int slot = b;
+    if (a.slots) {
+        slot = a.slots[b];
+        if (slot < 0 || slot >= a.pool) {
+            if (slot >= a.pool && threadIdx.x == 0) report_index_error(a.status);
+            return;
+        }
+    }
+    auto row = [&](const HeadsIn& r) { return static_cast<const T*>(r.p) + (int64_t)b * r.ld + (int64_t)(h / r.share) * r.hs; };
+    for (int c = threadIdx.x; c < a.Dk; c += 256) {
+        qs[c] = En::get(row(a.q)[c]);
+        ks[c] = En::get(row(a.k)[c]);
+    }
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = o + e < a.Dv ? En::get(row(a.v)[o + e]) : 0.f;
+    const float rate = a.rate[h];
+    const float decay = rate >= 0.f && rate < INFINITY ? (float)exp(-(double)rate) : NAN;
+    // the first row that names a slot has it; others of the same batch are refused
+    bool again = false;
+    if (a.slots)
+        for (int k = threadIdx.x; k < b; k += 256) again |= a.slots[k] == slot;
+    if (__syncthreads_or(again)) {
+        if (threadIdx.x == 0) report_index_error(a.status);
+        return;
+    }
+    const size_t at = ((size_t)slot * a.H + h) * a.Dk * a.Dv + o;
+    typedef float vec __attribute__((ext_vector_type(V)));
+    float acc[V] = {};
+    if (o < a.Dv) {
+#pragma unroll 4
+        for (int c = ty; c < a.Dk; c += TY) {
+            vec s = *reinterpret_cast<const vec*>(a.h_in + at + (size_t)c * a.Dv);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                s[e] = fmaf(decay, s[e], ks[c] * v[e]);
+                acc[e] = fmaf(qs[c], s[e], acc[e]);
+            }
+            *reinterpret_cast<vec*>(a.h_out + at + (size_t)c * a.Dv) = s;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[ty][tx * V + e] = acc[e];
+    __syncthreads();
+    const int c = threadIdx.x, col = (int)(blockIdx.x % parts) * TX * V + c;
+    if (c < TX * V && col < a.Dv) {
+        float x = 0.f;
+#pragma unroll
+        for (int r = 0; r < TY; ++r) x += sum[r][c];
+        static_cast<T*>(a.o)[((size_t)b * a.H + h) * a.Dv + col] = En::put(a.scale * x);
+    }
+}
+
+}  // namespace
+
+bool attn_step_fits(int B, int H, int Dv) { return (int64_t)B * H * ((Dv + 15) / 16) < (1 << 24); }
+
+hipError_t launch_attn_step(const AttnStepArgs& a, hipStream_t s) {
+    const bool four = a.Dv % 4 == 0 && reinterpret_cast<uintptr_t>(a.h_in) % 16 == 0 && reinterpret_cast<uintptr_t>(a.h_out) % 16 == 0;
+    const bool b = a.io == kRowBf16;
+    const int cols = four ? 32 : 16;
+    void (*f)(AttnStepArgs) = four ? (b ? k_attn_step<kRowBf16, 4, 8> : k_attn_step<kRowF32, 4, 8>)
+                                   : (b ? k_attn_step<kRowBf16, 1, 16> : k_attn_step<kRowF32, 1, 16>);
+    hipLaunchKernelGGL(f, dim3(a.H * ((a.Dv + cols - 1) / cols), a.B), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace pdssm

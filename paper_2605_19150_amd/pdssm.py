@@ -25,7 +25,13 @@ Gated recurrent layers (gated_fwd and the functions after it) take rows:
   of at most 2^24 entries, entries of a row next to each other.  rate [C] and
   the states [S,C] are float32.  What is returned for rows behind the last sequence
   (cu[S] < T) is zero.  Activations in the 8-bit form are pairs (q, e): int8
-  [T,C] and [ceil(T/32),C].  These functions run on the current stream of the
+  [T,C] and [ceil(T/32),C].
+Linear attention (decay_attn_fwd and the functions after it) takes heads' rows
+  q [B,L,Hq,Dk], k [B,L,Hk,Dk], v [B,L,Hv,Dv], or [T,heads,D] with cu; float32 or
+  bfloat16, parts of wider rows too (any steps from row to row and head to head,
+  the rows of a batch evenly spaced).  rate [H] and the states [S,H,Dk,Dv] are
+  float32; Hq, Hk and Hv divide H.  Group norm takes rows as the gated layers do.
+The functions of both kinds of layers run on the current stream of the
   tensors' device, or on the one given as stream, behind what the current stream
   has to do; who reads the results on another stream has to wait for that one.
 """
@@ -65,6 +71,20 @@ class Rows(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64), ("e", ctypes.c_void_p)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("ld", ctypes.c_int64), ("hs", ctypes.c_int64)]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "S", "H", "Hq", "Hk", "Hv", "Dk", "Dv")] + [
+        ("scale", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("C", ctypes.c_int32), ("G", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("flags", ctypes.c_uint32)]
+
+
 class GatedDesc(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("C", ctypes.c_int32), ("S", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
@@ -74,7 +94,9 @@ EXPORTS = ("pdssm_abi_version", "pdssm_chunk_len", "pdssm_num_chunks", "pdssm_wo
            "pdssm_scan_bwd", "pdssm_compose_chunks", "pdssm_scan_bwd_ste", "pdssm_ste_grads",
            "pdssm_softmax_vjp", "pdssm_decode_step", "pdssm_dict_argmax", "pdssm_route", "pdssm_project",
            "pdssm_gated_workspace_size", "pdssm_gated_fwd", "pdssm_gated_bwd", "pdssm_gated_step", "pdssm_pack8",
-           "pdssm_unpack8", "pdssm_project_wgrad_workspace_size", "pdssm_project_wgrad")
+           "pdssm_unpack8", "pdssm_project_wgrad_workspace_size", "pdssm_project_wgrad",
+           "pdssm_decay_attn_workspace_size", "pdssm_decay_attn_fwd", "pdssm_decay_attn_bwd", "pdssm_decay_attn_step",
+           "pdssm_group_norm", "pdssm_group_norm_workspace_size", "pdssm_group_norm_bwd")
 
 
 def lib_path():
@@ -136,6 +158,13 @@ def load():
     L.pdssm_unpack8.argtypes, L.pdssm_unpack8.restype = [I32, I32, U32, P, P, P, P], I
     L.pdssm_project_wgrad_workspace_size.argtypes, L.pdssm_project_wgrad_workspace_size.restype = [I32] * 3, Z
     L.pdssm_project_wgrad.argtypes, L.pdssm_project_wgrad.restype = [I32] * 3 + [P] * 5 + [Z, P], I
+    L.pdssm_decay_attn_workspace_size.argtypes, L.pdssm_decay_attn_workspace_size.restype = [P, I, I], Z
+    L.pdssm_decay_attn_fwd.argtypes, L.pdssm_decay_attn_fwd.restype = [P] * 10 + [Z, P, P], I
+    L.pdssm_decay_attn_bwd.argtypes, L.pdssm_decay_attn_bwd.restype = [P] * 14 + [Z, P, P], I
+    L.pdssm_decay_attn_step.argtypes, L.pdssm_decay_attn_step.restype = [P] * 11, I
+    L.pdssm_group_norm.argtypes, L.pdssm_group_norm.restype = [P] * 7, I
+    L.pdssm_group_norm_workspace_size.argtypes, L.pdssm_group_norm_workspace_size.restype = [P], Z
+    L.pdssm_group_norm_bwd.argtypes, L.pdssm_group_norm_bwd.restype = [P] * 11 + [Z, P], I
     if L.pdssm_abi_version() != 1:
         raise ImportError("libpdssm.so ABI version mismatch")
     _lib = L
@@ -994,3 +1023,222 @@ def project_wgrad(dP, u8, stream=None):
     s = _on(stream, dev, (dP, q, e, dW, ws))
     _done(load().pdssm_project_wgrad(T, M, Dm, dP_at, q_at, e_at, dW.data_ptr(), _at(ws), n, s), None, "pdssm_project_wgrad")
     return dW
+
+
+# ---- linear attention with a decay for each head ----------------------------
+
+_ATTN_DESC, _HEADS = struct.Struct("8ifI"), struct.Struct("Pqq")
+
+
+def _heads(t, name, dtype, lead, D, dev):
+    """(pdssm_heads, heads) of heads' rows [*lead, heads, D] that may be parts of wider rows."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    shape = t.shape
+    if len(shape) != len(lead) + 2 or shape[:-2] != lead or (D is not None and shape[-1] != D):
+        raise ValueError("%s must have shape (%s, heads, %s), got %s" % (name, ", ".join(map(str, lead)), D or "D", tuple(shape)))
+    if not t.is_cuda or t.device != dev:
+        raise ValueError("%s must be on %s" % (name, dev))
+    step = t.stride()
+    if step[-1] != 1 and shape[-1] > 1:
+        raise ValueError("%s: the entries of a row must be next to each other" % name)
+    ld = 0
+    if len(lead) == 2:
+        B, L = lead
+        if L > 1:
+            ld = step[1]
+            if B > 1 and step[0] != L * ld:
+                raise ValueError("%s: rows must be evenly spaced over the batch" % name)
+        elif B > 1:
+            ld = step[0]
+    elif lead[0] > 1:
+        ld = step[0]
+    return _HEADS.pack(t.data_ptr(), ld, step[-2] if shape[-2] > 1 else 0), shape[-2]
+
+
+def _attn(q, k, v, rate, scale, S, lead, T):
+    """(desc, pdssm_heads of q, k and v, address of rate, (H, Dk, Dv), device)."""
+    flags = _row_type(q)
+    dev = q.device
+    if not isinstance(rate, torch.Tensor) or rate.dim() != 1:
+        raise ValueError("rate must be [H]")
+    H = rate.shape[0]
+    rate_at = _tensor(rate, "rate", torch.float32, (H,), dev)
+    if not isinstance(v, torch.Tensor) or v.dim() != len(lead) + 2:
+        raise ValueError("v must be rows [%s,heads,D]" % ",".join("BL" if len(lead) == 2 else "T"))
+    Dk, Dv = q.shape[-1], v.shape[-1]
+    (q_at, hq), (k_at, hk), (v_at, hv) = (_heads(t, n, q.dtype, lead, D, dev)
+                                          for t, n, D in ((q, "q", Dk), (k, "k", Dk), (v, "v", Dv)))
+    for n, heads in (("q", hq), ("k", hk), ("v", hv)):
+        if heads < 1 or H % heads != 0:
+            raise ValueError("%s has %d heads, which do not divide the %d of rate" % (n, heads, H))
+    if not 1 <= Dk <= 256 or not 1 <= Dv <= 256:
+        raise ValueError("heads must have 1 to 256 entries, got %d and %d" % (Dk, Dv))
+    scale = Dk ** -0.5 if scale is None else float(scale)
+    if not abs(scale) < math.inf:
+        raise ValueError("scale must be finite")
+    _int32(T, S, H)
+    return _ATTN_DESC.pack(T, S, H, hq, hk, hv, Dk, Dv, scale, flags), (q_at, k_at, v_at), rate_at, (H, Dk, Dv), dev
+
+
+def _head_sequences(t, cu):
+    """(lead, T, S) of heads' rows t [B,L,heads,D], or [T,heads,D] with the bounds cu [S+1]."""
+    if not isinstance(t, torch.Tensor) or t.dim() != (4 if cu is None else 3):
+        raise ValueError("rows must be [B,L,heads,D], or [T,heads,D] with cu")
+    lead = t.shape[:-2]
+    if cu is None:
+        S, T = lead[0], lead[0] * lead[1]
+    else:
+        if not isinstance(cu, torch.Tensor) or cu.dim() != 1 or cu.shape[0] < 2:
+            raise ValueError("cu must be [S+1] with S >= 1")
+        S, T = cu.shape[0] - 1, lead[0]
+        _tensor(cu, "cu", torch.int32, (S + 1,), t.device)
+    if S < 1:
+        raise ValueError("rows need at least one sequence")
+    return lead, T, S
+
+
+def _attn_ws(desc, cu, op, dev):
+    n = load().pdssm_decay_attn_workspace_size(desc, cu is not None, op)
+    if n == OP_SIZE_ERROR:
+        raise PdssmError(ERR_UNSUPPORTED, "decay_attn_workspace_size")
+    return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+
+
+def _matrix_state(t, name, shape, dev):
+    return None if t is None else _tensor(t, name, torch.float32, shape, dev)
+
+
+@_on_its_device
+def decay_attn_fwd(q, k, v, rate, scale=None, cu=None, h0=None, check=True, stream=None):
+    """Linear attention with a decay for each head, over every sequence from its
+    state in h0 [S,H,Dk,Dv] (default 0): with a = exp(-rate[h]),
+    S_t = a S_{t-1} + k_t v_t^T and o_t = scale * S_t^T q_t (default scale
+    Dk**-0.5).  q, k and v may have fewer heads than the H of rate: head h reads
+    head h // (H / heads).  Returns (o [..,H,Dv] in the rows' type, h_final
+    [S,H,Dk,Dv]).  Rows behind the last sequence are zero.  check=False neither
+    synchronises nor reports a bad cu."""
+    lead, T, S = _head_sequences(q, cu)
+    d, rows, rate_at, (H, Dk, Dv), dev = _attn(q, k, v, rate, scale, S, lead, T)
+    h0_at = _matrix_state(h0, "h0", (S, H, Dk, Dv), dev)
+    o = q.new_empty((*lead, H, Dv))
+    h_final = rate.new_empty((S, H, Dk, Dv))
+    ws = _attn_ws(d, cu, OP_FWD, dev)
+    status = _status(check, dev)
+    s = _on(stream, dev, (q, k, v, rate, cu, h0, o, h_final, ws, status))
+    st = load().pdssm_decay_attn_fwd(d, *rows, rate_at, _at(cu), h0_at, o.data_ptr(), h_final.data_ptr(), _at(ws),
+                                     ws.numel() if ws is not None else 0, _at(status), s)
+    _done(st, status, "pdssm_decay_attn_fwd")
+    return o, h_final
+
+
+@_on_its_device
+def decay_attn_bwd(q, k, v, rate, do, scale=None, cu=None, h0=None, dh_final=None, check=True, stream=None):
+    """Gradients of decay_attn_fwd: (dq, dk, dv, dh0 [S,H,Dk,Dv]) from do (rows as
+    o) and dh_final [S,H,Dk,Dv] (default 0); the rest as in the forward.  dq, dk
+    and dv are dense, in the shapes of q, k and v; a head that several share has
+    the sum of theirs.  The rates are constants, there is no gradient of them."""
+    lead, T, S = _head_sequences(q, cu)
+    d, rows, rate_at, (H, Dk, Dv), dev = _attn(q, k, v, rate, scale, S, lead, T)
+    do_at, heads = _heads(do, "do", q.dtype, lead, Dv, dev)
+    if heads != H:
+        raise ValueError("do must have the %d heads of rate, got %d" % (H, heads))
+    h0_at, dhf_at = (_matrix_state(t, n, (S, H, Dk, Dv), dev) for t, n in ((h0, "h0"), (dh_final, "dh_final")))
+    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
+    dh0 = rate.new_empty((S, H, Dk, Dv))
+    ws = _attn_ws(d, cu, OP_BWD, dev)
+    status = _status(check, dev)
+    s = _on(stream, dev, (q, k, v, rate, do, cu, h0, dh_final, dq, dk, dv, dh0, ws, status))
+    st = load().pdssm_decay_attn_bwd(d, *rows, do_at, rate_at, _at(cu), h0_at, dhf_at, dq.data_ptr(), dk.data_ptr(),
+                                     dv.data_ptr(), dh0.data_ptr(), _at(ws), ws.numel() if ws is not None else 0,
+                                     _at(status), s)
+    _done(st, status, "pdssm_decay_attn_bwd")
+    return dq, dk, dv, dh0
+
+
+@_on_its_device
+def decay_attn_step(q, k, v, rate, h, scale=None, slots=None, out=None, o=None, check=True, stream=None):
+    """One token of decay_attn_fwd for each row of q [B,Hq,Dk], k [B,Hk,Dk] and
+    v [B,Hv,Dv]: returns (h_new [S,H,Dk,Dv], o [B,H,Dv]).  h [S,H,Dk,Dv] holds the
+    states; slots, out and skipped rows as in gated_step."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be [B,heads,D]")
+    if not isinstance(h, torch.Tensor) or h.dim() != 4:
+        raise ValueError("h must be [S,H,Dk,Dv]")
+    B, S = q.shape[0], h.shape[0]
+    d, rows, rate_at, (H, Dk, Dv), dev = _attn(q, k, v, rate, scale, S, q.shape[:1], B)
+    h_at = _tensor(h, "h", torch.float32, (S, H, Dk, Dv), dev)
+    out_at = h_at if out is None else _tensor(out, "out", torch.float32, (S, H, Dk, Dv), dev)
+    slots_at = None if slots is None else _tensor(slots, "slots", torch.int32, (B,), dev)
+    if o is None:
+        o = q.new_empty((B, H, Dv))
+    o_at = _tensor(o, "o", q.dtype, (B, H, Dv), dev)
+    status = _status(check, dev)
+    s = _on(stream, dev, (q, k, v, rate, h, out, slots, o, status))
+    st = load().pdssm_decay_attn_step(d, *rows, rate_at, slots_at, h_at, out_at, o_at, _at(status), s)
+    _done(st, status, "pdssm_decay_attn_step")
+    return h if out is None else out, o
+
+
+# ---- group norm --------------------------------------------------------------
+
+_NORM_DESC = struct.Struct("4ifI")
+_ACTS = {"none": 0, "silu": 1}
+
+
+def _norm(x, groups, weight, bias, gate, act, eps):
+    """(desc, rows of x, of gate or None, addresses of weight and bias, C, device)."""
+    flags = _row_type(x)
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [T,C] or [B,L,C]")
+    C, dev = x.shape[-1], x.device
+    T = math.prod(x.shape[:-1])
+    groups = int(groups)
+    if C < 1 or groups < 1 or C % groups != 0:
+        raise ValueError("groups must divide the %d channels, got %d" % (C, groups))
+    if act not in _ACTS:
+        raise ValueError("act must be 'none' or 'silu', got %r" % (act,))
+    eps = float(eps)
+    if not 0.0 <= eps < math.inf:
+        raise ValueError("eps must be finite and not negative")
+    _int32(T, C)
+    rows = _rows(x, "x", x.dtype, x.shape, dev)
+    gate_rows = None if gate is None else _rows(gate, "gate", x.dtype, x.shape, dev)
+    w_at, b_at = (None if t is None else _tensor(t, n, torch.float32, (C,), dev) for t, n in ((weight, "weight"), (bias, "bias")))
+    return _NORM_DESC.pack(T, C, groups, _ACTS[act], eps, flags), rows, gate_rows, w_at, b_at, C, dev
+
+
+@_on_its_device
+def group_norm(x, groups, weight=None, bias=None, gate=None, act="none", eps=1e-5, stream=None):
+    """Group norm of every row of x [T,C] or [B,L,C] over `groups` groups of
+    neighbouring channels, u = (x - mean) / sqrt(var + eps) * weight + bias, and
+    behind it act(u) or, with a gate (rows as x), u * act(gate); act is "none" or
+    "silu".  weight and bias [C] are float32.  Returns y, dense, in x's type."""
+    d, rows, gate_rows, w_at, b_at, _, dev = _norm(x, groups, weight, bias, gate, act, eps)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    s = _on(stream, dev, (x, weight, bias, gate, y))
+    _done(load().pdssm_group_norm(d, rows, gate_rows, w_at, b_at, y.data_ptr(), s), None, "pdssm_group_norm")
+    return y
+
+
+@_on_its_device
+def group_norm_bwd(x, dy, groups, weight=None, bias=None, gate=None, act="none", eps=1e-5, stream=None):
+    """Gradients of group_norm from dy (rows as y): (dx, dweight [C], dbias [C],
+    dgate); dgate is None without a gate, dweight and dbias without theirs."""
+    d, rows, gate_rows, w_at, b_at, C, dev = _norm(x, groups, weight, bias, gate, act, eps)
+    dy_rows = _rows(dy, "dy", x.dtype, x.shape, dev)
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    dgate = None if gate is None else torch.empty_like(dx)
+    dw, db = (None if t is None else torch.empty_like(t) for t in (weight, bias))
+    n = 0
+    if dw is not None or db is not None:
+        n = load().pdssm_group_norm_workspace_size(d)
+        if n == OP_SIZE_ERROR:
+            raise PdssmError(ERR_UNSUPPORTED, "group_norm_workspace_size")
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    s = _on(stream, dev, (x, dy, weight, bias, gate, dx, dgate, dw, db, ws))
+    _done(load().pdssm_group_norm_bwd(d, rows, gate_rows, dy_rows, w_at, b_at, dx.data_ptr(), _at(dgate), _at(dw), _at(db),
+                                      _at(ws), n, s), None, "pdssm_group_norm_bwd")
+    return dx, dw, db, dgate

@@ -1,0 +1,202 @@
+"""Group norm of rows on the GPU against its float64 reference.
+
+Tolerances in u = 2^-24 (half a step of fp32), c entries in a group.  A mean or
+sum over c entries in a tree of lanes is off by at most (c/64 + 16) u of the
+magnitudes' mean; deviations from the mean are off by that and by their own
+rounding, 1/sqrt by 4 u more, the activation by 8 u.  With k = c/64 + 40 a
+normed entry is off by k u (|n| + r mean|x|) and the results by what they make of
+it; a bf16 row output adds 2^-8 of itself.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decay_attn as R
+from paper_2605_19150_amd import pdssm
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DEV = "cuda"
+TYPES = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+
+
+def _np(t):
+    return None if t is None else t.detach().double().cpu().numpy()
+
+
+class Case:
+    def __init__(self, T, C, G, dtype, gate=True, act="silu", weight=True, pad=0, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        self.T, self.C, self.G, self.dtype, self.act = T, C, G, dtype, act
+        rows = torch.randn(T, 3 * C + pad, generator=g)
+        rows[:, pad:pad + C] = rows[:, pad:pad + C] * 2 + 0.5
+        rows = rows.to(dtype).to(DEV)
+        self.x, self.gate, self.dy = (rows[:, pad + k * C:pad + (k + 1) * C] for k in range(3))
+        if not gate:
+            self.gate = None
+        self.w, self.b = ((torch.randn(C, generator=g).to(DEV) for _ in range(2)) if weight else (None, None))
+
+    def kw(self):
+        return dict(weight=self.w, bias=self.b, gate=self.gate, act=self.act)
+
+    def fwd(self, **kw):
+        return pdssm.group_norm(self.x, self.G, **self.kw(), **kw)
+
+    def bwd(self, **kw):
+        return pdssm.group_norm_bwd(self.x, self.dy, self.G, **self.kw(), **kw)
+
+    def check(self, y, grads):
+        x, dy = _np(self.x), _np(self.dy)
+        kw = dict(weight=_np(self.w), bias=_np(self.b), gate=_np(self.gate), act=self.act)
+        c = self.C // self.G
+        want, f = R.norm(x, self.G, **kw), R.norm_bwd(x, dy, self.G, **kw)
+        w = np.ones(self.C) if self.w is None else np.abs(_np(self.w))
+        b = np.zeros(self.C) if self.b is None else np.abs(_np(self.b))
+        k = (c / 64 + 40) * U
+
+        def mean(v):
+            return np.repeat(v.reshape(self.T, self.G, c).mean(2), c, axis=1)
+
+        n, r = np.abs(f["n"]), f["r"]
+        # a group's mean is off by k u of mean|x|; so is every deviation, and the root by no more than that in n's unit
+        dn = k * (n + r * mean(np.abs(x))) * (1 + n)
+        du_ = dn * w + 3 * U * (n * w + b)     # of u
+        gf = np.ones_like(x) if self.gate is None else np.abs(R._act(_np(self.gate), self.act)[0])
+        slope = 1.1  # of silu and, times 1/2, of its own slope, at most
+        eps = 2.0 ** -8 if self.dtype == torch.bfloat16 else 2 * U
+        if self.gate is None:
+            near("y", y, want, slope * du_ + 10 * U * np.abs(want) + eps * np.abs(want))
+        else:
+            near("y", y, want, gf * du_ + 12 * U * np.abs(want) + eps * np.abs(want))
+        dx, dw, db, dgate = grads
+        # of du: the activation's slope moves with u
+        ddu = np.abs(dy) * (slope * du_ if self.gate is None and self.act == "silu" else 0) + 16 * U * (np.abs(f["du"]) + np.abs(dy))
+        if self.gate is not None:
+            ddu = 16 * U * np.abs(f["du"])
+        dd = ddu * w
+        dnabs = np.abs(f["du"]) * w
+        tol = r * (dd + mean(dd) + n * mean(dd * n) + dn * mean(dnabs * n) + n * mean(dnabs * dn))
+        # the root's error scales dx: that of var, a mean of squares of deviations that are off by k u (|d| + mean|x|)
+        tol += f["dx_size"] * k * (1 + mean(n * (n + r * mean(np.abs(x)))))
+        near("dx", dx, f["dx"], tol + eps * np.abs(f["dx"]))
+        if self.gate is not None:
+            df = np.abs(R._act(_np(self.gate), self.act)[1])
+            near("dgate", dgate, f["dgate"], np.abs(dy) * (du_ * df + 16 * U * (np.abs(f["u"]) * (1 + df))) + eps * np.abs(f["dgate"]))
+        if self.w is not None:
+            rows = (self.T / 16 + 48) * U
+            near("dw", dw, f["dw"], (ddu * n + np.abs(f["du"]) * dn).sum(0) + rows * f["dw_size"])
+            near("db", db, f["db"], ddu.sum(0) + rows * f["db_size"])
+
+
+def near(name, got, want, tol):
+    got = _np(got).reshape(want.shape)
+    bad = ~(np.abs(got - want) <= tol + 1e-30)
+    assert not bad.any(), "%s: %d of %d, worst %.3g of its tolerance" % (name, bad.sum(), bad.size,
+                                                                        np.nanmax(np.abs(got - want) / (tol + 1e-30)))
+
+
+SHAPES = [(1, 1, 1), (3, 2, 1), (5, 24, 8), (7, 37, 1), (9, 111, 3), (4, 1024, 8), (33, 512, 64), (2, 4096, 1), (3, 4100, 2),
+          (600, 96, 12), (1, 8192, 64), (2, 9001, 1), (3, 10240, 2)]
+
+
+@TYPES
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("gate", [False, True])
+@pytest.mark.parametrize("T,C,G", SHAPES)
+def test_norm_and_its_gradients(T, C, G, gate, act, dtype):
+    c = Case(T, C, G, dtype, gate, act, seed=C)
+    c.check(c.fwd(), c.bwd())
+
+
+@TYPES
+@pytest.mark.parametrize("pad", [1, 8])
+@pytest.mark.parametrize("weight", [False, True])
+def test_rows_where_they_stand(weight, pad, dtype):
+    c = Case(50, 256, 4, dtype, weight=weight, pad=pad)
+    c.check(c.fwd(), c.bwd())
+
+
+@TYPES
+def test_batches_and_single_arguments(dtype):
+    c = Case(12, 64, 4, dtype)
+    y, grads = c.fwd(), c.bwd()
+    x3, g3, d3 = (t.contiguous().view(3, 4, 64) for t in (c.x, c.gate, c.dy))
+    y3 = pdssm.group_norm(x3, 4, c.w, c.b, gate=g3, act="silu")
+    got = pdssm.group_norm_bwd(x3, d3, 4, c.w, c.b, gate=g3, act="silu")
+    assert y3.shape == x3.shape and torch.equal(y3.flatten(0, 1), y)
+    assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip(got, grads))
+    only_w = pdssm.group_norm_bwd(c.x, c.dy, 4, c.w)
+    only_b = pdssm.group_norm_bwd(c.x, c.dy, 4, bias=c.b)
+    assert only_w[2] is None and only_w[3] is None and only_b[1] is None and only_b[2] is not None
+
+
+def test_calls_without_rows():
+    x = torch.zeros(0, 16, device=DEV)
+    w = torch.ones(16, device=DEV)
+    assert pdssm.group_norm(x, 2, w, w).shape == (0, 16)
+    dx, dw, db, _ = pdssm.group_norm_bwd(x, x, 2, w, w)
+    assert dx.shape == (0, 16) and not dw.any() and not db.any()
+
+
+@TYPES
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_what_is_not_finite_stays_in_its_group(act, dtype):
+    plain, c = (Case(6, 64, 4, dtype, act=act) for _ in range(2))
+    c.x[2, 20] = math.inf
+    c.x[3, 40] = math.nan
+    (y, g), (z, h) = (plain.fwd(), plain.bwd()), (c.fwd(), c.bwd())
+    hit = torch.zeros(6, 64, dtype=torch.bool, device=DEV)
+    hit[2, 16:32] = hit[3, 32:48] = True
+    for a, b in ((y, z), (g[0], h[0]), (g[3], h[3])):
+        assert b[hit].isnan().all() and torch.equal(a[~hit], b[~hit])
+    for a, b in ((g[1], h[1]),):
+        assert b[16:48].isnan().all() and torch.equal(a[:16], b[:16]) and torch.equal(a[48:], b[48:])
+
+
+@TYPES
+def test_shut_and_open_gates(dtype):
+    c = Case(4, 32, 2, dtype)
+    low = torch.finfo(dtype).min
+    for k, v in enumerate((-math.inf, low, -200.0, math.inf)):
+        c.gate[k, 5] = v
+    y, (dx, dw, db, dgate) = c.fwd(), c.bwd()
+    assert not y[:3, 5].any() and y[3, 5].isinf() and not dgate[:3, 5].any()
+    u = pdssm.group_norm(c.x, 2, c.w, c.b)
+    # the slope is 1
+    torch.testing.assert_close(dgate[3, 5].float(), c.dy[3, 5].float() * u[3, 5].float(), rtol=2.0 ** -6, atol=1e-6)
+    assert dx[:3].isfinite().all()
+
+
+@TYPES
+def test_constant_groups_and_no_eps(dtype):
+    x = torch.full((3, 8), 4.0, device=DEV).to(dtype)
+    assert not pdssm.group_norm(x, 2).any()
+    assert pdssm.group_norm(x, 2, eps=0.0).isnan().all()
+
+
+def test_the_same_call_twice_streams_and_graphs():
+    c = Case(700, 512, 8, torch.bfloat16)
+    want = (c.fwd(), *c.bwd())
+    s = torch.cuda.Stream()
+    got = (c.fwd(stream=s), *c.bwd(stream=s))
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = (c.fwd(), *c.bwd())
+    for _ in range(3):
+        c.x.copy_(torch.randn(c.x.shape, device=DEV))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, (c.fwd(), *c.bwd())))
+
+
+def test_rows_past_32_bits():
+    T, ld = 300, 1 << 23
+    buf = torch.zeros(T * ld, dtype=torch.bfloat16, device=DEV)
+    c = Case(T, 64, 4, torch.bfloat16, gate=False)
+    x = torch.as_strided(buf, (T, 64), (ld, 1), 8)
+    x.copy_(c.x)
+    assert torch.equal(pdssm.group_norm(x, 4, c.w, c.b), pdssm.group_norm(c.x, 4, c.w, c.b))
