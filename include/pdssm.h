@@ -579,9 +579,9 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
  * head is the sum over those that read it.  Any Dk and Dv from 1 to 256, alignment
  * of an entry; 16-byte aligned rows of multiples of 16 bytes are the fast ones.
  * States (h0, h_final, dh_final, dh0) are fp32 [S, H, Dk, Dv], and so are rate and all
- * sums.  With bf16 rows the products run on bf16 numbers: the rows, which are
- * exact in it, and states, weighted rows and weighted scores each as the sum of two such numbers,
- * off by at most 2^-17 of themselves.  Outputs are rounded once, to nearest even.
+ * sums.  With bf16 rows the products run on bf16 numbers: the rows, which are exact in
+ * it; the rows that go into a state, weighted, as sums of three such numbers (24 bits); and, where a row
+ * output is made of them, states and weighted scores, rounded to one.  Outputs are rounded to nearest even.
  *
  * Sequences are as for the gated layers: S of T / S rows each, or cu [S+1], and
  * some may have no rows (h_final = h0, dh0 = dh_final, zeros where those are NULL).

@@ -24,7 +24,7 @@ namespace pdssm {
 namespace {
 
 constexpr int kFill = 512;      // workgroups that fill the card: two on each of 256 CUs
-constexpr int kSegmentMin = 256;  // rows below which a segment is not worth its state
+constexpr int kSegmentMin = 128;  // rows below which a segment is not worth its state
 
 struct Plan {
     int seg_rows, items;
@@ -32,7 +32,7 @@ struct Plan {
 };
 
 int slices(int cols, bool wide) { return (cols + (wide ? 127 : 63)) / (wide ? 128 : 64); }
-bool wide_cols(const AttnArgs& a, bool bwd) { return (bwd ? max(a.Dk, a.Dv) : a.Dv) > 64 && max(a.Dk, a.Dv) <= 128; }
+bool wide_cols(const AttnArgs& a, bool bwd) { return (bwd ? max(a.Dk, a.Dv) : a.Dv) > 64; }
 int members(const AttnArgs& a, bool bwd) {
     const bool wide = wide_cols(a, bwd);
     return bwd ? 2 * slices(a.Dk, wide) + slices(a.Dv, wide) : slices(a.Dv, wide);
@@ -80,19 +80,20 @@ Space space(const AttnArgs& a, const Plan& p, bool bwd) {
     return s;
 }
 
-// From what the segments add to the states that they begin with.  x: those of the
-// sequences' first rows.  A workgroup has a part of one state of the sequence whose
-// second segment has the slot.
-__global__ __launch_bounds__(256) void k_segments(AttnScan a, int64_t slots) {
+// From what the segments add to the states that they begin with.  A workgroup has kPart
+// entries of a head's state, of the sequence whose second segment has the slot (cu), or
+// of one sequence.  kAhead loads of a thread are under way at a time.
+constexpr int kPart = 1024, kAhead = 4;
+
+__global__ __launch_bounds__(256) void k_segments(AttnScan a) {
     const AttnRole& R = a.role[blockIdx.z];
-    const int h = blockIdx.y, parts = (a.state + 255) / 256;
-    const int64_t slot = blockIdx.x / parts;
-    const int e = (int)(blockIdx.x % parts) * 256 + threadIdx.x;
-    int s;
+    const int h = blockIdx.y, parts = (a.state + kPart - 1) / kPart;
+    const int e0 = (int)(blockIdx.x % parts) * kPart + threadIdx.x;
+    int s = blockIdx.x / parts;
     int64_t begin, len;
     if (a.cu) {
+        const int64_t slot = s, row = slot * a.seg_rows;
         int lo = 0, n = a.S;
-        const int64_t row = slot * a.seg_rows;
         while (n > 1) {  // the last sequence that begins at or before the slot's row
             const int step = (n + 255) / 256, at = lo + (int)threadIdx.x * step;
             const bool in = (int)threadIdx.x * step < n && min(max(a.cu[at], 0), a.T) <= row;
@@ -103,19 +104,37 @@ __global__ __launch_bounds__(256) void k_segments(AttnScan a, int64_t slots) {
         s = lo;
         begin = min(max(a.cu[s], 0), a.T);
         len = min(max(a.cu[s + 1], (int)begin), a.T) - begin;
+        if (begin / a.seg_rows != slot - 1) return;
     } else {
-        s = (int)min(slot * a.seg_rows / a.L, (int64_t)a.S - 1);
         begin = (int64_t)s * a.L;
         len = a.L;
     }
-    if (begin / a.seg_rows != slot - 1 || len <= a.seg_rows || e >= a.state) return;
+    if (len <= a.seg_rows) return;
     const float rate = a.rate[h];
     const float keep = rate >= 0.f && rate < INFINITY ? (float)exp(-(double)rate * a.seg_rows) : NAN;
-    float x = R.x0 ? R.x0[((size_t)s * a.H + h) * a.state + e] : 0.f;
     const int n = (int)((len + a.seg_rows - 1) / a.seg_rows);
-    float* p = const_cast<float*>(R.seg) + ((size_t)slot * a.H + h) * a.state + e;
     const size_t next = (size_t)a.H * a.state;
-    for (int seg = 1; seg < n; ++seg, p += next) *p = x = keep * x + *p;
+    float* p = const_cast<float*>(R.seg) + ((size_t)(begin / a.seg_rows + 1) * a.H + h) * a.state + e0;
+    const float* x0 = R.x0 ? R.x0 + ((size_t)s * a.H + h) * a.state + e0 : nullptr;
+    constexpr int E = kPart / 256;
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = x0 && e0 + e * 256 < a.state ? x0[e * 256] : 0.f;
+    for (int seg = 1; seg < n; seg += kAhead) {
+        float add[kAhead][E];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) add[k][e] = seg + k < n && e0 + e * 256 < a.state ? p[k * next + e * 256] : 0.f;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                x[e] = fmaf(keep, x[e], add[k][e]);
+                if (seg + k < n && e0 + e * 256 < a.state) p[k * next + e * 256] = x[e];
+            }
+        p += kAhead * next;
+    }
 }
 
 // The gradient of a shared head: the sum over the states' heads that read it.
@@ -177,8 +196,8 @@ void add_role(AttnScan& n, const AttnRole& r, bool wide) {
 hipError_t begin_segments(const AttnScan& n, const Plan& p, bool wide, hipStream_t s) {
     hipError_t e = scan(n, false, wide, s);
     if (e != hipSuccess) return e;
-    const dim3 grid((unsigned)(p.slots * ((n.state + 255) / 256)), n.H, n.roles);
-    hipLaunchKernelGGL(k_segments, grid, dim3(256), 0, s, n, p.slots);
+    const dim3 grid((unsigned)((n.cu ? p.slots : n.S) * ((n.state + kPart - 1) / kPart)), n.H, n.roles);
+    hipLaunchKernelGGL(k_segments, grid, dim3(256), 0, s, n);
     return hipGetLastError();
 }
 
@@ -204,8 +223,9 @@ size_t attn_workspace(const AttnArgs& a, bool bwd) { return space(a, plan(a, bwd
 
 bool attn_fits(const AttnArgs& a, bool bwd) {
     const Plan p = plan(a, bwd);
-    const int64_t parts = ((int64_t)a.Dk * a.Dv + 255) / 256;
-    return ((int64_t)p.items * a.H + 7) * members(a, bwd) < (1 << 24) && p.slots * parts * a.H * 2 < (1 << 24);
+    const int64_t parts = ((int64_t)a.Dk * a.Dv + kPart - 1) / kPart;
+    return ((int64_t)p.items * a.H + 7) * members(a, bwd) < (1 << 24) &&
+           (p.slots == 0 || (a.cu ? p.slots : a.S) * parts * a.H * 2 < (1 << 24));
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s) {
