@@ -1258,7 +1258,7 @@ int pdssm_group_norm(const pdssm_norm_desc* d, const pdssm_rows* x, const pdssm_
 }
 
 size_t pdssm_group_norm_workspace_size(const pdssm_norm_desc* d) {
-    return check_norm(d) == PDSSM_OK ? pdssm::norm_workspace(d->T, d->C, d->G) : (size_t)-1;
+    return check_norm(d) == PDSSM_OK ? pdssm::norm_workspace(d->T, d->C) : (size_t)-1;
 }
 
 int pdssm_group_norm_bwd(const pdssm_norm_desc* d, const pdssm_rows* x, const pdssm_rows* gate, const pdssm_rows* dy,
@@ -1278,7 +1278,7 @@ int pdssm_group_norm_bwd(const pdssm_norm_desc* d, const pdssm_rows* x, const pd
         gate = &none;
         dgate = nullptr;
     }
-    const size_t need = dweight || dbias ? pdssm::norm_workspace(T, C, d->G) : 0;
+    const size_t need = dweight || dbias ? pdssm::norm_workspace(T, C) : 0;
     if (need && (!ws || ws_bytes < need)) return PDSSM_ERR_WORKSPACE;
     if (need && misaligned_to(ws, kAlign)) return PDSSM_ERR_INVALID_ARG;
     if (any_overlap({{dx, n}, {dgate, n}, {dweight, nc}, {dbias, nc}, {ws, need}},

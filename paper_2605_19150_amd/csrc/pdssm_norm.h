@@ -29,7 +29,7 @@ struct NormArgs {
     int team;        // lanes that share a group's row, a power of two up to 64
     int blocks;      // blocks of rows: one wave's (or workgroup's) rows of some groups
 };
-size_t norm_workspace(int T, int C, int G);
+size_t norm_workspace(int T, int C);
 bool norm_fits(int T, int C, int G);
 hipError_t launch_norm_fwd(NormArgs a, hipStream_t s);
 hipError_t launch_norm_bwd(NormArgs a, hipStream_t s);

@@ -16,6 +16,8 @@
 // a wave's registers are read once for each pass by a workgroup.
 #include <math.h>
 
+#include <algorithm>
+
 #include "pdssm_norm.h"
 #include "pdssm_rows.h"
 
@@ -25,15 +27,13 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kBlocks = 512;  // blocks of rows at most: their sums are under 2 % of a large call's bytes
+constexpr int kBlocks = 512;      // blocks of rows that a call of any width may have
+constexpr int kNormWaves = 4096;  // waves that fill the card
+// Bytes of a row tensor from which on rows go past the caches, which they would only sweep: at 32768 rows of
+// 4096 channels, bf16 with a gate, 183 -> 178 us forward, 291 -> 280 us backward.
+constexpr int64_t kPast = 64 << 20;
 
-template <int IO, int V>
-struct Part {
-    using T = typename Entry<IO>::T;
-    T v[V];
-};
-
-template <int IO, int V>
+template <int IO, int V, bool PAST>
 __device__ __forceinline__ void load(const void* p, size_t i, float* x) {
     using T = typename Entry<IO>::T;
     const T* q = static_cast<const T*>(p) + i;
@@ -42,7 +42,7 @@ __device__ __forceinline__ void load(const void* p, size_t i, float* x) {
             u32x4 u;
             T v[V];
         } t;
-        t.u = *reinterpret_cast<const u32x4*>(q);
+        t.u = PAST ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(q)) : *reinterpret_cast<const u32x4*>(q);
 #pragma unroll
         for (int e = 0; e < V; ++e) x[e] = Entry<IO>::get(t.v[e]);
     } else {
@@ -50,7 +50,7 @@ __device__ __forceinline__ void load(const void* p, size_t i, float* x) {
         for (int e = 0; e < V; ++e) x[e] = Entry<IO>::get(q[e]);
     }
 }
-template <int IO, int V>
+template <int IO, int V, bool PAST>
 __device__ __forceinline__ void store(void* p, size_t i, const float* x) {
     using T = typename Entry<IO>::T;
     T* q = static_cast<T*>(p) + i;
@@ -61,7 +61,8 @@ __device__ __forceinline__ void store(void* p, size_t i, const float* x) {
         } t;
 #pragma unroll
         for (int e = 0; e < V; ++e) t.v[e] = Entry<IO>::put(x[e]);
-        *reinterpret_cast<u32x4*>(q) = t.u;
+        if constexpr (PAST) __builtin_nontemporal_store(t.u, reinterpret_cast<u32x4*>(q));
+        else *reinterpret_cast<u32x4*>(q) = t.u;
     } else {
 #pragma unroll
         for (int e = 0; e < V; ++e) q[e] = Entry<IO>::put(x[e]);
@@ -117,7 +118,7 @@ struct Lane {
     __device__ __forceinline__ bool has(int k, int team) const { return k * team * V < left; }
 };
 
-template <int IO, int V, int NV>
+template <int IO, int V, int NV, bool PAST>
 __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a) {
     const Lane<V, NV> l(a);
     if (l.block >= a.blocks) return;
@@ -138,8 +139,8 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a) {
         for (int k = 0; k < NV; ++k)
             if (l.has(k, a.team)) {
                 const size_t c = l.first + k * a.team * V;
-                load<IO, V>(a.x.p, (size_t)t * a.x.ld + c, x[k]);
-                if (a.gate.p) load<IO, V>(a.gate.p, (size_t)t * a.gate.ld + c, z[k]);
+                load<IO, V, PAST>(a.x.p, (size_t)t * a.x.ld + c, x[k]);
+                if (a.gate.p) load<IO, V, PAST>(a.gate.p, (size_t)t * a.gate.ld + c, z[k]);
             }
         float sum = 0.f;
 #pragma unroll
@@ -164,12 +165,12 @@ __global__ __launch_bounds__(256) void k_norm_fwd(NormArgs a) {
                     const float u = fmaf(x[k][e] * rstd, w[k][e], b[k][e]);
                     x[k][e] = a.gate.p ? u * act<false>(z[k][e], a.silu).f : act<false>(u, a.silu).f;
                 }
-                store<IO, V>(a.y, (size_t)t * a.C + l.first + k * a.team * V, x[k]);
+                store<IO, V, PAST>(a.y, (size_t)t * a.C + l.first + k * a.team * V, x[k]);
             }
     }
 }
 
-template <int IO, int V, int NV>
+template <int IO, int V, int NV, bool PAST>
 __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a) {
     const Lane<V, NV> l(a);
     if (l.block >= a.blocks) return;
@@ -190,9 +191,9 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a) {
         for (int k = 0; k < NV; ++k)
             if (l.has(k, a.team)) {
                 const size_t c = l.first + k * a.team * V;
-                load<IO, V>(a.x.p, (size_t)t * a.x.ld + c, x[k]);
-                load<IO, V>(a.dy.p, (size_t)t * a.dy.ld + c, d[k]);
-                if (a.gate.p) load<IO, V>(a.gate.p, (size_t)t * a.gate.ld + c, z[k]);
+                load<IO, V, PAST>(a.x.p, (size_t)t * a.x.ld + c, x[k]);
+                load<IO, V, PAST>(a.dy.p, (size_t)t * a.dy.ld + c, d[k]);
+                if (a.gate.p) load<IO, V, PAST>(a.gate.p, (size_t)t * a.gate.ld + c, z[k]);
             }
         float sum = 0.f;
 #pragma unroll
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a) {
                     s1 += d[k][e];
                     s2 = fmaf(d[k][e], n, s2);
                 }
-                if (a.gate.p) store<IO, V>(a.dgate, (size_t)t * a.C + l.first + k * a.team * V, z[k]);
+                if (a.gate.p) store<IO, V, PAST>(a.dgate, (size_t)t * a.C + l.first + k * a.team * V, z[k]);
             }
         s1 = team_sum(s1, a.team) * inv;
         s2 = team_sum(s2, a.team) * inv;
@@ -240,7 +241,7 @@ __global__ __launch_bounds__(256) void k_norm_bwd(NormArgs a) {
             if (l.has(k, a.team)) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) x[k][e] = rstd * (d[k][e] - s1 - x[k][e] * s2);
-                store<IO, V>(a.dx, (size_t)t * a.C + l.first + k * a.team * V, x[k]);
+                store<IO, V, PAST>(a.dx, (size_t)t * a.C + l.first + k * a.team * V, x[k]);
             }
     }
     if (!a.part) return;
@@ -323,8 +324,15 @@ __global__ __launch_bounds__(256) void k_norm_sum(const float* part, int blocks,
     __shared__ float lds[16][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), k = threadIdx.x >> 4;  // columns of dw, then those of db
     float sum = 0.f;
-    if (c < 2 * C)
-        for (int b = k; b < blocks; b += 16) sum += part[(size_t)b * 2 * C + c];
+    if (c < 2 * C) {
+        for (int b = k; b < blocks; b += 16 * 8) {  // eight loads are under way at a time
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = b + e * 16 < blocks ? part[(size_t)(b + e * 16) * 2 * C + c] : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += x[e];
+        }
+    }
     lds[k][threadIdx.x & 15] = sum;
     __syncthreads();
     if (k == 0 && c < 2 * C) {
@@ -353,23 +361,28 @@ Shape shape(const NormArgs& a) {
     return s;
 }
 
-int row_blocks(int T, int C, int G) { return T < kBlocks ? T : kBlocks; }
+// Blocks of rows, each of which is one wave's for some of the groups.  Enough waves to fill the
+// card; backward four rows or more in a block, whose sums take as much room as four bf16 rows.
+int row_blocks(int T, int C, bool bwd) {
+    const int waves = (C + 511) / 512, most = std::max(kBlocks, kNormWaves / waves);
+    return std::min(bwd ? (T + 3) / 4 : T, most);
+}
 
 }  // namespace
 
-size_t norm_workspace(int T, int C, int G) { return ((size_t)row_blocks(T, C, G) * 2 * C * 4 + 255) / 256 * 256; }
+size_t norm_workspace(int T, int C) { return ((size_t)row_blocks(T, C, true) * 2 * C * 4 + 255) / 256 * 256; }
 
-bool norm_fits(int T, int C, int G) { return (int64_t)row_blocks(T, C, G) * G < (1 << 24); }
+bool norm_fits(int T, int C, int G) { return (int64_t)row_blocks(T, C, false) * G < (1 << 24); }
 
 namespace {
 
-template <int IO, int V>
+template <int IO, int V, bool PAST>
 void (*pick(int num, bool bwd))(NormArgs) {
     switch (num) {
-        case 1: return bwd ? k_norm_bwd<IO, V, 1> : k_norm_fwd<IO, V, 1>;
-        case 2: return bwd ? k_norm_bwd<IO, V, 2> : k_norm_fwd<IO, V, 2>;
-        case 4: return bwd ? k_norm_bwd<IO, V, 4> : k_norm_fwd<IO, V, 4>;
-        default: return bwd ? k_norm_bwd<IO, V, 8> : k_norm_fwd<IO, V, 8>;
+        case 1: return bwd ? k_norm_bwd<IO, V, 1, PAST> : k_norm_fwd<IO, V, 1, PAST>;
+        case 2: return bwd ? k_norm_bwd<IO, V, 2, PAST> : k_norm_fwd<IO, V, 2, PAST>;
+        case 4: return bwd ? k_norm_bwd<IO, V, 4, PAST> : k_norm_fwd<IO, V, 4, PAST>;
+        default: return bwd ? k_norm_bwd<IO, V, 8, PAST> : k_norm_fwd<IO, V, 8, PAST>;
     }
 }
 
@@ -377,13 +390,15 @@ hipError_t rows(NormArgs& a, bool bwd, hipStream_t s) {
     const Shape sh = shape(a);
     const bool b = a.io == kRowBf16;
     a.team = sh.team;
-    a.blocks = row_blocks(a.T, a.C, a.G);
+    a.blocks = row_blocks(a.T, a.C, bwd);
     if (a.T == 0) return hipSuccess;
     void (*f)(NormArgs);
     unsigned grid;
     if (sh.num) {
-        f = sh.vec > 1 ? (b ? pick<kRowBf16, 8>(sh.num, bwd) : pick<kRowF32, 4>(sh.num, bwd))
-                       : (b ? pick<kRowBf16, 1>(sh.num, bwd) : pick<kRowF32, 1>(sh.num, bwd));
+        const bool past = (int64_t)a.T * a.C * (b ? 2 : 4) >= kPast;
+        if (sh.vec == 1) f = b ? pick<kRowBf16, 1, false>(sh.num, bwd) : pick<kRowF32, 1, false>(sh.num, bwd);
+        else if (past) f = b ? pick<kRowBf16, 8, true>(sh.num, bwd) : pick<kRowF32, 4, true>(sh.num, bwd);
+        else f = b ? pick<kRowBf16, 8, false>(sh.num, bwd) : pick<kRowF32, 4, false>(sh.num, bwd);
         const int per = 64 / sh.team, sets = (a.G + per - 1) / per;
         grid = (unsigned)(((int64_t)sets * a.blocks + 3) / 4);
     } else {

@@ -1031,21 +1031,25 @@ _ATTN_DESC, _HEADS = struct.Struct("8ifI"), struct.Struct("Pqq")
 
 
 def _heads(t, name, dtype, lead, D, dev):
-    """(pdssm_heads, heads) of heads' rows [*lead, heads, D] that may be parts of wider rows."""
+    """(address, entries from row to row, from head to head, heads) of heads' rows [*lead, heads, D] that may be
+    parts of wider rows."""
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
     if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    shape = t.shape
-    if len(shape) != len(lead) + 2 or shape[:-2] != lead or (D is not None and shape[-1] != D):
-        raise ValueError("%s must have shape (%s, heads, %s), got %s" % (name, ", ".join(map(str, lead)), D or "D", tuple(shape)))
+    n, shape = len(lead), t.shape
+    if len(shape) != n + 2 or shape[0] != lead[0] or (n == 2 and shape[1] != lead[1]) or shape[-1] != D:
+        raise ValueError("%s must have shape (%s, heads, %s), got %s" % (name, ", ".join(map(str, lead)), D, tuple(shape)))
     if not t.is_cuda or t.device != dev:
         raise ValueError("%s must be on %s" % (name, dev))
+    heads = shape[n]
+    if t.is_contiguous():
+        return t.data_ptr(), heads * D, D, heads
     step = t.stride()
-    if step[-1] != 1 and shape[-1] > 1:
+    if step[-1] != 1 and D > 1:
         raise ValueError("%s: the entries of a row must be next to each other" % name)
     ld = 0
-    if len(lead) == 2:
+    if n == 2:
         B, L = lead
         if L > 1:
             ld = step[1]
@@ -1055,13 +1059,13 @@ def _heads(t, name, dtype, lead, D, dev):
             ld = step[0]
     elif lead[0] > 1:
         ld = step[0]
-    return _HEADS.pack(t.data_ptr(), ld, step[-2] if shape[-2] > 1 else 0), shape[-2]
+    return t.data_ptr(), ld, step[n] if heads > 1 else 0, heads
 
 
 def _attn(q, k, v, rate, scale, S, lead, T):
     """(desc, pdssm_heads of q, k and v, address of rate, (H, Dk, Dv), device)."""
     flags = _row_type(q)
-    dev = q.device
+    dev, dtype = q.device, q.dtype
     if not isinstance(rate, torch.Tensor) or rate.dim() != 1:
         raise ValueError("rate must be [H]")
     H = rate.shape[0]
@@ -1069,18 +1073,20 @@ def _attn(q, k, v, rate, scale, S, lead, T):
     if not isinstance(v, torch.Tensor) or v.dim() != len(lead) + 2:
         raise ValueError("v must be rows [%s,heads,D]" % ",".join("BL" if len(lead) == 2 else "T"))
     Dk, Dv = q.shape[-1], v.shape[-1]
-    (q_at, hq), (k_at, hk), (v_at, hv) = (_heads(t, n, q.dtype, lead, D, dev)
-                                          for t, n, D in ((q, "q", Dk), (k, "k", Dk), (v, "v", Dv)))
-    for n, heads in (("q", hq), ("k", hk), ("v", hv)):
-        if heads < 1 or H % heads != 0:
-            raise ValueError("%s has %d heads, which do not divide the %d of rate" % (n, heads, H))
+    qp, ql, qs, hq = _heads(q, "q", dtype, lead, Dk, dev)
+    kp, kl, ks, hk = _heads(k, "k", dtype, lead, Dk, dev)
+    vp, vl, vs, hv = _heads(v, "v", dtype, lead, Dv, dev)
+    if hq < 1 or hk < 1 or hv < 1 or H % hq or H % hk or H % hv:
+        raise ValueError("q, k and v have %d, %d and %d heads, which have to divide the %d of rate" % (hq, hk, hv, H))
     if not 1 <= Dk <= 256 or not 1 <= Dv <= 256:
         raise ValueError("heads must have 1 to 256 entries, got %d and %d" % (Dk, Dv))
     scale = Dk ** -0.5 if scale is None else float(scale)
     if not abs(scale) < math.inf:
         raise ValueError("scale must be finite")
-    _int32(T, S, H)
-    return _ATTN_DESC.pack(T, S, H, hq, hk, hv, Dk, Dv, scale, flags), (q_at, k_at, v_at), rate_at, (H, Dk, Dv), dev
+    if T > 0x7fffffff or S > 0x7fffffff:
+        _int32(T, S)
+    return (_ATTN_DESC.pack(T, S, H, hq, hk, hv, Dk, Dv, scale, flags),
+            (_HEADS.pack(qp, ql, qs), _HEADS.pack(kp, kl, ks), _HEADS.pack(vp, vl, vs)), rate_at, (H, Dk, Dv), dev)
 
 
 def _head_sequences(t, cu):
@@ -1101,7 +1107,7 @@ def _head_sequences(t, cu):
 
 
 def _attn_ws(desc, cu, op, dev):
-    n = load().pdssm_decay_attn_workspace_size(desc, cu is not None, op)
+    n = load().pdssm_decay_attn_workspace_size(desc, 0 if cu is None else 1, op)
     if n == OP_SIZE_ERROR:
         raise PdssmError(ERR_UNSUPPORTED, "decay_attn_workspace_size")
     return torch.empty(n, dtype=torch.uint8, device=dev) if n else None
@@ -1142,7 +1148,8 @@ def decay_attn_bwd(q, k, v, rate, do, scale=None, cu=None, h0=None, dh_final=Non
     the sum of theirs.  The rates are constants, there is no gradient of them."""
     lead, T, S = _head_sequences(q, cu)
     d, rows, rate_at, (H, Dk, Dv), dev = _attn(q, k, v, rate, scale, S, lead, T)
-    do_at, heads = _heads(do, "do", q.dtype, lead, Dv, dev)
+    *do_at, heads = _heads(do, "do", q.dtype, lead, Dv, dev)
+    do_at = _HEADS.pack(*do_at)
     if heads != H:
         raise ValueError("do must have the %d heads of rate, got %d" % (H, heads))
     h0_at, dhf_at = (_matrix_state(t, n, (S, H, Dk, Dv), dev) for t, n in ((h0, "h0"), (dh_final, "dh_final")))
@@ -1174,7 +1181,9 @@ def decay_attn_step(q, k, v, rate, h, scale=None, slots=None, out=None, o=None, 
     slots_at = None if slots is None else _tensor(slots, "slots", torch.int32, (B,), dev)
     if o is None:
         o = q.new_empty((B, H, Dv))
-    o_at = _tensor(o, "o", q.dtype, (B, H, Dv), dev)
+        o_at = o.data_ptr()
+    else:
+        o_at = _tensor(o, "o", q.dtype, (B, H, Dv), dev)
     status = _status(check, dev)
     s = _on(stream, dev, (q, k, v, rate, h, out, slots, o, status))
     st = load().pdssm_decay_attn_step(d, *rows, rate_at, slots_at, h_at, out_at, o_at, _at(status), s)
@@ -1206,7 +1215,8 @@ def _norm(x, groups, weight, bias, gate, act, eps):
     _int32(T, C)
     rows = _rows(x, "x", x.dtype, x.shape, dev)
     gate_rows = None if gate is None else _rows(gate, "gate", x.dtype, x.shape, dev)
-    w_at, b_at = (None if t is None else _tensor(t, n, torch.float32, (C,), dev) for t, n in ((weight, "weight"), (bias, "bias")))
+    w_at = None if weight is None else _tensor(weight, "weight", torch.float32, (C,), dev)
+    b_at = None if bias is None else _tensor(bias, "bias", torch.float32, (C,), dev)
     return _NORM_DESC.pack(T, C, groups, _ACTS[act], eps, flags), rows, gate_rows, w_at, b_at, C, dev
 
 
@@ -1231,7 +1241,8 @@ def group_norm_bwd(x, dy, groups, weight=None, bias=None, gate=None, act="none",
     dy_rows = _rows(dy, "dy", x.dtype, x.shape, dev)
     dx = torch.empty_like(x, memory_format=torch.contiguous_format)
     dgate = None if gate is None else torch.empty_like(dx)
-    dw, db = (None if t is None else torch.empty_like(t) for t in (weight, bias))
+    dw = None if weight is None else torch.empty_like(weight)
+    db = None if bias is None else torch.empty_like(bias)
     n = 0
     if dw is not None or db is not None:
         n = load().pdssm_group_norm_workspace_size(d)
