@@ -51,7 +51,8 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // the state, an fp32 output that sums up (two: 720 us, and 2.5e-6 off in place of 2e-7).
 constexpr int kStateTerms = 1;  // the state where a row reads it
 constexpr int kScoreTerms = 1;  // weighted scores
-constexpr int kRowTerms = 3;    // weighted rows that go into the state
+constexpr int kRowTerms = 3;    // weighted rows that go into a state
+constexpr int kInnerTerms = 2;  // the same where that is no output
 
 // A tile of rows in LDS.  Its pitch is 8 banks past a multiple of 64 (bf16), and of
 // rows 8 to 15 of each 16 the 16-byte pieces change places in pairs: so neither 16 lanes with
@@ -127,26 +128,26 @@ struct Mat<kRowF32> {
     static __device__ __forceinline__ float get(Frag f, int e) { return f[e]; }
 };
 
-// The largest magnitude's bits of a thread's entries, those of an infinity or a NaN on top.
+// Whether one of a thread's entries is an infinity or a NaN: the largest magnitude's bits.
 template <int IO>
-struct Largest;
+struct Wild;
 template <>
-struct Largest<kRowBf16> {
+struct Wild<kRowBf16> {
     u16x2 top = {};
     __device__ __forceinline__ void add(u32x4 x) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
     }
-    __device__ __forceinline__ bool wild() const { return max(top.x, top.y) >= 0x7f80; }
+    __device__ __forceinline__ bool any() const { return max(top.x, top.y) >= 0x7f80; }
 };
 template <>
-struct Largest<kRowF32> {
+struct Wild<kRowF32> {
     uint32_t top = 0;
     __device__ __forceinline__ void add(u32x4 x) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = max(top, x[e] & 0x7fffffffu);
     }
-    __device__ __forceinline__ bool wild() const { return top >= 0x7f800000u; }
+    __device__ __forceinline__ bool any() const { return top >= 0x7f800000u; }
 };
 
 constexpr uint32_t kOutside = 0x80000000u;  // an offset past every chunk: loads of zeros, stores that are dropped
@@ -198,7 +199,7 @@ struct Stage {
             }
         }
     }
-    __device__ __forceinline__ void store(T* tile, int c0, Largest<IO>& top) {
+    __device__ __forceinline__ void store(T* tile, int c0, Wild<IO>& top) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int r = row + u * kRows;
@@ -207,6 +208,11 @@ struct Stage {
         }
     }
 };
+
+// Two bf16 numbers, to nearest even, the first in the low half.
+__device__ __forceinline__ uint32_t pair(float x, float y) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, bf16x2));
+}
 
 // x as the sum of N numbers of the operands' type.
 template <int IO, int N>
@@ -218,7 +224,7 @@ __device__ __forceinline__ void split(const float* x, typename Mat<IO>::Frag (&f
             f32x2 rest = {x[2 * e], x[2 * e + 1]};
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2));
+                const uint32_t u = pair(rest.x, rest.y);
                 to[n][e] = u;
                 rest.x -= __uint_as_float(u << 16);
                 rest.y -= __uint_as_float(u & 0xffff0000u);
@@ -247,7 +253,7 @@ struct Shared {
 };
 
 // The scan of a segment of a head, for the W columns of out from W * member on.
-template <int IO, int DC, int NW, int NT, bool FULL, int BY, bool LATE>
+template <int IO, int DC, int NW, int NT, bool FULL, int BY, bool LATE, int TERMS>
 __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& R, int64_t group, int member,
                                              Shared<IO, DC, NW * NT * 16, FULL>& lds) {
     using M = Mat<IO>;
@@ -255,7 +261,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
     using Frag = typename M::Frag;
     constexpr int C = M::kChunk, KB = M::kDepth, W = NW * NT * 16, NTH = NW * 64, B = KB / 16;
     constexpr int PK = DC + Tile<IO>::kPad, PV = W + Tile<IO>::kPad, PA = C + 16 / sizeof(T), NI = C / 16, ND = DC / 16, E = KB / 4;
-    constexpr int NS = M::kSplit ? kStateTerms : 1, NA = M::kSplit ? kScoreTerms : 1, NV = M::kSplit ? kRowTerms : 1;
+    constexpr int NS = M::kSplit ? kStateTerms : 1, NA = M::kSplit ? kScoreTerms : 1, NV = M::kSplit ? TERMS : 1;
     T *const ks = lds.ks, *const vs = lds.vs, *const qs = lds.qs, *const as = lds.as;
     float *const up = lds.up, *const down = lds.down, *const pw = lds.pw;
     int& bad = lds.bad;
@@ -409,11 +415,11 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
     int p = 0;
     for (; p < rows; p += C) {
         const int n = min(C, rows - p);
-        Largest<IO> top;
+        Wild<IO> top;
         sk.store(ks, 0, top);
         if constexpr (FULL) sq.store(qs, 0, top);
         sv.store(vs, col0, top);
-        if (top.wild()) bad = 1;
+        if (top.any()) bad = 1;
         __syncthreads();
         if (bad) break;
         if (p + C < rows) load(p + C);
@@ -504,20 +510,17 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
                     for (int i = 0; i < NI; ++i) {
                         const int bi = block(i) * 16;
                         const f32x4 x = acc[i][t];
-                        uint32_t v[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) v[e] = Entry<kRowBf16>::put(x[e]);
                         if constexpr (BY == 16) {
                             const uint32_t at = bi + lr < n && c < R.Do ? off + (uint32_t)bi * (uint32_t)out_ld * size : kOutside;
                             if (f32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at, 0, 0);
-                            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{v[0] | v[1] << 16, v[2] | v[3] << 16}, to, at, 0, 0);
+                            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{pair(x[0], x[1]), pair(x[2], x[3])}, to, at, 0, 0);
                         } else if (bi + lr < n) {
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const int64_t o = base + (bi + lr) * out_ld + c + e;
                                 if (c + e >= R.Do) continue;
                                 if (f32) static_cast<float*>(R.out)[o] = x[e];
-                                else static_cast<uint16_t*>(R.out)[o] = (uint16_t)v[e];
+                                else static_cast<uint16_t*>(R.out)[o] = Entry<kRowBf16>::put(x[e]);
                             }
                         }
                     }
@@ -561,7 +564,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
         const int n = min(C, rows - p);
         __syncthreads();
         load(p);
-        Largest<IO> top;
+        Wild<IO> top;
         sk.store(ks, 0, top);
         if constexpr (FULL) sq.store(qs, 0, top);
         sv.store(vs, col0, top);
@@ -624,8 +627,14 @@ __global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : 2) void k_attn_scan(At
     int ri = 0;
     while (ri + 1 < a.roles && member >= a.role[ri].slices) member -= a.role[ri++].slices;
     const AttnRole& R = a.role[ri];
-    if (R.late) scan_segment<IO, DC, NW, NT, FULL, BY, true>(a, R, group, member, lds);
-    else scan_segment<IO, DC, NW, NT, FULL, BY, false>(a, R, group, member, lds);
+    constexpr int kLess = FULL && BY == 16 ? kInnerTerms : kRowTerms;
+    if (R.late) {
+        if (!FULL || R.fin) scan_segment<IO, DC, NW, NT, FULL, BY, true, kRowTerms>(a, R, group, member, lds);
+        else scan_segment<IO, DC, NW, NT, FULL, BY, true, kLess>(a, R, group, member, lds);
+    } else {
+        if (!FULL || R.fin) scan_segment<IO, DC, NW, NT, FULL, BY, false, kRowTerms>(a, R, group, member, lds);
+        else scan_segment<IO, DC, NW, NT, FULL, BY, false, kLess>(a, R, group, member, lds);
+    }
 }
 
 template <int IO, int DC, int NW, int NT, bool FULL>
