@@ -86,9 +86,10 @@ struct Mat<kRowBf16> {
         const u32x2 lo = *reinterpret_cast<const u32x2*>(p), hi = *reinterpret_cast<const u32x2*>(p + 16);
         return __builtin_bit_cast(Frag, u32x4{lo.x, lo.y, hi.x, hi.y});
     }
-    // where a lane begins to read columns, and the read: 16 lanes hand each other the four entries of their four rows
+    // where a lane begins to read columns of eight neighbouring rows, and the read: 16 lanes hand each other the
+    // four entries of their four rows
     static __device__ __forceinline__ int col_at(int lane, int pitch) {
-        const int r = (lane >> 4) * 4 + ((lane & 15) >> 2);
+        const int r = (lane >> 4) * 8 + ((lane & 15) >> 2);
         return r * pitch + Tile<kRowBf16>::col(r, (lane & 3) * 4);
     }
     static __device__ __forceinline__ Frag col(const T* p, int pitch) {
@@ -97,7 +98,7 @@ struct Mat<kRowBf16> {
             Frag f;
         } u;
         u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * pitch));
+        u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * pitch));
         return u.f;
     }
     // 16 bytes of a row: eight neighbours of the summed axis, where both operands are read so
@@ -128,17 +129,16 @@ struct Mat<kRowF32> {
     static __device__ __forceinline__ float get(Frag f, int e) { return f[e]; }
 };
 
-// Whether one of a thread's entries is an infinity or a NaN: the largest magnitude's bits.
+// Whether one of a wave's entries is an infinity or a NaN.
 template <int IO>
 struct Wild;
 template <>
 struct Wild<kRowBf16> {
-    u16x2 top = {};
+    f32x4 sum = {};  // of the entries times zero: NaN then.  On the matrix cores, which have time; by their bits 8 operations more for each 16 bytes
     __device__ __forceinline__ void add(u32x4 x) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
+        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), bf16x8{}, sum, 0, 0, 0);
     }
-    __device__ __forceinline__ bool any() const { return max(top.x, top.y) >= 0x7f80; }
+    __device__ __forceinline__ bool any() const { return !(sum.x + sum.y + sum.z + sum.w == 0.f); }
 };
 template <>
 struct Wild<kRowF32> {
@@ -492,7 +492,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
                     for (int i = kb * B; i < NI; ++i)
 #pragma unroll
                         for (int m = 0; m < NA; ++m) {
-                            const Frag af = M::row(as + (m * C + block(i) * 16 + lr) * PA + bj + g * 4);
+                            const Frag af = M::near(as + (m * C + block(i) * 16 + lr) * PA + bj + g * M::kNear);
 #pragma unroll
                             for (int t = 0; t < NT; ++t) acc[i][t] = M::mul(vf[t], af, acc[i][t]);
                         }
@@ -542,7 +542,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
                         const Frag vf = M::col(vcol + kb * KB * PV + t * 16, PV);
                         float e[8];
 #pragma unroll
-                        for (int r = 0; r < E; ++r) e[r] = M::get(vf, r) * in[kb * KB + g * 4 + r + (r >= 4 ? 12 : 0)];
+                        for (int r = 0; r < E; ++r) e[r] = M::get(vf, r) * in[kb * KB + g * M::kNear + r];
                         split<IO>(e, f[t]);
                     }
 #pragma unroll
@@ -616,7 +616,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
 
 // DC: entries of q and k rows, filled up; NW waves, each of which owns NT blocks of 16 columns of v.
 template <int IO, int DC, int NW, int NT, bool FULL, int BY>
-__global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : 2) void k_attn_scan(AttnScan a) {
+__global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : NW / 2) void k_attn_scan(AttnScan a) {
     __shared__ Shared<IO, DC, NW * NT * 16, FULL> lds;
     // the workgroups of one segment of a head are neighbours on one of the 8 XCDs,
     // so that rows which several of them read come from its L2
@@ -665,7 +665,11 @@ hipError_t launch_attn_scan(const AttnScan& a, bool full, bool wide, hipStream_t
         if (full && (R.Do % 4 != 0 || reinterpret_cast<uintptr_t>(R.out) % 16 != 0 || (int64_t)a.H * R.Do > 1 << 24)) by = std::min(by, 4);
     }
     // 128 columns: two blocks a wave, or for rows past 128 entries, whose state needs the registers, one
+    #ifdef EIGHT
+    constexpr int NW = 8, NT = 1;
+#else
     constexpr int NW = DC > 128 ? 8 : 4, NT = DC > 128 ? 1 : 2;
+#endif
     void (*f)(AttnScan);
     if (b) f = full ? (wide ? pick<kRowBf16, DC, NW, NT, true>(by) : pick<kRowBf16, DC, 4, 1, true>(by))
                     : (wide ? pick<kRowBf16, DC, NW, NT, false>(by) : pick<kRowBf16, DC, 4, 1, false>(by));
