@@ -24,6 +24,7 @@ namespace pdssm {
 namespace {
 
 constexpr int kFill = 512;      // workgroups that fill the card: two on each of 256 CUs
+constexpr int kFillPacked = 768;  // the same where lengths differ
 constexpr int kSegmentMin = 128;  // rows below which a segment is not worth its state
 
 struct Plan {
@@ -44,7 +45,8 @@ Plan plan(const AttnArgs& a, bool bwd) {
     Plan p = {};
     if (!a.cu) {
         const int64_t whole = a.S * heads;
-        int64_t n = whole >= kFill ? 1 : min((kFill + whole - 1) / whole, max((int64_t)a.L / kSegmentMin, (int64_t)1));
+        const int fill = max(a.Dk, a.Dv) <= 64 ? kFill * 3 / 2 : kFill;
+        int64_t n = whole >= fill ? 1 : min((fill + whole - 1) / whole, max((int64_t)a.L / kSegmentMin, (int64_t)1));
         const int64_t rows = (max(a.L, 1) + n - 1) / n;
         p.seg_rows = (int)((rows + chunk - 1) / chunk * chunk);
         n = max((a.L + p.seg_rows - 1) / p.seg_rows, 1);
@@ -52,7 +54,7 @@ Plan plan(const AttnArgs& a, bool bwd) {
         p.slots = n > 1 ? a.T / p.seg_rows + 1 : 0;
     } else {
         // lengths are not known here: segments of what a workgroup has if all rows are shared out
-        int64_t rows = max((int64_t)kSegmentMin, (a.T * heads + kFill - 1) / kFill);
+        int64_t rows = max((int64_t)kSegmentMin, (a.T * heads + kFillPacked - 1) / kFillPacked);
         rows = min(rows, (int64_t)max(a.T, 1));
         p.seg_rows = (int)((rows + chunk - 1) / chunk * chunk);
         p.items = a.T / p.seg_rows + a.S;
@@ -137,19 +139,38 @@ __global__ __launch_bounds__(256) void k_segments(AttnScan a) {
     }
 }
 
-// The gradient of a shared head: the sum over the states' heads that read it.
-template <int IO>
-__global__ __launch_bounds__(256) void k_share(const float* part, typename Entry<IO>::T* out, int64_t T, const int* cu, int S,
-                                               int heads, int share, int D) {
-    const int64_t rest = cu ? min((int64_t)max(cu[S], 0), T) : T, n = T * heads * D;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / D / heads;
-        float sum = 0.f;
-        if (row < rest) {
-            const float* p = part + (i / D) * share * D + i % D;
-            for (int r = 0; r < share; ++r) sum += p[(int64_t)r * D];
-        }
-        out[i] = Entry<IO>::put(sum);
+// The gradients of shared heads: the sums over the states' heads that read them, of up
+// to three tensors.  A thread has V entries of a head, of every so many-th row.
+struct ShareArgs {
+    struct {
+        const float* part;  // [T, heads * share, D]
+        void* out;          // [T, heads, D]
+        int heads, share, D;
+    } of[3];
+    int T, S;
+    const int* cu;
+};
+constexpr int kShareRows = 2048;  // workgroups, or rows, that are under way
+
+template <int IO, int V>
+__global__ __launch_bounds__(256) void k_share(ShareArgs a) {
+    typedef float vec __attribute__((ext_vector_type(V)));
+    const auto& o = a.of[blockIdx.z];
+    const int rest = a.cu ? min(max(a.cu[a.S], 0), a.T) : a.T;
+    const int per = o.D / V, all = o.heads * per;  // vectors of a head, of a row
+    const int rows = max(256 / all, 1);            // rows that a workgroup has at a time
+    const int e = blockIdx.x * 256 + threadIdx.x % (256 / rows), row = blockIdx.y * rows + threadIdx.x / (256 / rows);
+    if (e >= all || (int)threadIdx.x / (256 / rows) >= rows) return;
+    const int head = e / per, d = e % per * V, step = gridDim.y * rows;
+    const int64_t wide = (int64_t)o.heads * o.D;
+    const float* p = o.part + (row * wide + (int64_t)head * o.D) * o.share + d;
+    auto* out = static_cast<typename Entry<IO>::T*>(o.out) + row * wide + (int64_t)head * o.D + d;
+    for (int t = row; t < a.T; t += step, p += step * wide * o.share, out += step * wide) {
+        vec sum = {};
+        if (t < rest)
+            for (int r = 0; r < o.share; ++r) sum += *reinterpret_cast<const vec*>(p + r * o.D);
+#pragma unroll
+        for (int k = 0; k < V; ++k) out[k] = Entry<IO>::put(sum[k]);
     }
 }
 
@@ -207,13 +228,27 @@ hipError_t check_bounds(const AttnArgs& a, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int IO>
-hipError_t add_shared(const AttnArgs& a, const float* part, void* out, const HeadsIn& x, int D, hipStream_t s) {
-    const int64_t n = (int64_t)a.T * (a.H / x.share) * D;
-    if (x.share == 1 || n == 0) return hipSuccess;
-    const unsigned blocks = (unsigned)min((n + 255) / 256, (int64_t)8192);
-    hipLaunchKernelGGL(k_share<IO>, dim3(blocks), dim3(256), 0, s, part, static_cast<typename Entry<IO>::T*>(out), (int64_t)a.T, a.cu,
-                       a.S, a.H / x.share, x.share, D);
+hipError_t add_shared(const AttnArgs& a, float* const (&part)[3], hipStream_t s) {
+    ShareArgs n = {};
+    int z = 0, most = 0;
+    bool four = true;
+    auto add = [&](const float* p, void* out, const HeadsIn& x, int D) {
+        if (x.share == 1) return;
+        n.of[z++] = {p, out, a.H / x.share, x.share, D};
+        four = four && D % 4 == 0;
+        most = max(most, a.H / x.share * D);
+    };
+    add(part[0], a.dq, a.q, a.Dk);
+    add(part[1], a.dk, a.k, a.Dk);
+    add(part[2], a.dv, a.v, a.Dv);
+    if (z == 0 || a.T == 0) return hipSuccess;
+    n.T = a.T;
+    n.S = a.S;
+    n.cu = a.cu;
+    const int wide = four ? 1024 : 256;
+    void (*f)(ShareArgs) = a.io == kRowBf16 ? (four ? k_share<kRowBf16, 4> : k_share<kRowBf16, 1>)
+                                            : (four ? k_share<kRowF32, 4> : k_share<kRowF32, 1>);
+    hipLaunchKernelGGL(f, dim3((most + wide - 1) / wide, min(a.T, kShareRows), z), dim3(256), 0, s, n);
     return hipGetLastError();
 }
 
@@ -321,10 +356,7 @@ hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t s) {
         if ((e = scan(m, true, wide, s)) != hipSuccess) return e;
     }
     if ((e = scan(n, true, wide, s)) != hipSuccess) return e;
-    auto* add = a.io == kRowBf16 ? add_shared<kRowBf16> : add_shared<kRowF32>;
-    if ((e = add(a, part[0], a.dq, a.q, a.Dk, s)) != hipSuccess) return e;
-    if ((e = add(a, part[1], a.dk, a.k, a.Dk, s)) != hipSuccess) return e;
-    return add(a, part[2], a.dv, a.v, a.Dv, s);
+    return add_shared(a, part, s);
 }
 
 // ---- one token -------------------------------------------------------------------------------------------------------

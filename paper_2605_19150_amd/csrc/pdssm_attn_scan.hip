@@ -616,7 +616,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
 
 // DC: entries of q and k rows, filled up; NW waves, each of which owns NT blocks of 16 columns of v.
 template <int IO, int DC, int NW, int NT, bool FULL, int BY>
-__global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : NW / 2) void k_attn_scan(AttnScan a) {
+__global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : 2) void k_attn_scan(AttnScan a) {
     __shared__ Shared<IO, DC, NW * NT * 16, FULL> lds;
     // the workgroups of one segment of a head are neighbours on one of the 8 XCDs,
     // so that rows which several of them read come from its L2
@@ -665,17 +665,13 @@ hipError_t launch_attn_scan(const AttnScan& a, bool full, bool wide, hipStream_t
         if (full && (R.Do % 4 != 0 || reinterpret_cast<uintptr_t>(R.out) % 16 != 0 || (int64_t)a.H * R.Do > 1 << 24)) by = std::min(by, 4);
     }
     // 128 columns: two blocks a wave, or for rows past 128 entries, whose state needs the registers, one
-    #ifdef EIGHT
-    constexpr int NW = 8, NT = 1;
-#else
     constexpr int NW = DC > 128 ? 8 : 4, NT = DC > 128 ? 1 : 2;
-#endif
     void (*f)(AttnScan);
     if (b) f = full ? (wide ? pick<kRowBf16, DC, NW, NT, true>(by) : pick<kRowBf16, DC, 4, 1, true>(by))
-                    : (wide ? pick<kRowBf16, DC, NW, NT, false>(by) : pick<kRowBf16, DC, 4, 1, false>(by));
+                    : (wide ? pick<kRowBf16, DC, 8, 1, false>(by) : pick<kRowBf16, DC, 4, 1, false>(by));
     else f = full ? (wide ? pick<kRowF32, DC, NW, NT, true>(by) : pick<kRowF32, DC, 4, 1, true>(by))
-                  : (wide ? pick<kRowF32, DC, NW, NT, false>(by) : pick<kRowF32, DC, 4, 1, false>(by));
-    hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(wide ? NW * 64 : 256), 0, s, a);
+                  : (wide ? pick<kRowF32, DC, 8, 1, false>(by) : pick<kRowF32, DC, 4, 1, false>(by));
+    hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(!wide ? 256 : full ? NW * 64 : 512), 0, s, a);
     return hipGetLastError();
 }
 template hipError_t launch_attn_scan<PDSSM_DC>(const AttnScan&, bool, bool, hipStream_t);
