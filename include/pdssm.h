@@ -580,8 +580,10 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
  * of an entry; 16-byte aligned rows of multiples of 16 bytes are the fast ones.
  * States (h0, h_final, dh_final, dh0) are fp32 [S, H, Dk, Dv], and so are rate and all
  * sums.  With bf16 rows the products run on bf16 numbers: the rows, which are exact in
- * it; the rows that go into a state, weighted, as sums of three such numbers (24 bits); and, where a row
- * output is made of them, states and weighted scores, rounded to one.  Outputs are rounded to nearest even.
+ * it; the rows that go into a state, weighted, as sums of three such numbers (24 bits; of two in a
+ * backward pass for states that only row gradients are made of); and, where a row output is made of
+ * them, states and weighted scores, rounded to one, or in calls that leave CUs idle to the sum of two.
+ * Outputs are rounded to nearest even.
  *
  * Sequences are as for the gated layers: S of T / S rows each, or cu [S+1], and
  * some may have no rows (h_final = h0, dh0 = dh_final, zeros where those are NULL).

@@ -92,6 +92,7 @@ struct AttnScan {
     const int* cu;
     int members;         // workgroups of a head's segment, over all roles
     int64_t groups;      // items * H
+    int fine;            // bf16 rows: operands of more bits in two terms each
 };
 
 // States only (full = 0): what the rows of each segment but the last add.

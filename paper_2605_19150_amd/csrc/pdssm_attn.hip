@@ -211,6 +211,7 @@ void add_role(AttnScan& n, const AttnRole& r, bool wide) {
     to = r;
     to.slices = slices(r.Do, wide);
     n.members += to.slices;
+    n.fine = n.groups * n.members <= kFill / 2;  // one on a CU at most
 }
 
 // The states that segments begin with, of the roles in n.

@@ -45,14 +45,17 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // With bf16 rows, the bf16 numbers whose sum an operand of more bits is taken as.
-// One is off by at most 2^-8 of the value, as the row outputs are by their own rounding: enough
-// for what only such an output is made from (two of each: 887 us for 771 in the backward
-// pass at 8 x 4096 rows of 32 heads of 128).  Three hold 24 bits, for what goes into
-// the state, an fp32 output that sums up (two: 720 us, and 2.5e-6 off in place of 2e-7).
-constexpr int kStateTerms = 1;  // the state where a row reads it
-constexpr int kScoreTerms = 1;  // weighted scores
-constexpr int kRowTerms = 3;    // weighted rows that go into a state
-constexpr int kInnerTerms = 2;  // the same where that is no output
+struct Terms {
+    int state;  // the state where a row reads it
+    int score;  // weighted scores
+    int row;    // weighted rows that go into the state
+};
+// Three hold the 24 bits of what goes into a state that is an output, a sum in fp32 (two: 2.5e-6 off in
+// place of 2e-7).  One is off by at most 2^-8 of the value, as a row output is by its own
+// rounding: the two together make row outputs 1.4 times as far off as the rounding alone does.
+// Two of each cost 16 % at 8 x 4096 rows of 32 heads of 128 (711 -> 826 us backward), and nothing
+// where CUs are idle: calls that leave some take two.
+constexpr Terms kFine = {2, 2, 3}, kOut = {1, 1, 3}, kInner = {1, 1, 2};
 
 // A tile of rows in LDS.  Its pitch is 8 banks past a multiple of 64 (bf16), and of
 // rows 8 to 15 of each 16 the 16-byte pieces change places in pairs: so neither 16 lanes with
@@ -241,11 +244,11 @@ template <int IO, int DC, int W, bool FULL>
 struct Shared {
     using T = typename Mat<IO>::T;
     static constexpr int C = Mat<IO>::kChunk, PK = DC + Tile<IO>::kPad, PV = W + Tile<IO>::kPad, PA = C + 16 / sizeof(T);
-    static constexpr int NA = Mat<IO>::kSplit ? kScoreTerms : 1;
+    static constexpr int NA = Mat<IO>::kSplit ? kFine.score : 1;
     alignas(16) T ks[C * PK];
     alignas(16) T vs[C * PV];
     alignas(16) T qs[FULL ? C * PK : 8];
-    alignas(16) T as[FULL ? NA * C * PA : 8];  // weighted scores, in NA terms
+    alignas(16) T as[FULL ? NA * C * PA : 8];  // weighted scores, in their terms
     // weights of a chunk's rows: a^(r+1), and from C - n on a^(n-1-r) with zeros behind it; the ones of
     // the state in out, and of rows in the state (late: the other way round); and powers of a
     float up[C], down[2 * C], pw[C + 1];
@@ -253,7 +256,7 @@ struct Shared {
 };
 
 // The scan of a segment of a head, for the W columns of out from W * member on.
-template <int IO, int DC, int NW, int NT, bool FULL, int BY, bool LATE, int TERMS>
+template <int IO, int DC, int NW, int NT, bool FULL, int BY, bool LATE, int STATE, int SCORE, int ROW>
 __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& R, int64_t group, int member,
                                              Shared<IO, DC, NW * NT * 16, FULL>& lds) {
     using M = Mat<IO>;
@@ -261,7 +264,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
     using Frag = typename M::Frag;
     constexpr int C = M::kChunk, KB = M::kDepth, W = NW * NT * 16, NTH = NW * 64, B = KB / 16;
     constexpr int PK = DC + Tile<IO>::kPad, PV = W + Tile<IO>::kPad, PA = C + 16 / sizeof(T), NI = C / 16, ND = DC / 16, E = KB / 4;
-    constexpr int NS = M::kSplit ? kStateTerms : 1, NA = M::kSplit ? kScoreTerms : 1, NV = M::kSplit ? TERMS : 1;
+    constexpr int NS = M::kSplit ? STATE : 1, NA = M::kSplit ? SCORE : 1, NV = M::kSplit ? ROW : 1;
     T *const ks = lds.ks, *const vs = lds.vs, *const qs = lds.qs, *const as = lds.as;
     float *const up = lds.up, *const down = lds.down, *const pw = lds.pw;
     int& bad = lds.bad;
@@ -627,13 +630,20 @@ __global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : 2) void k_attn_scan(At
     int ri = 0;
     while (ri + 1 < a.roles && member >= a.role[ri].slices) member -= a.role[ri++].slices;
     const AttnRole& R = a.role[ri];
-    constexpr int kLess = FULL && BY == 16 ? kInnerTerms : kRowTerms;
+    // slower loads do without the variant that is faster
+    const bool fine = FULL && (a.fine || BY != 16), out = !FULL || R.fin;
     if (R.late) {
-        if (!FULL || R.fin) scan_segment<IO, DC, NW, NT, FULL, BY, true, kRowTerms>(a, R, group, member, lds);
-        else scan_segment<IO, DC, NW, NT, FULL, BY, true, kLess>(a, R, group, member, lds);
+        if (fine || IO == kRowF32) scan_segment<IO, DC, NW, NT, FULL, BY, true, kFine.state, kFine.score, kFine.row>(a, R, group, member, lds);
+        else if constexpr (IO == kRowBf16 && (BY == 16 || !FULL)) {
+            if (out) scan_segment<IO, DC, NW, NT, FULL, BY, true, kOut.state, kOut.score, kOut.row>(a, R, group, member, lds);
+            else if constexpr (FULL) scan_segment<IO, DC, NW, NT, FULL, BY, true, kInner.state, kInner.score, kInner.row>(a, R, group, member, lds);
+        }
     } else {
-        if (!FULL || R.fin) scan_segment<IO, DC, NW, NT, FULL, BY, false, kRowTerms>(a, R, group, member, lds);
-        else scan_segment<IO, DC, NW, NT, FULL, BY, false, kLess>(a, R, group, member, lds);
+        if (fine || IO == kRowF32) scan_segment<IO, DC, NW, NT, FULL, BY, false, kFine.state, kFine.score, kFine.row>(a, R, group, member, lds);
+        else if constexpr (IO == kRowBf16 && (BY == 16 || !FULL)) {
+            if (out) scan_segment<IO, DC, NW, NT, FULL, BY, false, kOut.state, kOut.score, kOut.row>(a, R, group, member, lds);
+            else if constexpr (FULL) scan_segment<IO, DC, NW, NT, FULL, BY, false, kInner.state, kInner.score, kInner.row>(a, R, group, member, lds);
+        }
     }
 }
 
