@@ -364,7 +364,9 @@ Shape shape(const NormArgs& a) {
 // Blocks of rows, each of which is one wave's for some of the groups.  Enough waves to fill the
 // card; backward four rows or more in a block, whose sums take as much room as four bf16 rows.
 int row_blocks(int T, int C, bool bwd) {
-    const int waves = (C + 511) / 512, most = std::max(kBlocks, kNormWaves / waves);
+    const int waves = (C + 511) / 512;
+    int most = std::max(kBlocks, kNormWaves / waves);
+    if (bwd) most = std::min(most, std::max(64, (1 << 23) / C));  // the sums of very wide rows: 64 MB, or 64 blocks
     return std::min(bwd ? (T + 3) / 4 : T, most);
 }
 

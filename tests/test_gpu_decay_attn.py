@@ -139,6 +139,44 @@ def test_shared_heads_behind_the_last_sequence(dtype):
 
 
 @TYPES
+def test_shared_heads_of_odd_sizes(dtype):
+    c = Case([0, 3, 90], 6, 7, 9, dtype, heads=(6, 2, 3))
+    c.check_fwd(*c.fwd())
+    c.check_bwd(c.bwd())
+
+
+@TYPES
+@pytest.mark.parametrize("H,D,share", [(300, (24, 40), 1), (300, (64, 64), 4), (140, (128, 128), 1), (140, (96, 72), 2),
+                                       (130, (200, 72), 1), (130, (72, 256), 1)], ids=str)
+def test_many_heads(H, D, share, dtype):
+    """Calls that fill the card (bf16: scores and states rounded once); three heads of them against the reference."""
+    bounds = [0, 70, 201]
+    c = Case(bounds, H, *D, dtype, heads=(H, H // share, H // share), seed=H)
+    (o, fin), grads = c.fwd(), c.bwd()
+    picked = [0, H // 2 // share * share, H - share]
+    users = [h + k for h in picked for k in range(share)]
+    part = Case(bounds, len(users), *D, dtype, heads=(len(users), len(picked), len(picked)), states=False)
+    of = lambda t, heads: t[:, torch.tensor(heads, device=DEV)]  # noqa: E731
+    shared = [h // share for h in picked]
+    part.q, part.k, part.v, part.do = of(c.q, users), of(c.k, shared), of(c.v, shared), of(c.do, users)
+    part.rate, part.h0, part.dhf = c.rate[users], of(c.h0, users), of(c.dhf, users)
+    part.check_fwd(of(o, users), of(fin, users))
+    part.check_bwd((of(grads[0], users), of(grads[1], shared), of(grads[2], shared), of(grads[3], users)))
+
+
+@TYPES
+def test_many_sequences(dtype):
+    """More sequences than a workgroup has threads: most of them short or empty, one long."""
+    g = np.random.default_rng(2)
+    n = np.where(g.random(1500) < 0.5, 0, g.integers(0, 6, 1500))
+    n[700] = 900
+    bounds = [0, *np.cumsum(n).tolist()]
+    c = Case(bounds, 1, 8, 8, dtype, T=bounds[-1] + 2)
+    c.check_fwd(*c.fwd())
+    c.check_bwd(c.bwd())
+
+
+@TYPES
 @pytest.mark.parametrize("pad", [0, 1, 8])
 @pytest.mark.parametrize("dense", [False, True])
 def test_sequences_in_segments(dense, pad, dtype):

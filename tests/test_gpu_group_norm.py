@@ -193,6 +193,28 @@ def test_the_same_call_twice_streams_and_graphs():
         assert all(torch.equal(a, b) for a, b in zip(out, (c.fwd(), *c.bwd())))
 
 
+@TYPES
+def test_large_calls(dtype):
+    """Rows that go past the caches: the same bits as in calls of some of them, and sums as in 64 bits."""
+    T, C, G = 8300 if dtype == torch.bfloat16 else 4200, 4096, 32
+    c = Case(T, C, G, dtype, seed=1)
+    y, (dx, dw, db, dgate) = c.fwd(), c.bwd()
+    kw = dict(act="silu")
+    for a in (0, 1000, T - 300):
+        x, gate, dy = (t[a:a + 300] for t in (c.x, c.gate, c.dy))
+        assert torch.equal(pdssm.group_norm(x, G, c.w, c.b, gate=gate, **kw), y[a:a + 300])
+        got = pdssm.group_norm_bwd(x, dy, G, c.w, c.b, gate=gate, **kw)
+        assert torch.equal(got[0], dx[a:a + 300]) and torch.equal(got[3], dgate[a:a + 300])
+    x = c.x.double().reshape(T, G, C // G)
+    n = ((x - x.mean(2, keepdim=True)) / torch.sqrt(x.var(2, correction=0, keepdim=True) + 1e-5)).reshape(T, C)
+    z = c.gate.double()
+    du = c.dy.double() * z * torch.sigmoid(z)
+    # a block of rows adds T/blocks terms one by one, and 512 blocks are added 16 at a time; 60 for the terms themselves
+    units = (T / 512 + 32 + 16 + 60) * U
+    near("dw", dw, _np((du * n).sum(0)), units * _np((du * n).abs().sum(0)))
+    near("db", db, _np(du.sum(0)), units * _np(du.abs().sum(0)))
+
+
 def test_rows_past_32_bits():
     T, ld = 300, 1 << 23
     buf = torch.zeros(T * ld, dtype=torch.bfloat16, device=DEV)
