@@ -663,8 +663,9 @@ int pdssm_decay_attn_step(const pdssm_attn_desc* desc, const pdssm_heads* q, con
  * rounded once.  A silu whose argument is under -88 (also -inf and the
  * type's lowest value: a shut gate) is 0, and its slope too; a NaN or an infinity
  * in x gives NaN in its group's row and in no other, in the gradients of weight and bias in its
- * columns of the group.  0 <= T <= 2^30, 1 <= C <= 2^24, min(T, 4096) * G < 2^24,
- * else PDSSM_ERR_UNSUPPORTED.  Results are deterministic. */
+ * columns of the group.  0 <= T <= 2^30, 1 <= C <= 2^24 and
+ * launches below 2^32 threads (min(T, 4096) * G < 2^24 is enough), else
+ * PDSSM_ERR_UNSUPPORTED.  Results are deterministic. */
 #define PDSSM_ACT_NONE 0
 #define PDSSM_ACT_SILU 1
 
