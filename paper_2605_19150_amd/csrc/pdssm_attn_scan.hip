@@ -202,12 +202,16 @@ struct Stage {
             }
         }
     }
+    // where u-th 16 bytes are in a tile
+    __device__ __forceinline__ int at(int u, int c0) const {
+        const int r = row + u * kRows;
+        return r * P + Tile<IO>::col(r, c - c0);
+    }
     __device__ __forceinline__ void store(T* tile, int c0, Wild<IO>& top) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int r = row + u * kRows;
             top.add(x[u]);
-            *reinterpret_cast<u32x4*>(tile + r * P + Tile<IO>::col(r, c - c0)) = x[u];
+            *reinterpret_cast<u32x4*>(tile + at(u, c0)) = x[u];
         }
     }
 };
@@ -415,15 +419,41 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
     const T* vcol = vs + M::col_at(lane, PV) + wc;
     auto block = [&](int i) { return LATE ? NI - 1 - i : i; };  // of 16 rows, the i-th on the way
 
+    // Rows of out as whole lines: a chunk's are put into the place of its q, and the threads that stage the
+    // next q there take them out first (each the 16 bytes that it will overwrite).  Stored as the
+    // accumulators hold them, 32 bytes of a row at a time, they cost a twelfth more at rows
+    // of 64 entries (174 -> 160 us backward at B16 L2048, 16 heads), 4 % at 128.
+    constexpr bool kWhole = FULL && BY == 16 && DC == W;
+    const bool tile = kWhole && (IO == kRowF32 || !R.out32);
+    int left = 0;  // rows of out that are there
+    using Out = Stage<IO, DC, NTH>;
+    auto take = [&](u32x4 (&y)[Out::U]) {
+#pragma unroll
+        for (int u = 0; u < Out::U; ++u) y[u] = *reinterpret_cast<const u32x4*>(qs + sq.at(u, 0));
+    };
+    auto put = [&](const u32x4 (&y)[Out::U], int64_t row, int n) {  // n rows from the first one on
+        const __amdgpu_buffer_rsrc_t to = row_block(static_cast<T*>(R.out) + out_row(row) + col0, n > 0 ? (uint32_t)((n - 1) * out_ld + R.Do - col0) * (uint32_t)sizeof(T) : 0);
+#pragma unroll
+        for (int u = 0; u < Out::U; ++u) {
+            const int r = sq.row + u * Out::kRows;
+            const uint32_t off = ((uint32_t)r * (uint32_t)out_ld + sq.c) * (uint32_t)sizeof(T);
+            __builtin_amdgcn_raw_buffer_store_b128(y[u], to, r < n && col0 + sq.c < R.Do ? off : kOutside, 0, 0);
+        }
+    };
+
     int p = 0;
     for (; p < rows; p += C) {
         const int n = min(C, rows - p);
         Wild<IO> top;
+        u32x4 y[Out::U];
+        if constexpr (kWhole) take(y);
         sk.store(ks, 0, top);
         if constexpr (FULL) sq.store(qs, 0, top);
         sv.store(vs, col0, top);
         if (top.any()) bad = 1;
         __syncthreads();
+        if constexpr (kWhole) put(y, left > 0 ? low(p - C, left) : 0, left);
+        left = 0;
         if (bad) break;
         if (p + C < rows) load(p + C);
         {
@@ -501,29 +531,42 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
                         }
                 }
                 // lane: row lr of a block of 16, columns 4 g .. 4 g + 3
-                const int64_t base = out_row(low(p, n));
-                const bool f32 = IO == kRowF32 || R.out32;
-                const uint32_t size = f32 ? 4 : 2;
-                const __amdgpu_buffer_rsrc_t to = row_block(static_cast<char*>(R.out) + base * size, (uint32_t)((n - 1) * out_ld + R.Do) * size);
+                if (kWhole && tile) {
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int c = col0 + wc + t * 16 + g * 4;
-                    const uint32_t off = ((uint32_t)lr * (uint32_t)out_ld + c) * size;
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) {
-                        const int bi = block(i) * 16;
-                        const f32x4 x = acc[i][t];
-                        if constexpr (BY == 16) {
-                            const uint32_t at = bi + lr < n && c < R.Do ? off + (uint32_t)bi * (uint32_t)out_ld * size : kOutside;
-                            if (f32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at, 0, 0);
-                            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{pair(x[0], x[1]), pair(x[2], x[3])}, to, at, 0, 0);
-                        } else if (bi + lr < n) {
+                        for (int i = 0; i < NI; ++i) {
+                            T* to = qs + (block(i) * 16 + lr) * PK + Tile<IO>::col(lr, wc + t * 16 + g * 4);
+                            const f32x4 x = acc[i][t];
+                            if constexpr (IO == kRowBf16) *reinterpret_cast<u32x2*>(to) = u32x2{pair(x[0], x[1]), pair(x[2], x[3])};
+                            else *reinterpret_cast<f32x4*>(to) = x;
+                        }
+                    left = n;
+                } else {
+                    const int64_t base = out_row(low(p, n));
+                    const bool f32 = IO == kRowF32 || R.out32;
+                    const uint32_t size = f32 ? 4 : 2;
+                    const __amdgpu_buffer_rsrc_t to = row_block(static_cast<char*>(R.out) + base * size, (uint32_t)((n - 1) * out_ld + R.Do) * size);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int64_t o = base + (bi + lr) * out_ld + c + e;
-                                if (c + e >= R.Do) continue;
-                                if (f32) static_cast<float*>(R.out)[o] = x[e];
-                                else static_cast<uint16_t*>(R.out)[o] = Entry<kRowBf16>::put(x[e]);
+                    for (int t = 0; t < NT; ++t) {
+                        const int c = col0 + wc + t * 16 + g * 4;
+                        const uint32_t off = ((uint32_t)lr * (uint32_t)out_ld + c) * size;
+#pragma unroll
+                        for (int i = 0; i < NI; ++i) {
+                            const int bi = block(i) * 16;
+                            const f32x4 x = acc[i][t];
+                            if constexpr (BY == 16) {
+                                const uint32_t at = bi + lr < n && c < R.Do ? off + (uint32_t)bi * (uint32_t)out_ld * size : kOutside;
+                                if (f32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at, 0, 0);
+                                else __builtin_amdgcn_raw_buffer_store_b64(u32x2{pair(x[0], x[1]), pair(x[2], x[3])}, to, at, 0, 0);
+                            } else if (bi + lr < n) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int64_t o = base + (bi + lr) * out_ld + c + e;
+                                    if (c + e >= R.Do) continue;
+                                    if (f32) static_cast<float*>(R.out)[o] = x[e];
+                                    else static_cast<uint16_t*>(R.out)[o] = Entry<kRowBf16>::put(x[e]);
+                                }
                             }
                         }
                     }
@@ -561,6 +604,11 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
             }
         }
         __syncthreads();
+    }
+    if constexpr (kWhole) {
+        u32x4 y[Out::U];
+        take(y);
+        put(y, left > 0 ? low((rows - 1) / C * C, left) : 0, left);
     }
     // row by row, as the recurrence is written
     for (; p < rows; p += C) {
