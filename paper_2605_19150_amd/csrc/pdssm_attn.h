@@ -92,6 +92,7 @@ struct AttnScan {
     const int* cu;
     int members;         // workgroups of a head's segment, over all roles
     int64_t groups;      // items * H
+    int past;            // out goes past the caches
     int fine;            // bf16 rows: operands of more bits in two terms each
 };
 

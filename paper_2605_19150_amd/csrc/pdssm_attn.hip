@@ -24,6 +24,7 @@ namespace pdssm {
 namespace {
 
 constexpr int kFill = 512;      // workgroups that fill the card: two on each of 256 CUs
+constexpr int64_t kPast = 64 << 20;  // bytes of a row output that the caches do not keep for its reader
 constexpr int kFillPacked = 768;  // the same where lengths differ
 constexpr int kSegmentMin = 128;  // rows below which a segment is not worth its state
 
@@ -211,6 +212,7 @@ void add_role(AttnScan& n, const AttnRole& r, bool wide) {
     to = r;
     to.slices = slices(r.Do, wide);
     n.members += to.slices;
+    n.past = n.past || (int64_t)n.T * n.H * r.Do * (n.io == kRowBf16 ? 2 : 4) >= kPast;
     n.fine = n.groups * n.members <= kFill / 2;  // one on a CU at most
 }
 

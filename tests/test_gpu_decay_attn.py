@@ -164,6 +164,20 @@ def test_many_heads(H, D, share, dtype):
     part.check_bwd((of(grads[0], users), of(grads[1], shared), of(grads[2], shared), of(grads[3], users)))
 
 
+def test_outputs_that_go_past_the_caches():
+    """64 MB and more of bf16 rows; two heads of them against the reference."""
+    L, S, H = 2048, 16, 17
+    c = Case(list(range(0, S * L + 1, L)), H, 64, 64, torch.bfloat16, dense=True, seed=6)
+    (o, fin), grads = c.fwd(), c.bwd()
+    picked = [3, 16]
+    part = Case([0, L, 2 * L], 2, 64, 64, torch.bfloat16, dense=True, states=False)
+    of = lambda t: t.reshape(S * L, H, -1)[2 * L:4 * L, picked]  # noqa: E731
+    part.q, part.k, part.v, part.do = (of(t) for t in (c.q, c.k, c.v, c.do))
+    part.rate, part.h0, part.dhf = c.rate[picked], c.h0[2:4, picked], c.dhf[2:4, picked]
+    part.check_fwd(of(o), fin[2:4, picked])
+    part.check_bwd((*(of(t) for t in grads[:3]), grads[3][2:4, picked]))
+
+
 @TYPES
 def test_many_sequences(dtype):
     """More sequences than a workgroup has threads: most of them short or empty, one long."""
