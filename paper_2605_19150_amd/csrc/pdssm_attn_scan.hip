@@ -53,8 +53,9 @@ struct Terms {
 // Three hold the 24 bits of what goes into a state that is an output, a sum in fp32 (two: 2.5e-6 off in
 // place of 2e-7).  One is off by at most 2^-8 of the value, as a row output is by its own
 // rounding: the two together make row outputs 1.4 times as far off as the rounding alone does.
-// Two of each cost 16 % at 8 x 4096 rows of 32 heads of 128 (711 -> 826 us backward), and nothing
-// where CUs are idle: calls that leave some take two.
+// Two of each cost 18 % at 8 x 4096 rows of 32 heads of 128 (688 -> 813 us backward), and nothing
+// where CUs are idle: calls that leave some take two.  Three terms for the states of dq and dk, which
+// only rows are made of, would cost 5 % (724 us).
 constexpr Terms kFine = {2, 2, 3}, kOut = {1, 1, 3}, kInner = {1, 1, 2};
 
 // A tile of rows in LDS.  Its pitch is 8 banks past a multiple of 64 (bf16), and of
