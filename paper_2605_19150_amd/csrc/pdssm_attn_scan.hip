@@ -41,7 +41,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // With bf16 rows, the bf16 numbers whose sum an operand of more bits is taken as.
@@ -462,149 +461,147 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
         left = 0;
         if (bad) break;
         if (p + C < rows) load(p + C);
-        {
-            if constexpr (FULL) {
-                // the scores that count, 16 x 16 of them at a time
-                for (int b = wave; b < NI * (NI + 1) / 2; b += NW) {
-                    int i = 0, j = b;
-                    while (j > i) j -= ++i;
-                    const int bi = block(i) * 16, bj = block(j) * 16;
-                    f32x4 sc = {};
+        if constexpr (FULL) {
+            // the scores that count, 16 x 16 of them at a time
+            for (int b = wave; b < NI * (NI + 1) / 2; b += NW) {
+                int i = 0, j = b;
+                while (j > i) j -= ++i;
+                const int bi = block(i) * 16, bj = block(j) * 16;
+                f32x4 sc = {};
 #pragma unroll
-                    for (int kb = 0; kb < DC / KB; ++kb) sc = M::mul(M::near(knear + bj * PK + kb * KB), M::near(qnear + bi * PK + kb * KB), sc);
-                    float far = one;
-                    for (int d = 1; d < i - j; ++d) far *= sixteen;
-                    float e[8] = {};
+                for (int kb = 0; kb < DC / KB; ++kb) sc = M::mul(M::near(knear + bj * PK + kb * KB), M::near(qnear + bi * PK + kb * KB), sc);
+                float far = one;
+                for (int d = 1; d < i - j; ++d) far *= sixteen;
+                float e[8] = {};
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) e[r] = i == j ? (w0[r] != 0.f ? sc[r] * w0[r] : 0.f) : sc[r] * (w1[r] * far);
-                    Frag f[NA];
-                    split<IO>(e, f);
-                    T* to = as + (bi + lr) * PA + bj + g * 4;
+                for (int r = 0; r < 4; ++r) e[r] = i == j ? (w0[r] != 0.f ? sc[r] * w0[r] : 0.f) : sc[r] * (w1[r] * far);
+                Frag f[NA];
+                split<IO>(e, f);
+                T* to = as + (bi + lr) * PA + bj + g * 4;
 #pragma unroll
-                    for (int m = 0; m < NA; ++m)
-                        if constexpr (M::kSplit) {
-                            const u32x4 u = __builtin_bit_cast(u32x4, f[m]);
-                            *reinterpret_cast<u32x2*>(to + m * C * PA) = u32x2{u.x, u.y};
-                        } else {
-                            *reinterpret_cast<Frag*>(to) = f[0];
-                        }
-                }
-                // S^T q
-                f32x4 acc[NI][NT] = {};
-#pragma unroll
-                for (int kb = 0; kb < DC / KB; ++kb) {
-                    Frag f[NT][NS];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        float e[8];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            e[r] = S[kb * B][t][r];
-                            e[4 + r] = S[kb * B + B - 1][t][r];
-                        }
-                        split<IO>(e, f[t]);
+                for (int m = 0; m < NA; ++m)
+                    if constexpr (M::kSplit) {
+                        const u32x4 u = __builtin_bit_cast(u32x4, f[m]);
+                        *reinterpret_cast<u32x2*>(to + m * C * PA) = u32x2{u.x, u.y};
+                    } else {
+                        *reinterpret_cast<Frag*>(to) = f[0];
                     }
+            }
+            // S^T q
+            f32x4 acc[NI][NT] = {};
 #pragma unroll
-                    for (int i = 0; i < NI; ++i) {
-                        const Frag qf = M::row(qrow + block(i) * 16 * PK + kb * KB);
+            for (int kb = 0; kb < DC / KB; ++kb) {
+                Frag f[NT][NS];
 #pragma unroll
-                        for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    float e[8];
 #pragma unroll
-                            for (int m = 0; m < NS; ++m) acc[i][t] = M::mul(f[t][m], qf, acc[i][t]);
+                    for (int r = 0; r < 4; ++r) {
+                        e[r] = S[kb * B][t][r];
+                        e[4 + r] = S[kb * B + B - 1][t][r];
                     }
+                    split<IO>(e, f[t]);
                 }
-                const float* in = LATE ? down + C - n : up;
 #pragma unroll
                 for (int i = 0; i < NI; ++i) {
-                    const float w = in[block(i) * 16 + lr];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) acc[i][t] *= w;
-                }
-                __syncthreads();
-#pragma unroll
-                for (int kb = 0; kb < C / KB; ++kb) {
-                    const int bj = LATE ? C - KB - kb * KB : kb * KB;
-                    Frag vf[NT];
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) vf[t] = M::col(vcol + bj * PV + t * 16, PV);
-#pragma unroll
-                    for (int i = kb * B; i < NI; ++i)
-#pragma unroll
-                        for (int m = 0; m < NA; ++m) {
-                            const Frag af = M::near(as + (m * C + block(i) * 16 + lr) * PA + bj + g * M::kNear);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) acc[i][t] = M::mul(vf[t], af, acc[i][t]);
-                        }
-                }
-                // lane: row lr of a block of 16, columns 4 g .. 4 g + 3
-                if (kWhole && tile) {
+                    const Frag qf = M::row(qrow + block(i) * 16 * PK + kb * KB);
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int i = 0; i < NI; ++i) {
-                            T* to = qs + (block(i) * 16 + lr) * PK + Tile<IO>::col(lr, wc + t * 16 + g * 4);
-                            const f32x4 x = acc[i][t];
-                            if constexpr (IO == kRowBf16) *reinterpret_cast<u32x2*>(to) = u32x2{pair(x[0], x[1]), pair(x[2], x[3])};
-                            else *reinterpret_cast<f32x4*>(to) = x;
-                        }
-                    left = n;
-                } else {
-                    const int64_t base = out_row(low(p, n));
-                    const bool f32 = IO == kRowF32 || R.out32;
-                    const uint32_t size = f32 ? 4 : 2;
-                    const __amdgpu_buffer_rsrc_t to = row_block(static_cast<char*>(R.out) + base * size, (uint32_t)((n - 1) * out_ld + R.Do) * size);
+                        for (int m = 0; m < NS; ++m) acc[i][t] = M::mul(f[t][m], qf, acc[i][t]);
+                }
+            }
+            const float* in = LATE ? down + C - n : up;
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const int c = col0 + wc + t * 16 + g * 4;
-                        const uint32_t off = ((uint32_t)lr * (uint32_t)out_ld + c) * size;
+            for (int i = 0; i < NI; ++i) {
+                const float w = in[block(i) * 16 + lr];
 #pragma unroll
-                        for (int i = 0; i < NI; ++i) {
-                            const int bi = block(i) * 16;
-                            const f32x4 x = acc[i][t];
-                            if constexpr (BY == 16) {
-                                const uint32_t at = bi + lr < n && c < R.Do ? off + (uint32_t)bi * (uint32_t)out_ld * size : kOutside;
-                                if (f32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at, 0, 0);
-                                else __builtin_amdgcn_raw_buffer_store_b64(u32x2{pair(x[0], x[1]), pair(x[2], x[3])}, to, at, 0, 0);
-                            } else if (bi + lr < n) {
+                for (int t = 0; t < NT; ++t) acc[i][t] *= w;
+            }
+            __syncthreads();
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) {
-                                    const int64_t o = base + (bi + lr) * out_ld + c + e;
-                                    if (c + e >= R.Do) continue;
-                                    if (f32) static_cast<float*>(R.out)[o] = x[e];
-                                    else static_cast<uint16_t*>(R.out)[o] = Entry<kRowBf16>::put(x[e]);
-                                }
+            for (int kb = 0; kb < C / KB; ++kb) {
+                const int bj = LATE ? C - KB - kb * KB : kb * KB;
+                Frag vf[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) vf[t] = M::col(vcol + bj * PV + t * 16, PV);
+#pragma unroll
+                for (int i = kb * B; i < NI; ++i)
+#pragma unroll
+                    for (int m = 0; m < NA; ++m) {
+                        const Frag af = M::near(as + (m * C + block(i) * 16 + lr) * PA + bj + g * M::kNear);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) acc[i][t] = M::mul(vf[t], af, acc[i][t]);
+                    }
+            }
+            // lane: row lr of a block of 16, columns 4 g .. 4 g + 3
+            if (kWhole && tile) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) {
+                        T* to = qs + (block(i) * 16 + lr) * PK + Tile<IO>::col(lr, wc + t * 16 + g * 4);
+                        const f32x4 x = acc[i][t];
+                        if constexpr (IO == kRowBf16) *reinterpret_cast<u32x2*>(to) = u32x2{pair(x[0], x[1]), pair(x[2], x[3])};
+                        else *reinterpret_cast<f32x4*>(to) = x;
+                    }
+                left = n;
+            } else {
+                const int64_t base = out_row(low(p, n));
+                const bool f32 = IO == kRowF32 || R.out32;
+                const uint32_t size = f32 ? 4 : 2;
+                const __amdgpu_buffer_rsrc_t to = row_block(static_cast<char*>(R.out) + base * size, (uint32_t)((n - 1) * out_ld + R.Do) * size);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int c = col0 + wc + t * 16 + g * 4;
+                    const uint32_t off = ((uint32_t)lr * (uint32_t)out_ld + c) * size;
+#pragma unroll
+                    for (int i = 0; i < NI; ++i) {
+                        const int bi = block(i) * 16;
+                        const f32x4 x = acc[i][t];
+                        if constexpr (BY == 16) {
+                            const uint32_t at = bi + lr < n && c < R.Do ? off + (uint32_t)bi * (uint32_t)out_ld * size : kOutside;
+                            if (f32) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), to, at, 0, 0);
+                            else __builtin_amdgcn_raw_buffer_store_b64(u32x2{pair(x[0], x[1]), pair(x[2], x[3])}, to, at, 0, 0);
+                        } else if (bi + lr < n) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int64_t o = base + (bi + lr) * out_ld + c + e;
+                                if (c + e >= R.Do) continue;
+                                if (f32) static_cast<float*>(R.out)[o] = x[e];
+                                else static_cast<uint16_t*>(R.out)[o] = Entry<kRowBf16>::put(x[e]);
                             }
                         }
                     }
                 }
             }
-            if (p + C < rows || to_state) {
-                // the state behind the chunk
-                const float keep = pw[n];
+        }
+        if (p + C < rows || to_state) {
+            // the state behind the chunk
+            const float keep = pw[n];
 #pragma unroll
-                for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) S[d][t] *= keep;
-                const float* in = LATE ? up : down + C - n;
+                for (int t = 0; t < NT; ++t) S[d][t] *= keep;
+            const float* in = LATE ? up : down + C - n;
 #pragma unroll
-                for (int kb = 0; kb < C / KB; ++kb) {
-                    Frag f[NT][NV];
+            for (int kb = 0; kb < C / KB; ++kb) {
+                Frag f[NT][NV];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const Frag vf = M::col(vcol + kb * KB * PV + t * 16, PV);
+                    float e[8];
+#pragma unroll
+                    for (int r = 0; r < E; ++r) e[r] = M::get(vf, r) * in[kb * KB + g * M::kNear + r];
+                    split<IO>(e, f[t]);
+                }
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const Frag kf = M::col(kcol + kb * KB * PK + d * 16, PK);
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        const Frag vf = M::col(vcol + kb * KB * PV + t * 16, PV);
-                        float e[8];
 #pragma unroll
-                        for (int r = 0; r < E; ++r) e[r] = M::get(vf, r) * in[kb * KB + g * M::kNear + r];
-                        split<IO>(e, f[t]);
-                    }
-#pragma unroll
-                    for (int d = 0; d < ND; ++d) {
-                        const Frag kf = M::col(kcol + kb * KB * PK + d * 16, PK);
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-                            for (int m = 0; m < NV; ++m) S[d][t] = M::mul(kf, f[t][m], S[d][t]);
-                        }
+                        for (int m = 0; m < NV; ++m) S[d][t] = M::mul(kf, f[t][m], S[d][t]);
                     }
                 }
             }
@@ -725,8 +722,9 @@ hipError_t launch_attn_scan(const AttnScan& a, bool full, bool wide, hipStream_t
     for (int r = 0; r < a.roles; ++r) {
         const AttnRole& R = a.role[r];
         by = std::min({by, load_bytes(R.q, R.Dc, b ? 2 : 4), load_bytes(R.k, R.Dc, b ? 2 : 4), load_bytes(R.v, R.Do, b ? 2 : 4)});
-        // with 16 rows of out are stored four entries at a time, at offsets of 32 bits within a chunk
-        if (full && (R.Do % 4 != 0 || reinterpret_cast<uintptr_t>(R.out) % 16 != 0 || (int64_t)a.H * R.Do > 1 << 24)) by = std::min(by, 4);
+        // with 16 rows of out are stored four entries at a time, at offsets below kOutside within a chunk
+        const int64_t chunk = (int64_t)(b ? Mat<kRowBf16>::kChunk : Mat<kRowF32>::kChunk) * a.H * R.Do * (b && !R.out32 ? 2 : 4);
+        if (full && (R.Do % 4 != 0 || reinterpret_cast<uintptr_t>(R.out) % 16 != 0 || chunk > (int64_t)kOutside)) by = std::min(by, 4);
     }
     // 128 columns: two blocks a wave, or for rows past 128 entries, whose state needs the registers, one
     constexpr int NW = DC > 128 ? 8 : 4, NT = DC > 128 ? 1 : 2;

@@ -164,6 +164,24 @@ def test_many_heads(H, D, share, dtype):
     part.check_bwd((of(grads[0], users), of(grads[1], shared), of(grads[2], shared), of(grads[3], users)))
 
 
+def test_rows_of_eight_million_entries():
+    """Very many heads: the fp32 rows of a chunk, from which shared heads' gradients are summed, take 2^31 bytes and
+    more.  Six heads against the reference."""
+    H, D, T, share = 40000, 216, 64, 2
+    g = torch.Generator(DEV).manual_seed(4)
+    q, k, v, do = (torch.randn(T, n, D, generator=g, device=DEV, dtype=torch.bfloat16) for n in (H, H // share, H // share, H))
+    rate = torch.linspace(2.0 ** -8, 1.0, H, device=DEV)
+    cu = torch.tensor([0, T], dtype=torch.int32, device=DEV)
+    o, fin = pdssm.decay_attn_fwd(q, k, v, rate, scale=D ** -0.5, cu=cu)
+    grads = pdssm.decay_attn_bwd(q, k, v, rate, do, scale=D ** -0.5, cu=cu)
+    picked = [0, H // 2, H - share]
+    users, shared = [h + i for h in picked for i in range(share)], [h // share for h in picked]
+    part = Case([0, T], len(users), D, D, torch.bfloat16, heads=(len(users), len(shared), len(shared)), states=False)
+    part.q, part.k, part.v, part.do, part.rate = q[:, users], k[:, shared], v[:, shared], do[:, users], rate[users]
+    part.check_fwd(o[:, users], fin[:, users])
+    part.check_bwd((grads[0][:, users], grads[1][:, shared], grads[2][:, shared], grads[3][:, users]))
+
+
 def test_outputs_that_go_past_the_caches():
     """64 MB and more of bf16 rows; two heads of them against the reference."""
     L, S, H = 2048, 16, 17
