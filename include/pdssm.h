@@ -582,7 +582,9 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
  * sums.  With bf16 rows the products run on bf16 numbers: the rows, which are exact in
  * it; the rows that go into a state, weighted, as sums of three such numbers (24 bits; of two in a
  * backward pass for states that only row gradients are made of); and, where a row output is made of
- * them, states and weighted scores, rounded to one, or in calls that leave CUs idle to the sum of two.
+ * them, states and weighted scores as sums of two.  Two are off by 2^-16 of the number, so a row output
+ * is off by its own rounding and by 2^-16 of its terms' magnitudes.  q . k and its terms have to be in
+ * the range of fp32.
  * Outputs are rounded to nearest even.
  *
  * Sequences are as for the gated layers: S of T / S rows each, or cu [S+1], and

@@ -61,6 +61,39 @@ def bwd(q, k, v, rate, do, scale, bounds, h0=None, dh_final=None, absolute=False
     return dict(dq=together(dq, heads[0]), dk=together(dk, heads[1]), dv=together(dv, heads[2]), dh0=after)
 
 
+def to_bf16(x):
+    """float64 rounded to bf16, to nearest even (numbers in the range of normal ones)."""
+    x = np.asarray(x, np.float64)
+    m, e = np.frexp(x)
+    return np.ldexp(np.round(m * 256), e - 8)
+
+
+# How far bf16 results may be off as a whole; entry by entry there is only the size of the terms, which is
+# tens of times an entry where a thousand of them add up.
+#
+# A row output is rounded once.  That alone is off by the rms of to_bf16(want) - want.  Scores, states and weighted rows
+# are sums of two or three bf16 numbers, off by 2^-16 of themselves at most and each for itself, so what they bring in
+# is 2^-16 of the root of the sum of an output's terms squared: 0.4 of the rounding up to terms a hundred
+# times an output.  Squares add: 1 + 0.16 + what fp32 sums bring.
+ROWS_OFF = 1.1
+# A state's weighted rows are sums of three bf16 numbers (2^-24 of themselves); weights are rounded to fp32 and
+# so are products, and each chunk rounds a weight, a product and two sums of 32 rows by three numbers:
+# 16 roundings of 2^-24 that are not independent.  Of two bf16 numbers the rows are off by 2^-16 at most and 2.5e-6 in the mean.
+STATES_OFF = 16 * 2.0 ** -24
+
+
+def rows_off(got, want):
+    """For each head of rows [T, heads, D], the rms error in units of what one rounding to bf16 makes."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    return np.sqrt(((got - want) ** 2).sum((0, 2)) / ((to_bf16(want) - want) ** 2).sum((0, 2)))
+
+
+def states_off(got, want):
+    """For each state of [S, H, Dk, Dv], the rms error relative to its rms."""
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    return np.sqrt(((got - want) ** 2).sum((2, 3)) / (want ** 2).sum((2, 3)))
+
+
 def _sigmoid(z):
     with np.errstate(over="ignore"):
         return 1 / (1 + np.exp(-z))

@@ -93,7 +93,6 @@ struct AttnScan {
     int members;         // workgroups of a head's segment, over all roles
     int64_t groups;      // items * H
     int past;            // out goes past the caches
-    int fine;            // bf16 rows: operands of more bits in two terms each
 };
 
 // States only (full = 0): what the rows of each segment but the last add.

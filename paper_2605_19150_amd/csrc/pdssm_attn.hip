@@ -213,7 +213,6 @@ void add_role(AttnScan& n, const AttnRole& r, bool wide) {
     to.slices = slices(r.Do, wide);
     n.members += to.slices;
     n.past = n.past || (int64_t)n.T * n.H * r.Do * (n.io == kRowBf16 ? 2 : 4) >= kPast;
-    n.fine = n.groups * n.members <= kFill / 2;  // one on a CU at most
 }
 
 // The states that segments begin with, of the roles in n.

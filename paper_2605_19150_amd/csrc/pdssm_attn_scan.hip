@@ -43,19 +43,15 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// With bf16 rows, the bf16 numbers whose sum an operand of more bits is taken as.
-struct Terms {
-    int state;  // the state where a row reads it
-    int score;  // weighted scores
-    int row;    // weighted rows that go into the state
-};
-// Three hold the 24 bits of what goes into a state that is an output, a sum in fp32 (two: 2.5e-6 off in
-// place of 2e-7).  One is off by at most 2^-8 of the value, as a row output is by its own
-// rounding: the two together make row outputs 1.4 times as far off as the rounding alone does.
-// Two of each cost 18 % at 8 x 4096 rows of 32 heads of 128 (688 -> 813 us backward), and nothing
-// where CUs are idle: calls that leave some take two.  Three terms for the states of dq and dk, which
-// only rows are made of, would cost 5 % (724 us).
-constexpr Terms kFine = {2, 2, 3}, kOut = {1, 1, 3}, kInner = {1, 1, 2};
+// With bf16 rows, the bf16 numbers whose sum an operand of more bits is taken as.  The state where a row reads it and
+// weighted scores: kTerms, off by 2^-16 of themselves, so that a row output is off by its own rounding alone, also where
+// k or v stands ten deviations off centre and what it is multiplied by has no constant part.  With one number
+// rows were 1.4 times as far off, and 9 times in that case, for 8 to 16 % less time (703 us in place of 815 backward
+// at 8 x 4096 rows of 32 heads of 128).
+// Weighted rows that go into a state: kRow, the 24 bits of what a sum in fp32 holds (with two a state is 2.5e-6 off in
+// place of 2e-7), or kInner in the scans of dq and dk, whose states rows alone are made of, by way of
+// kTerms numbers.
+constexpr int kTerms = 2, kRow = 3, kInner = 2;
 
 // A tile of rows in LDS.  Its pitch is 8 banks past a multiple of 64 (bf16), and of
 // rows 8 to 15 of each 16 the 16-byte pieces change places in pairs: so neither 16 lanes with
@@ -251,7 +247,7 @@ template <int IO, int DC, int W, bool FULL>
 struct Shared {
     using T = typename Mat<IO>::T;
     static constexpr int C = Mat<IO>::kChunk, PK = DC + Tile<IO>::kPad, PV = W + Tile<IO>::kPad, PA = C + 16 / sizeof(T);
-    static constexpr int NA = Mat<IO>::kSplit ? kFine.score : 1;
+    static constexpr int NA = Mat<IO>::kSplit ? kTerms : 1;
     alignas(16) T ks[C * PK];
     alignas(16) T vs[C * PV];
     alignas(16) T qs[FULL ? C * PK : 8];
@@ -263,7 +259,7 @@ struct Shared {
 };
 
 // The scan of a segment of a head, for the W columns of out from W * member on.
-template <int IO, int DC, int NW, int NT, bool FULL, int BY, bool LATE, int STATE, int SCORE, int ROW>
+template <int IO, int DC, int NW, int NT, bool FULL, int BY, bool LATE, int ROW>
 __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& R, int64_t group, int member,
                                              Shared<IO, DC, NW * NT * 16, FULL>& lds) {
     using M = Mat<IO>;
@@ -271,7 +267,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
     using Frag = typename M::Frag;
     constexpr int C = M::kChunk, KB = M::kDepth, W = NW * NT * 16, NTH = NW * 64, B = KB / 16;
     constexpr int PK = DC + Tile<IO>::kPad, PV = W + Tile<IO>::kPad, PA = C + 16 / sizeof(T), NI = C / 16, ND = DC / 16, E = KB / 4;
-    constexpr int NS = M::kSplit ? STATE : 1, NA = M::kSplit ? SCORE : 1, NV = M::kSplit ? ROW : 1;
+    constexpr int NS = M::kSplit ? kTerms : 1, NA = NS, NV = M::kSplit ? ROW : 1;
     T *const ks = lds.ks, *const vs = lds.vs, *const qs = lds.qs, *const as = lds.as;
     float *const up = lds.up, *const down = lds.down, *const pw = lds.pw;
     int& bad = lds.bad;
@@ -682,20 +678,15 @@ __global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : 2) void k_attn_scan(At
     while (ri + 1 < a.roles && member >= a.role[ri].slices) member -= a.role[ri++].slices;
     const AttnRole& R = a.role[ri];
     // slower loads do without the variant that is faster
-    const bool fine = FULL && (a.fine || BY != 16), out = !FULL || R.fin;
-    if (R.late) {
-        if (fine || IO == kRowF32) scan_segment<IO, DC, NW, NT, FULL, BY, true, kFine.state, kFine.score, kFine.row>(a, R, group, member, lds);
-        else if constexpr (IO == kRowBf16 && (BY == 16 || !FULL)) {
-            if (out) scan_segment<IO, DC, NW, NT, FULL, BY, true, kOut.state, kOut.score, kOut.row>(a, R, group, member, lds);
-            else if constexpr (FULL) scan_segment<IO, DC, NW, NT, FULL, BY, true, kInner.state, kInner.score, kInner.row>(a, R, group, member, lds);
-        }
-    } else {
-        if (fine || IO == kRowF32) scan_segment<IO, DC, NW, NT, FULL, BY, false, kFine.state, kFine.score, kFine.row>(a, R, group, member, lds);
-        else if constexpr (IO == kRowBf16 && (BY == 16 || !FULL)) {
-            if (out) scan_segment<IO, DC, NW, NT, FULL, BY, false, kOut.state, kOut.score, kOut.row>(a, R, group, member, lds);
-            else if constexpr (FULL) scan_segment<IO, DC, NW, NT, FULL, BY, false, kInner.state, kInner.score, kInner.row>(a, R, group, member, lds);
+    if constexpr (FULL && IO == kRowBf16 && BY == 16) {
+        if (!R.fin) {
+            if (R.late) scan_segment<IO, DC, NW, NT, FULL, BY, true, kInner>(a, R, group, member, lds);
+            else scan_segment<IO, DC, NW, NT, FULL, BY, false, kInner>(a, R, group, member, lds);
+            return;
         }
     }
+    if (R.late) scan_segment<IO, DC, NW, NT, FULL, BY, true, kRow>(a, R, group, member, lds);
+    else scan_segment<IO, DC, NW, NT, FULL, BY, false, kRow>(a, R, group, member, lds);
 }
 
 template <int IO, int DC, int NW, int NT, bool FULL>

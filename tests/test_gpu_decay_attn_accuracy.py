@@ -1,0 +1,69 @@
+"""Attention with bf16 rows as a whole, head by head: row outputs are off by the
+rounding of the output and little else, states by what fp32 sums make
+(oracle.decay_attn.ROWS_OFF and STATES_OFF, which say why; what they see is
+tested without a GPU)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decay_attn as R
+from test_gpu_decay_attn import DEV, Case, _np
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def _fill(H, D, bounds, share=1, seed=0, **kw):
+    return Case(bounds, H, *D, BF16, heads=(H, H // share, H // share), seed=seed, **kw)
+
+
+def _check(c, got, grads, picked, share=1):
+    """Heads of keys and values in picked, and the users of each, against the reference."""
+    users = [h * share + k for h in picked for k in range(share)]
+    of = lambda t, heads: _np(t.reshape(c.T, -1, t.shape[-1])[:, heads])  # noqa: E731
+    q, k, v, do = of(c.q, users), of(c.k, picked), of(c.v, picked), of(c.do, users)
+    rate, h0, dhf = _np(c.rate)[users], _np(c.h0[:, users]), _np(c.dhf[:, users])
+    o, fin = R.fwd(q, k, v, rate, c.scale, c.bounds, h0)
+    want = R.bwd(q, k, v, rate, do, c.scale, c.bounds, h0, dhf)
+    for name, x, heads, y in (("o", got[0], users, o), ("dq", grads[0], users, want["dq"]), ("dk", grads[1], picked, want["dk"]),
+                              ("dv", grads[2], picked, want["dv"])):
+        off = R.rows_off(of(x, heads), y)
+        assert (off < R.ROWS_OFF).all(), (name, off)
+    for name, x, y in (("h_final", got[1], fin), ("dh0", grads[3], want["dh0"])):
+        off = R.states_off(_np(x[:, users]), y)
+        assert (off < _states_bound(c)).all(), (name, off)
+
+
+def _states_bound(c):
+    # weights of chunks, rounded to fp32, multiply where a state outlives several of them
+    return R.STATES_OFF + 2.0 ** -24 * min(c.longest / 64, 1 / (64 * float(c.rate.min())))
+
+
+@pytest.mark.parametrize("H,D,share", [(300, (64, 64), 1), (300, (40, 64), 1), (140, (128, 128), 1), (140, (96, 72), 2),
+                                       (130, (200, 72), 1), (130, (72, 256), 1), (320, (64, 64), 4)], ids=str)
+def test_calls_that_fill_the_card(H, D, share):
+    c = _fill(H, D, [0, 70, 271], share, seed=H)
+    _check(c, c.fwd(), c.bwd(), [0, H // share // 2, H // share - 1], share)
+
+
+@pytest.mark.parametrize("H,D,share,pad", [(2, (64, 64), 1, 0), (4, (40, 64), 2, 1), (2, (128, 96), 1, 2), (1, (256, 256), 1, 0)],
+                         ids=str)
+def test_calls_that_leave_cus_idle(H, D, share, pad):
+    """Few heads, some of whose sequences are cut; rows at odd addresses, too."""
+    c = _fill(H, D, [0, 0, 1200, 1200, 1500], share, pad=pad, seed=pad, rate=[2.0 ** -3 / 4 ** h for h in range(H)])
+    _check(c, c.fwd(), c.bwd(), list(range(H // share)), share)
+
+
+@pytest.mark.parametrize("H", [1, 300])
+@pytest.mark.parametrize("centre", [1.0, 4.0, 10.0])
+@pytest.mark.parametrize("which", ["qk", "vdo"])
+def test_rows_that_cancel(which, centre, H):
+    """Keys or values off centre, and what they are multiplied by without a constant part, as the gradient of a norm is: the
+    state's entries are much larger than their sum."""
+    c = _fill(H, (64, 64), [0, 1024], states=False, rate=[2.0 ** -9] if H == 1 else np.geomspace(2.0 ** -2, 2.0 ** -9, H, dtype=np.float32))
+    c.h0 = torch.zeros(1, H, 64, 64, device=DEV)
+    c.dhf = torch.zeros_like(c.h0)
+    flat, shifted = (c.q, c.k) if which == "qk" else (c.do, c.v)
+    flat.copy_(flat.float() - flat.float().mean(2, keepdim=True))
+    shifted.copy_(shifted.float() + centre)
+    _check(c, c.fwd(), c.bwd(), [0, H // 2, H - 1] if H > 1 else [0])
