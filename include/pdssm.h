@@ -601,7 +601,8 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
  * by one, with those behind them in their segment, many times slower.
  *
  * Results are deterministic, but depend in their last bits on how many rows and
- * heads a call has: long sequences of few heads are cut into segments. */
+ * heads a call has (long sequences of few heads are cut into segments) and on the
+ * alignment of its rows; not on which optional outputs it has. */
 typedef struct pdssm_heads {
     const void* p;  /* entry (t, head, d) at p + t*ld + head*hs + d */
     int64_t ld;     /* entries from one row to the next, 0 <= ld <= 2^24 */

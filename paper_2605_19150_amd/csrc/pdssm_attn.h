@@ -78,6 +78,7 @@ struct AttnRole {
     int Dc, Do;           // entries of q and k rows, of v rows
     int rs, cs;           // entry (c, o) of a state at c * rs + o * cs
     int late;
+    int inner;            // dq and dk: rows alone are made of the states
     int slices;           // workgroups that share the Do columns
 };
 struct AttnScan {

@@ -312,6 +312,7 @@ hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t s) {
     dq.Do = a.Dk;
     dq.rs = 1;
     dq.cs = a.Dv;
+    dq.inner = 1;
     dk = dq;
     dk.q = a.v;
     dk.k = a.dout;

@@ -679,7 +679,7 @@ __global__ __launch_bounds__(NW * 64, DC > 128 ? NW / 4 : 2) void k_attn_scan(At
     const AttnRole& R = a.role[ri];
     // slower loads do without the variant that is faster
     if constexpr (FULL && IO == kRowBf16 && BY == 16) {
-        if (!R.fin) {
+        if (R.inner) {
             if (R.late) scan_segment<IO, DC, NW, NT, FULL, BY, true, kInner>(a, R, group, member, lds);
             else scan_segment<IO, DC, NW, NT, FULL, BY, false, kInner>(a, R, group, member, lds);
             return;

@@ -2,11 +2,14 @@
 rounding of the output and little else, states by what fp32 sums make
 (oracle.decay_attn.ROWS_OFF and STATES_OFF, which say why; what they see is
 tested without a GPU)."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import decay_attn as R
+from paper_2605_19150_amd import pdssm
 from test_gpu_decay_attn import DEV, Case, _np
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +70,22 @@ def test_rows_that_cancel(which, centre, H):
     flat.copy_(flat.float() - flat.float().mean(2, keepdim=True))
     shifted.copy_(shifted.float() + centre)
     _check(c, c.fwd(), c.bwd(), [0, H // 2, H - 1] if H > 1 else [0])
+
+def test_rows_do_not_depend_on_whether_states_are_asked_for():
+    """The C entries without h_final and without dh0, in a call that fills the card."""
+    H, D, T = 300, 64, 200
+    c = _fill(H, (D, D), [0, 70, T])
+    (o, _), (dq, dk, dv, _) = c.fwd(), c.bwd()
+    desc = ctypes.byref(pdssm.AttnDesc(T, 2, H, H, H, H, D, D, c.scale, pdssm.FLAG_BF16_IO))
+    heads = [ctypes.byref(pdssm.Heads(t.data_ptr(), t.stride(0), t.stride(1))) for t in (c.q, c.k, c.v, c.do)]
+    lib, at = pdssm.load(), lambda t: t.data_ptr()  # noqa: E731
+    ws = [torch.empty(max(lib.pdssm_decay_attn_workspace_size(desc, 1, op), 1), dtype=torch.uint8, device=DEV)
+          for op in (pdssm.OP_FWD, pdssm.OP_BWD)]
+    outs = [torch.empty_like(t) for t in (o, dq, dk, dv)]
+    s = torch.cuda.current_stream().cuda_stream
+    assert lib.pdssm_decay_attn_fwd(desc, *heads[:3], at(c.rate), at(c.cu), at(c.h0), at(outs[0]), None, at(ws[0]), ws[0].numel(),
+                                    None, s) == 0
+    assert lib.pdssm_decay_attn_bwd(desc, *heads, at(c.rate), at(c.cu), at(c.h0), at(c.dhf), *(at(t) for t in outs[1:]), None,
+                                    at(ws[1]), ws[1].numel(), None, s) == 0
+    for name, x, y in zip(("o", "dq", "dk", "dv"), outs, (o, dq, dk, dv)):
+        assert torch.equal(x, y), name
