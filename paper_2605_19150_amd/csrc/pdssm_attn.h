@@ -39,7 +39,7 @@ struct AttnArgs {
     float* dh0;         // [S, H, Dk, Dv] or null
 };
 size_t attn_workspace(const AttnArgs& a, bool bwd);
-// Whether the launches of these sizes stay below 2^32 threads.
+// Whether the launches of these sizes stay below 2^32 threads along an axis of the grid.
 bool attn_fits(const AttnArgs& a, bool bwd);
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_bwd(const AttnArgs& a, hipStream_t s);
@@ -95,6 +95,9 @@ struct AttnScan {
     int64_t groups;      // items * H
     int past;            // out goes past the caches
 };
+
+// Threads of a workgroup of the scan of rows of up to Dc entries.
+constexpr int attn_threads(int Dc, bool full, bool wide) { return wide && (!full || Dc > 128) ? 512 : 256; }
 
 // States only (full = 0): what the rows of each segment but the last add.
 template <int DC>

@@ -260,9 +260,17 @@ size_t attn_workspace(const AttnArgs& a, bool bwd) { return space(a, plan(a, bwd
 
 bool attn_fits(const AttnArgs& a, bool bwd) {
     const Plan p = plan(a, bwd);
-    const int64_t parts = ((int64_t)a.Dk * a.Dv + kPart - 1) / kPart;
-    return ((int64_t)p.items * a.H + 7) * members(a, bwd) < (1 << 24) &&
-           (p.slots == 0 || (a.cu ? p.slots : a.S) * parts * a.H * 2 < (1 << 24));
+    const bool wide = wide_cols(a, bwd);
+    const int64_t groups = ((int64_t)p.items * a.H + 7) / 8 * 8, most = 1LL << 32;
+    auto fits = [&](int Dc, bool full, int members) { return groups * members * attn_threads(Dc, full, wide) < most; };
+    const int k = slices(a.Dk, wide), v = slices(a.Dv, wide);
+    if (p.slots) {
+        const int64_t parts = ((int64_t)a.Dk * a.Dv + kPart - 1) / kPart;
+        if (!fits(a.Dk, false, bwd ? 2 * v : v) || (a.cu ? p.slots : a.S) * parts * a.H * 2 >= (1 << 24)) return false;
+    }
+    if (!bwd) return fits(a.Dk, true, v);
+    if (length_class(a.Dk) == length_class(a.Dv)) return fits(a.Dk, true, 2 * k + v);
+    return fits(a.Dv, true, 2 * k) && fits(a.Dk, true, v);
 }
 
 hipError_t launch_attn_fwd(const AttnArgs& a, hipStream_t s) {

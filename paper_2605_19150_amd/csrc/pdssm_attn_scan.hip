@@ -718,13 +718,14 @@ hipError_t launch_attn_scan(const AttnScan& a, bool full, bool wide, hipStream_t
         if (full && (R.Do % 4 != 0 || reinterpret_cast<uintptr_t>(R.out) % 16 != 0 || chunk > (int64_t)kOutside)) by = std::min(by, 4);
     }
     // 128 columns: two blocks a wave, or for rows past 128 entries, whose state needs the registers, one
-    constexpr int NW = DC > 128 ? 8 : 4, NT = DC > 128 ? 1 : 2;
+    constexpr int NW = attn_threads(DC, true, true) / 64, NT = DC > 128 ? 1 : 2;
+    static_assert(attn_threads(DC, false, true) == 512 && attn_threads(DC, true, false) == 256 && attn_threads(DC, false, false) == 256, "waves below");
     void (*f)(AttnScan);
     if (b) f = full ? (wide ? pick<kRowBf16, DC, NW, NT, true>(by) : pick<kRowBf16, DC, 4, 1, true>(by))
                     : (wide ? pick<kRowBf16, DC, 8, 1, false>(by) : pick<kRowBf16, DC, 4, 1, false>(by));
     else f = full ? (wide ? pick<kRowF32, DC, NW, NT, true>(by) : pick<kRowF32, DC, 4, 1, true>(by))
                   : (wide ? pick<kRowF32, DC, 8, 1, false>(by) : pick<kRowF32, DC, 4, 1, false>(by));
-    hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(!wide ? 256 : full ? NW * 64 : 512), 0, s, a);
+    hipLaunchKernelGGL(f, dim3((unsigned)n), dim3(attn_threads(DC, full, wide)), 0, s, a);
     return hipGetLastError();
 }
 template hipError_t launch_attn_scan<PDSSM_DC>(const AttnScan&, bool, bool, hipStream_t);

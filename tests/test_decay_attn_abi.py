@@ -168,6 +168,28 @@ def test_launches_past_the_grid(lib):
     assert c.step() == ERR_UNSUPPORTED
 
 
+M = 1 << 20
+
+
+@pytest.mark.parametrize("H,Dk,Dv,T,op,fits,refused", [
+    (8, 1, 72, 1000, OP_FWD, M - 8, M - 7),               # 7 segments more than sequences: states alone, more than 64 columns
+    (1, 1, 72, 1000, OP_BWD, 4 * M - 15, 4 * M - 7),      # two scans of states alone
+    (8, 129, 65, None, OP_FWD, M - 1, M),                 # rows past 128 entries
+    (2, 130, 256, None, OP_BWD, 699048, 699052),          # six workgroups a head
+    (8, 1, 72, 100, OP_FWD, 2 * M - 1, 2 * M),            # 256 threads each: nothing is cut
+    (8, 128, 65, None, OP_FWD, 2 * M - 1, 2 * M)], ids=str)
+def test_launches_of_512_threads(lib, H, Dk, Dv, T, op, fits, refused):
+    """2^32 threads and more are refused: 2^23 workgroups of the scan where they have 512 threads, 2^24 where they have 256.
+    T rows of packed sequences, or a row for each."""
+    for S, bad in ((fits, False), (refused, True)):
+        d = AttnDesc(T or S, S, H, H, H, H, Dk, Dv, 1.0, 0)
+        assert (lib.pdssm_decay_attn_workspace_size(P(d), int(T is not None), op) == BAD) == bad
+    c = Attn(lib)
+    c.d, c.ws, c.h0, c.fin, c.dhf, c.dh0 = d, _at(10), None, None, None, None
+    c.cu = c.cu if T else None
+    assert (c.fwd if op == OP_FWD else c.bwd)() == ERR_UNSUPPORTED
+
+
 class Norm:
     def __init__(self, lib, T=300, C=96, G=6, act=1, eps=1e-5, flags=0):
         self.lib, self.d = lib, NormDesc(T, C, G, act, eps, flags)
