@@ -89,3 +89,20 @@ def test_rows_do_not_depend_on_whether_states_are_asked_for():
                                     at(ws[1]), ws[1].numel(), None, s) == 0
     for name, x, y in zip(("o", "dq", "dk", "dv"), outs, (o, dq, dk, dv)):
         assert torch.equal(x, y), name
+
+
+def test_sums_of_shared_heads_by_more_than_2_32_threads():
+    """Three tensors of gradients, each the sum over two heads: 2734 x 2048 x 3 workgroups of 256.  Two pairs against the
+    reference."""
+    H, D, T, share = 5488, 255, 2048, 2
+    g = torch.Generator(DEV).manual_seed(3)
+    q, k, v, do = (torch.randn(T, n, D, generator=g, device=DEV, dtype=BF16) for n in (H // share,) * 3 + (H,))
+    rate = torch.linspace(2.0 ** -5, 1.0, H, device=DEV)
+    cu = torch.tensor([0, T], dtype=torch.int32, device=DEV)
+    grads = pdssm.decay_attn_bwd(q, k, v, rate, do, scale=D ** -0.5, cu=cu)
+    for h in (0, H // share - 1):
+        users = [2 * h, 2 * h + 1]
+        want = R.bwd(*(_np(t[:, [h]]) for t in (q, k, v)), _np(rate[users]), _np(do[:, users]), D ** -0.5, [0, T])
+        for name, t in zip(("dq", "dk", "dv"), grads):
+            off = R.rows_off(_np(t[:, [h]]), want[name])
+            assert (off < R.ROWS_OFF).all(), (h, name, off)
