@@ -79,6 +79,7 @@ struct AttnRole {
     int rs, cs;           // entry (c, o) of a state at c * rs + o * cs
     int late;
     int inner;            // dq and dk: rows alone are made of the states
+    int past;             // out goes past the caches: large, and its heads' rows are whole pieces
     int slices;           // workgroups that share the Do columns
 };
 struct AttnScan {
@@ -93,7 +94,6 @@ struct AttnScan {
     const int* cu;
     int members;         // workgroups of a head's segment, over all roles
     int64_t groups;      // items * H
-    int past;            // out goes past the caches
 };
 
 // Threads of a workgroup of the scan of rows of up to Dc entries.

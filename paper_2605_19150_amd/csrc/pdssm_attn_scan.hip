@@ -149,8 +149,8 @@ struct Wild<kRowF32> {
     __device__ __forceinline__ bool any() const { return top >= 0x7f800000u; }
 };
 
-// Cache policy of stores of lines that are whole: past the caches, which a large out would only sweep (162 ->
-// 151 us backward at B16 L2048, 16 heads of 64; for parts of lines it is ruinous).
+// Cache policy of stores past the caches, which a large out would only sweep (160 -> 150 us backward at B16 L2048,
+// 16 heads of 64, with states and scores in one term; for pieces of 32 bytes, an accumulator's, it is ruinous).
 constexpr int kPastCaches = 2;
 constexpr uint32_t kOutside = 0x80000000u;  // an offset past every chunk: loads of zeros, stores that are dropped
 
@@ -437,7 +437,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
             const int r = sq.row + u * Out::kRows;
             const uint32_t off = ((uint32_t)r * (uint32_t)out_ld + sq.c) * (uint32_t)sizeof(T);
             const uint32_t at = r < n && col0 + sq.c < R.Do ? off : kOutside;
-            if (a.past) __builtin_amdgcn_raw_buffer_store_b128(y[u], to, at, 0, kPastCaches);
+            if (R.past) __builtin_amdgcn_raw_buffer_store_b128(y[u], to, at, 0, kPastCaches);
             else __builtin_amdgcn_raw_buffer_store_b128(y[u], to, at, 0, 0);
         }
     };

@@ -91,6 +91,23 @@ def test_rows_do_not_depend_on_whether_states_are_asked_for():
         assert torch.equal(x, y), name
 
 
+
+@pytest.mark.parametrize("H,D,share", [(29, 40, 1), (23, 48, 1), (12, 96, 1), (12, 104, 2)], ids=str)
+def test_large_outputs_whose_rows_are_no_whole_lines(H, D, share):
+    """64 MB and more of rows of 80, 96, 192 and 208 bytes; two heads of two sequences against the reference."""
+    L, S = 2048, 16
+    c = Case(list(range(0, S * L + 1, L)), H, D, D, BF16, heads=(H, H // share, H // share), dense=True, seed=D)
+    got, grads = c.fwd(), c.bwd()
+    picked = [1, H // share - 1]
+    users = [h * share + k for h in picked for k in range(share)]
+    part = Case([0, L, 2 * L], len(users), D, D, BF16, heads=(len(users), len(picked), len(picked)), dense=True, states=False)
+    of = lambda t, heads: t.reshape(S * L, -1, D)[2 * L:4 * L, heads]  # noqa: E731
+    part.q, part.k, part.v, part.do = of(c.q, users), of(c.k, picked), of(c.v, picked), of(c.do, users)
+    part.rate, part.h0, part.dhf = c.rate[users], c.h0[2:4, users], c.dhf[2:4, users]
+    _check(part, (of(got[0], users), got[1][2:4, users]), (of(grads[0], users), of(grads[1], picked), of(grads[2], picked),
+                                                          grads[3][2:4, users]), list(range(len(picked))), share)
+
+
 def test_sums_of_shared_heads_by_more_than_2_32_threads():
     """Three tensors of gradients, each the sum over two heads: 2734 x 2048 x 3 workgroups of 256.  Two pairs against the
     reference."""
