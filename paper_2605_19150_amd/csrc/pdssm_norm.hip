@@ -29,9 +29,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBlocks = 512;      // blocks of rows that a call of any width may have
 constexpr int kNormWaves = 4096;  // waves that fill the card
-// Bytes of a row tensor from which on rows go past the caches, which they would only sweep: at 32768 rows of
-// 4096 channels, bf16 with a gate, 183 -> 178 us forward, 291 -> 280 us backward.
+// Bytes of a row tensor from which on rows go past the caches, which they would only sweep, if what a wave has of a
+// row and the row are whole pieces of kPiece bytes.  At 32768 rows, bf16 with a gate: 4096 channels in 32 groups 167 ->
+// 161 us forward, 298 -> 290 us backward, in 512 groups 164 -> 150 and 287 -> 275; 4080 channels, whose rows are not, in
+// 170 groups 218 -> 224 and 376 -> 398, in 102 groups 222 -> 234 and 418 -> 416.
 constexpr int64_t kPast = 64 << 20;
+constexpr int kPiece = 64;
 
 template <int IO, int V, bool PAST>
 __device__ __forceinline__ void load(const void* p, size_t i, float* x) {
@@ -397,7 +400,8 @@ hipError_t rows(NormArgs& a, bool bwd, hipStream_t s) {
     void (*f)(NormArgs);
     unsigned grid;
     if (sh.num) {
-        const bool past = (int64_t)a.T * a.C * (b ? 2 : 4) >= kPast;
+        const int size = b ? 2 : 4, wave = 64 / sh.team * (a.C / a.G) * size;
+        const bool past = (int64_t)a.T * a.C * size >= kPast && a.C * size % kPiece == 0 && wave % kPiece == 0;
         if (sh.vec == 1) f = b ? pick<kRowBf16, 1, false>(sh.num, bwd) : pick<kRowF32, 1, false>(sh.num, bwd);
         else if (past) f = b ? pick<kRowBf16, 8, true>(sh.num, bwd) : pick<kRowF32, 4, true>(sh.num, bwd);
         else f = b ? pick<kRowBf16, 8, false>(sh.num, bwd) : pick<kRowF32, 4, false>(sh.num, bwd);

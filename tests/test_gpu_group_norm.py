@@ -215,6 +215,22 @@ def test_large_calls(dtype):
     near("db", db, _np(du.sum(0)), units * _np(du.abs().sum(0)))
 
 
+@TYPES
+@pytest.mark.parametrize("C,G", [(4080, 170), (4080, 102), (4104, 57), (4096, 512)])
+def test_large_calls_of_odd_pieces(C, G, dtype):
+    """64 MB and more of rows, with and without whole pieces of 64 bytes: the same bits as in calls of some of them."""
+    T = 8400 if dtype == torch.bfloat16 else 4300
+    c = Case(T, C, G, dtype, seed=2)
+    y, (dx, _, _, dgate) = c.fwd(), c.bwd()
+    for a in (0, T - 200):
+        part = Case(1, C, G, dtype)
+        part.T, part.w, part.b = 200, c.w, c.b
+        part.x, part.gate, part.dy = (t[a:a + 200] for t in (c.x, c.gate, c.dy))
+        z, grads = part.fwd(), part.bwd()
+        part.check(z, grads)
+        assert torch.equal(z, y[a:a + 200]) and torch.equal(grads[0], dx[a:a + 200]) and torch.equal(grads[3], dgate[a:a + 200])
+
+
 def test_rows_past_32_bits():
     T, ld = 300, 1 << 23
     buf = torch.zeros(T * ld, dtype=torch.bfloat16, device=DEV)
