@@ -50,10 +50,12 @@ KERNEL_SOURCES = {
     "k_project_wide": ["pdssm_select.hip", "pdssm_select.h", "pdssm_project_rule.h", "pdssm_device.h", "pdssm_io.h"],
     "k_gated_fwd": ["pdssm_gated.hip", "pdssm_gated.h", "pdssm_gated_math.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h"],
     "k_gated_bwd": ["pdssm_gated.hip", "pdssm_gated.h", "pdssm_gated_math.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h"],
-    "k_attn_scan": ["pdssm_attn_scan.hip", "pdssm_attn.h", "pdssm_rows.h", "pdssm_device.h"],
-    "k_attn_step": ["pdssm_attn.hip", "pdssm_attn.h", "pdssm_rows.h", "pdssm_device.h"],
-    "k_norm_fwd": ["pdssm_norm.hip", "pdssm_norm.h", "pdssm_rows.h"],
-    "k_norm_bwd": ["pdssm_norm.hip", "pdssm_norm.h", "pdssm_rows.h"],
+    "k_attn_scan": ["pdssm_attn_scan.hip", "pdssm_attn.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h",
+                    "pdssm_io.h"],
+    "k_attn_step": ["pdssm_attn.hip", "pdssm_attn.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h",
+                    "pdssm_io.h"],
+    "k_norm_fwd": ["pdssm_norm.hip", "pdssm_norm.h", "pdssm_rows.h", "pdssm_kept.h"],
+    "k_norm_bwd": ["pdssm_norm.hip", "pdssm_norm.h", "pdssm_rows.h", "pdssm_kept.h"],
     "k_gated_step": ["pdssm_gated.hip", "pdssm_gated.h", "pdssm_gated_math.h", "pdssm_rows.h", "pdssm_kept.h", "pdssm_device.h"],
     "k_pack8": ["pdssm_kept.hip", "pdssm_kept.h", "pdssm_rows.h", "pdssm_device.h"],
     "k_unpack8": ["pdssm_kept.hip", "pdssm_kept.h", "pdssm_rows.h", "pdssm_device.h"],

@@ -3,7 +3,11 @@ traffic figure of a kernel comes from its traffic summary, never from a
 counter summary of the same kernel and workload, and only while the kernel
 sources are the ones the counters were taken on."""
 import os
+import re
 
+import pytest
+
+from paper_2605_19150_amd import profiling
 from paper_2605_19150_amd.profiling import read_traffic_summary, source_hash
 
 W = "fsa-perm B16 L2048 H16 N64 K16"
@@ -46,3 +50,15 @@ def test_committed_summaries_parse():
                     kv[k] = v
         got = read_traffic_summary(root, kv["kernel"], kv["workload"])
         assert got is None or got > 0, name
+
+
+@pytest.mark.parametrize("kernel", ["k_attn_scan", "k_attn_step", "k_norm_fwd", "k_norm_bwd"])
+def test_a_summary_goes_stale_with_any_header_of_its_kernel(kernel):
+    csrc = os.path.join(profiling.PKG, "csrc")
+    todo, seen = [profiling.KERNEL_SOURCES[kernel][0]], set()
+    while todo:
+        f = todo.pop()
+        seen.add(f)
+        with open(os.path.join(csrc, f), encoding="utf-8") as fh:
+            todo += [m for m in re.findall(r'#include "([^"]+)"', fh.read()) if m not in seen and os.path.exists(os.path.join(csrc, m))]
+    assert seen == set(profiling.KERNEL_SOURCES[kernel])
