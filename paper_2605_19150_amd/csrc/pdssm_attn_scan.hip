@@ -14,7 +14,7 @@
 // hold S with its columns across the lanes and four rows a lane: what an operand of
 // S^T q has to be, when q is read in the same order.  Weighted by powers of a are v
 // (for S') and results; where a product's operand has more bits than bf16 (S, the
-// weighted v, the weighted scores) it is taken as the sum of one to three bf16 numbers.
+// weighted v, the weighted scores) it is taken as the sum of two or three bf16 numbers.
 // fp32 rows go through the fp32 matrix instructions.
 //
 // In reverse rows stand in LDS as they do in memory; scores above the diagonal
@@ -46,16 +46,18 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // With bf16 rows, the bf16 numbers whose sum an operand of more bits is taken as.  The state where a row reads it and
 // weighted scores: kTerms, off by 2^-16 of themselves, so that a row output is off by its own rounding alone, also where
 // k or v stands ten deviations off centre and what it is multiplied by has no constant part.  With one number
-// rows were 1.4 times as far off, and 9 times in that case, for 8 to 16 % less time (703 us in place of 815 backward
-// at 8 x 4096 rows of 32 heads of 128).
-// Weighted rows that go into a state: kRow, the 24 bits of what a sum in fp32 holds (with two a state is 2.5e-6 off in
-// place of 2e-7), or kInner in the scans of dq and dk, whose states rows alone are made of, by way of
-// kTerms numbers.
+// rows were 1.4 times as far off, and 9 times in that case, for 8 to 14 % less time (684 us in place of 800 backward
+// at 8 x 4096 rows of 32 heads of 128, 89 in place of 97 forward at 16 x 2048 of 16 of 64).
+// Weighted rows that go into a state: kRow, the 24 bits of what a sum in fp32 holds (with two a state is 2.4e-6 off in
+// place of 1e-7 to 3e-7), or kInner in the scans of dq and dk, whose states rows alone are made of, by way of
+// kTerms numbers (with three 837 us in place of 800).
 constexpr int kTerms = 2, kRow = 3, kInner = 2;
 
-// A tile of rows in LDS.  Its pitch is 8 banks past a multiple of 64 (bf16), and of
-// rows 8 to 15 of each 16 the 16-byte pieces change places in pairs: so neither 16 lanes with
-// a row each meet in a bank, nor 32 with four neighbouring entries of eight rows.
+// A tile of rows in LDS.  Its pitch is 8 banks past a multiple of 32 (bf16), and of
+// rows 8 to 15 of each 16 the 16-byte pieces change places in pairs, so that 16 lanes with
+// a row each do not meet in a bank.  Reads of columns do: 32 lanes have four entries of rows 0 to 3 and of rows 8 to 11,
+// which begin in the same bank, two lanes a bank.  Such conflicts are two fifths of the cycles that LDS is
+// active in (the counters of the backward and forward at heads of 64 and 128).
 template <int IO>
 struct Tile;
 template <>
@@ -149,8 +151,8 @@ struct Wild<kRowF32> {
     __device__ __forceinline__ bool any() const { return top >= 0x7f800000u; }
 };
 
-// Cache policy of stores past the caches, which a large out would only sweep (160 -> 150 us backward at B16 L2048,
-// 16 heads of 64, with states and scores in one term; for pieces of 32 bytes, an accumulator's, it is ruinous).
+// Cache policy of stores past the caches, which a large out would only sweep (176 -> 168 us backward at B16 L2048,
+// 16 heads of 64; for pieces of 32 bytes, an accumulator's, it is ruinous).
 constexpr int kPastCaches = 2;
 constexpr uint32_t kOutside = 0x80000000u;  // an offset past every chunk: loads of zeros, stores that are dropped
 
@@ -420,8 +422,8 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
 
     // Rows of out as whole lines: a chunk's are put into the place of its q, and the threads that stage the
     // next q there take them out first (each the 16 bytes that it will overwrite).  Stored as the
-    // accumulators hold them, 32 bytes of a row at a time, they cost a twelfth more at rows
-    // of 64 entries (174 -> 160 us backward at B16 L2048, 16 heads), 4 % at 128.
+    // accumulators hold them, 32 bytes of a row at a time, they cost 7 % more at rows
+    // of 64 entries (180 -> 168 us backward at B16 L2048, 16 heads), 2 % at 128.
     constexpr bool kWhole = FULL && BY == 16 && DC == W;
     const bool tile = kWhole && (IO == kRowF32 || !R.out32);
     int left = 0;  // rows of out that are there
