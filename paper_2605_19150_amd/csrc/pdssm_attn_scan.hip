@@ -130,6 +130,16 @@ struct Mat<kRowF32> {
     static __device__ __forceinline__ float get(Frag f, int e) { return f[e]; }
 };
 
+// The hardware does not hold back a reader of a matrix instruction's result: the compiler has to keep up to ten wait
+// states between them.  Where the paths between them join behind a short branch it counts along one path only and
+// may leave too few (scores of fp32 rows past 128 entries lost their last product that way).  So no branch stands behind
+// the scores, and the ten states stand here behind products that a later block reads.
+__device__ __forceinline__ void settle() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 9");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // Whether one of a wave's entries is an infinity or a NaN.
 template <int IO>
 struct Wild;
@@ -465,14 +475,18 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
                 int i = 0, j = b;
                 while (j > i) j -= ++i;
                 const int bi = block(i) * 16, bj = block(j) * 16;
+                // weights first: no branch may stand between the products and what reads them (settle)
+                float far = one;
+                for (int d = 1; d < i - j; ++d) far *= sixteen;
+                float w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w[r] = i == j ? w0[r] : w1[r] * far;
                 f32x4 sc = {};
 #pragma unroll
                 for (int kb = 0; kb < DC / KB; ++kb) sc = M::mul(M::near(knear + bj * PK + kb * KB), M::near(qnear + bi * PK + kb * KB), sc);
-                float far = one;
-                for (int d = 1; d < i - j; ++d) far *= sixteen;
                 float e[8] = {};
 #pragma unroll
-                for (int r = 0; r < 4; ++r) e[r] = i == j ? (w0[r] != 0.f ? sc[r] * w0[r] : 0.f) : sc[r] * (w1[r] * far);
+                for (int r = 0; r < 4; ++r) e[r] = w[r] != 0.f ? sc[r] * w[r] : 0.f;
                 Frag f[NA];
                 split<IO>(e, f);
                 T* to = as + (bi + lr) * PA + bj + g * 4;
@@ -603,6 +617,7 @@ __device__ __forceinline__ void scan_segment(const AttnScan& a, const AttnRole& 
                     }
                 }
             }
+            settle();
         }
         __syncthreads();
     }

@@ -120,6 +120,16 @@ def test_packed_sequences(which, D, dtype):
 
 
 @TYPES
+@pytest.mark.parametrize("pad", [0, 1, 2])
+@pytest.mark.parametrize("D", [(256, 16), (16, 256), (256, 64), (200, 48), (255, 33), (136, 8), (128, 48), (96, 20)], ids=str)
+def test_long_rows_of_few_columns(D, pad, dtype):
+    """Products whose results are read at once: every entry of a row counts."""
+    c = Case([0, 14, 28, 60, 190, 400], 2, *D, dtype, pad=pad, seed=D[0])
+    c.check_fwd(*c.fwd())
+    c.check_bwd(c.bwd())
+
+
+@TYPES
 @pytest.mark.parametrize("B,L", [(1, 1), (3, 64), (2, 201)])
 @pytest.mark.parametrize("heads", [(4, 4, 4), (4, 2, 2), (1, 1, 4), (2, 4, 1)], ids=str)
 def test_dense_batches_and_shared_heads(B, L, heads, dtype):
