@@ -583,9 +583,8 @@ int pdssm_project_wgrad(int32_t T, int32_t M, int32_t Dm, const uint16_t* dP, co
  * it; the rows that go into a state, weighted, as sums of three such numbers (24 bits; of two in a
  * backward pass for states that only row gradients are made of); and, where a row output is made of
  * them, states and weighted scores as sums of two.  Two are off by 2^-16 of the number, so a row output
- * is off by its own rounding and by 2^-16 of its terms' magnitudes.  q . k and its terms have to be in
- * the range of fp32.
- * Outputs are rounded to nearest even.
+ * is off by its own rounding (to nearest even) and by 2^-16 of its terms' magnitudes.  q . k and its
+ * terms have to be in the range of fp32.
  *
  * Sequences are as for the gated layers: S of T / S rows each, or cu [S+1], and
  * some may have no rows (h_final = h0, dh0 = dh_final, zeros where those are NULL).
