@@ -218,7 +218,7 @@ void add_role(AttnScan& n, const AttnRole& r, bool wide) {
     to.slices = slices(r.Do, wide);
     n.members += to.slices;
     const int64_t row = (int64_t)r.Do * (n.io == kRowBf16 && !r.out32 ? 2 : 4);  // bytes of a head's
-    to.past = n.T * n.H * row >= kPast && row % kPiece == 0 && reinterpret_cast<uintptr_t>(r.out) % kPiece == 0;
+    to.past = (int64_t)n.T * n.H * row >= kPast && row % kPiece == 0 && reinterpret_cast<uintptr_t>(r.out) % kPiece == 0;
 }
 
 // The states that segments begin with, of the roles in n.
